@@ -339,6 +339,124 @@ int gala_he_conv_outrot(const gala_ctx *ctx, void *stream, const gala_conv_plan 
                         const uint64_t *r, uint64_t mask_seed, uint64_t *ct_out, void *workspace, size_t workspace_bytes,
                         gala_opcount *counts);
 
+/* ---- a language model's steps between two linear layers (client side, device) --------------------------------
+ * The paper's protocol returns every linear layer's output to the parties, and a decoder layer's steps that have no
+ * weights come between two of them (Sec. II, Sec. III-A(3)).  A client that has its outputs in the clear -- its own
+ * share plus the server's, added mod p -- runs them here: positions are rotated into queries and keys, keys and
+ * values go into the client's cache, queries attend to it, and the last layer's outputs become a token.
+ * (Who may see a layer's output in the clear is the protocol's matter, not this library's.)
+ *
+ * Values: rows of numbers in device memory, a row's numbers contiguous, `stride` elements (>= 0) from one row to the
+ * next, so that parts of a fused projection are passed where they lie.  GALA_RESIDUE: uint64_t modulo the context's
+ * p, as gala_fc_unpack_share_batch writes them; a residue stands for unit times its representative nearest to zero,
+ * and a value becomes one by rounding it to the nearest unit, ties to even, held to the representatives there are
+ * (NaN becomes 0).  Elsewhere unit is ignored.  Every sum, maximum and rotation is carried in 32 bits or more. */
+typedef enum { GALA_F32 = 0, GALA_F16 = 1, GALA_BF16 = 2, GALA_RESIDUE = 3 } gala_type;
+typedef struct {
+    void *data;
+    int64_t stride;
+    int32_t type;                /* gala_type */
+    float unit;                  /* > 0 */
+} gala_values;
+
+/* The cache: pages of GALA_KV_BLOCK tokens in any order, all memory the caller's.  Of each page and head: the keys'
+ * codes, then the values' codes, gala_kv_cache_bytes(1, 1, head_dim) bytes together, and two scales; a code is a
+ * whole number in [-127, 127] that stands for code * scale.  With m = ceil(head_dim / 16) the code of channel d of
+ * token t of the page lies
+ *   keys:    at ((t/16)*m + d/16)*256 + (t%16)*16 + d%16
+ *   values:  at 64*16*m + (d/16)*1024 + ((t%16)/4)*256 + (d%16)*16 + (t/16)*4 + t%4
+ * and channels from head_dim to 16*m hold 0.  No length is kept: a page's rows behind a sequence's end are never
+ * looked at, and need no clearing. */
+#define GALA_KV_BLOCK 64
+typedef struct {
+    int32_t heads, head_dim;     /* heads of keys and values; 1 <= head_dim <= 256 */
+    int32_t pages;
+    int32_t reserved;
+    int8_t *codes;               /* pages x heads x (keys, values); 16-byte aligned */
+    float *scales;               /* pages x heads x 2 */
+} gala_kv_cache;
+size_t gala_kv_cache_bytes(int pages, int heads, int head_dim);
+
+/* A call's sequences.  Sequence b brings rows starts[b] .. starts[b+1]-1 of the values, the last tokens of its
+ * lens[b] (the new ones are counted): row i of n stands at position lens[b] - n + i.  Its token t lives in page
+ * table[b*table_stride + t/64].  starts, lens and table are device memory; max_new and max_len are upper bounds that
+ * the host knows (they size the launch; rows from max_new on are not processed, and attention sees no key from max_len
+ * on).  Tokens at negative positions, behind the table, or whose page number is not in [0, pages) are skipped: not
+ * written, not seen.  So pages that a window has left behind can be given back and their entries set to -1.
+ * No page may be written by two sequences of one call. */
+typedef struct {
+    int32_t count, max_new, max_len, table_stride;
+    const int32_t *starts;       /* count + 1 */
+    const int32_t *lens;         /* count */
+    const int32_t *table;        /* count x table_stride */
+} gala_kv_batch;
+
+/* Rotary positions.  table holds (cos, sin) of rot_dim/2 angles for each position (device memory).  The pair i of a
+ * head's first rot_dim channels -- (i, i + rot_dim/2), or (2i, 2i+1) where interleaved -- turns by its angle:
+ * (a, b) -> (a cos - b sin, b cos + a sin), every product and difference rounded to 32 bits once.  Other channels are
+ * left as they are.  A row whose position the table does not have comes out as NaN, and its key is not stored. */
+typedef struct {
+    const float *table;
+    int32_t positions, rot_dim, interleaved, reserved;
+} gala_rope;
+/* Fills a table in host memory (positions x rot_dim/2 x 2), angles in 64 bits: position * f_i, f_i = base^(-2i/rot_dim).
+ * For contexts longer than the model was trained on: GALA_ROPE_LINEAR divides positions by factor; GALA_ROPE_RAMP
+ * divides only the slow frequencies: f_i is kept where original * f_i / 2pi, its turns over the trained context, is
+ * at least `high`, divided by factor where it is at most `low`, and in between mixed linearly in the turns. */
+typedef enum { GALA_ROPE_PLAIN = 0, GALA_ROPE_LINEAR = 1, GALA_ROPE_RAMP = 2 } gala_rope_scaling;
+int gala_rope_table(int positions, int rot_dim, double base, int scaling, double factor, double original, double low,
+                    double high, float *table_host);
+
+/* New keys (rotated) and values into the cache, and the queries rotated on the way.  k, v: rows of heads x head_dim;
+ * q, q_out: rows of heads_q x head_dim (NULL both and heads_q = 0 for none; q_out is not GALA_RESIDUE and may be q
+ * where the types agree); k and v may both be NULL (queries alone); rope NULL leaves everything unrotated.
+ * A block's scale is max|x| / 127 over its tokens; where new tokens join earlier ones of a block the scale only
+ * grows, max(scale, max|x| / 127), and if it does the codes that are there are rounded to it.  A block that begins
+ * with a new token starts a scale of its own.  x is stored as rint(x * (1 / scale)) held to +-127.  Infinities are
+ * stored as +-127 and NaN as 0, and neither counts for the scale: 8 bits hold neither, and one of them would
+ * otherwise take the other tokens of its block along.  Asynchronous on `stream`; allocates nothing. */
+int gala_kv_append(const gala_ctx *ctx, void *stream, const gala_kv_cache *cache, const gala_kv_batch *batch,
+                   const gala_rope *rope, int heads_q, const gala_values *q, const gala_values *q_out,
+                   const gala_values *k, const gala_values *v);
+/* Reads rows of the cache back as the values they stand for: row i of sequence b gets position lens[b] - n + i, as
+ * above (the whole of a sequence with n = lens[b]).  Rows of skipped tokens are written as 0. */
+int gala_kv_export(const gala_ctx *ctx, void *stream, const gala_kv_cache *cache, const gala_kv_batch *batch,
+                   const gala_values *k_out, const gala_values *v_out);
+
+/* out = sum_j w_j v_j / sum_j w_j, w_j = exp(scale * q.k_j), over the keys that a query at position t sees: j <= t, and
+ * with window > 0 also j > t - window or j < sinks (the first tokens stay visible).  A query that sees nothing gives
+ * 0, one that holds a NaN or an infinity gives NaN (its own heads' rows alone).  q, out: rows of heads_q x head_dim,
+ * heads_q a multiple of the cache's heads; query head h reads head h / (heads_q / heads); out may be q where the
+ * types agree.  Queries enter the products as whole numbers of 16 bits of their row's largest, weights as 15 bits of
+ * the largest so far; 24 and 23 where q or out is GALA_F32 or GALA_RESIDUE: below the rounding of the outputs.
+ * workspace: device scratch, caller-owned, of gala_kv_attention_workspace bytes (0 for bad arguments).  Asynchronous,
+ * allocates nothing; results do not depend on timing.  Errors: GALA_EARG, GALA_ENOMEM (workspace too small), GALA_EHIP. */
+size_t gala_kv_attention_workspace(const gala_kv_cache *cache, const gala_kv_batch *batch, int heads_q, int window,
+                                   int sinks);
+int gala_kv_attention(const gala_ctx *ctx, void *stream, const gala_kv_cache *cache, const gala_kv_batch *batch,
+                      int heads_q, float scale, int window, int sinks, const gala_values *q, const gala_values *out,
+                      void *workspace, size_t workspace_bytes);
+
+/* One token a row from `rows` rows of `vocab` logits and uniform numbers u in [0, 1).  Order: larger logits first, of
+ * equal ones the lower index first.  A token's weight is exp((z - largest) * (1 / temperature)) in 32 bits, taken
+ * down to a whole multiple of 2^-40, so that sums are exact and in any order the same.  Kept are
+ *   top-k: the first top_k tokens (0 or less: all);
+ *   top-p: of those, each whose predecessors' weights add up to less than top_p times the weight of all of them
+ *          (1 and NaN: all);
+ *   min-p: of those, each whose weight is at least min_p (0 and NaN: all; above 1 counts as 1);
+ * and always the first.  The token is the lowest index at which the running sum of kept weights, in the order of
+ * indices, exceeds u times their sum.  temperature <= 0: the first token.  NaN logits are never drawn; a row with
+ * nothing but NaN and -infinity gives -1; where the largest is +infinity it alone has weight.  temperature, top_k,
+ * top_p, min_p, u: one number a row, device memory; each but u may be NULL (1, 0, 1, 0).  tokens: rows of int32_t. */
+typedef struct {
+    const float *temperature;
+    const int32_t *top_k;
+    const float *top_p, *min_p, *u;
+} gala_sampling;
+size_t gala_sample_workspace(int rows, int vocab);
+int gala_sample(const gala_ctx *ctx, void *stream, const gala_values *logits, int rows, int vocab,
+                const gala_sampling *how, int32_t *tokens, void *workspace, size_t workspace_bytes);
+
 /* ---- spatial tiling and stride for images larger than half a ciphertext (host) ---- */
 /* The paper assumes u_w*u_h fits a ciphertext (Sec. III-B(1), footnote) and never mentions stride.
  * Here an in_h x in_w image is cut into overlapping tile_h x tile_w tiles (tile_h*tile_w <= n/2) whose

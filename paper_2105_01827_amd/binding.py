@@ -51,6 +51,28 @@ class ConvPolyphase(C.Structure):
                 [(k, C.c_int32) for k in ("c_i_poly", "k_h_poly", "k_w_poly", "out_h", "out_w")])
 
 
+class ValuesArg(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("stride", C.c_int64), ("type", C.c_int32), ("unit", C.c_float)]
+
+
+class KvCacheArg(C.Structure):
+    _fields_ = [(k, C.c_int32) for k in ("heads", "head_dim", "pages", "reserved")] + [("codes", C.c_void_p),
+                                                                                      ("scales", C.c_void_p)]
+
+
+class KvBatchArg(C.Structure):
+    _fields_ = ([(k, C.c_int32) for k in ("count", "max_new", "max_len", "table_stride")] +
+                [(k, C.c_void_p) for k in ("starts", "lens", "table")])
+
+
+class RopeArg(C.Structure):
+    _fields_ = [("table", C.c_void_p)] + [(k, C.c_int32) for k in ("positions", "rot_dim", "interleaved", "reserved")]
+
+
+class SamplingArg(C.Structure):
+    _fields_ = [(k, C.c_void_p) for k in ("temperature", "top_k", "top_p", "min_p", "u")]
+
+
 class OpCount(C.Structure):
     _fields_ = [("perm", C.c_int64), ("decperm_in", C.c_int64), ("hstperm_in", C.c_int64),
                 ("scmult", C.c_int64), ("add", C.c_int64)]
@@ -130,6 +152,14 @@ SIGNATURES = {
     "gala_he_fc_hybrid": (_I, [_VP, _VP, _VP, _U64P, _I, _U64P, C.c_uint64, _U64P, _VP, C.c_size_t, C.POINTER(OpCount)]),
     "gala_he_conv_outrot_workspace": (C.c_size_t, [_VP, _I]),
     "gala_he_conv_outrot": (_I, [_VP, _VP, _VP, _U64P, _I, _U64P, C.c_uint64, _U64P, _VP, C.c_size_t, C.POINTER(OpCount)]),
+    "gala_kv_cache_bytes": (C.c_size_t, [_I, _I, _I]),
+    "gala_rope_table": (_I, [_I, _I, C.c_double, _I, C.c_double, C.c_double, C.c_double, C.c_double, _VP]),
+    "gala_kv_append": (_I, [_VP, _VP, _VP, _VP, _VP, _I, _VP, _VP, _VP, _VP]),
+    "gala_kv_export": (_I, [_VP, _VP, _VP, _VP, _VP, _VP]),
+    "gala_kv_attention_workspace": (C.c_size_t, [_VP, _VP, _I, _I, _I]),
+    "gala_kv_attention": (_I, [_VP, _VP, _VP, _VP, _I, C.c_float, _I, _I, _VP, _VP, _VP, C.c_size_t]),
+    "gala_sample_workspace": (C.c_size_t, [_I, _I]),
+    "gala_sample": (_I, [_VP, _VP, _VP, _I, _I, _VP, _VP, _VP, C.c_size_t]),
     "gala_conv_tiling_plan": (_I, [_VP, _I, _I, _I, _I, _I, C.POINTER(ConvTiling)]),
     "gala_conv_tile_extract": (_I, [C.POINTER(ConvTiling), _I, _U64P, _I, _U64P]),
     "gala_conv_tile_mask": (_I, [C.POINTER(ConvTiling), _I, _U64P, _I, _U64P]),
@@ -182,6 +212,39 @@ def _stream(s):
     if s is None:
         return None
     return C.c_void_p(s if isinstance(s, int) else s.cuda_stream)
+
+
+_TYPES = {"torch.float32": 0, "torch.float16": 1, "torch.bfloat16": 2, "torch.int64": 3, "torch.uint64": 3}
+_types = {}                                    # the same by the dtype itself, filled as dtypes are met
+
+
+def _values(t, unit):
+    """gala_values of a tensor: rows are its first dimension, the rest of a row has to be contiguous."""
+    kind = _types.get(t.dtype)
+    if kind is None:
+        if str(t.dtype) not in _TYPES:
+            raise TypeError(f"values are float32, float16, bfloat16, or residues in 64-bit words: got {t.dtype}")
+        kind = _types[t.dtype] = _TYPES[str(t.dtype)]
+    strides, step = t.stride(), 1
+    for size, stride in zip(reversed(t.shape[1:]), reversed(strides[1:])):
+        if size != 1 and stride != step:
+            raise ValueError("the values of a row have to be contiguous")
+        step *= size
+    return ValuesArg(t.data_ptr(), strides[0], kind, unit)
+
+
+def _words(t, dtype, what):
+    if str(t.dtype) != dtype or not t.is_contiguous():
+        raise TypeError(f"{what} has to be a contiguous {dtype} tensor")
+    return t.data_ptr()
+
+
+def rope_table(positions, rot_dim, base=10000.0, scaling=0, factor=1.0, original=0.0, low=0.0, high=0.0):
+    """(positions, rot_dim/2, 2) cosines and sines on the host; scaling 0 none, 1 linear, 2 the ramp over turns."""
+    out = np.empty((positions, rot_dim // 2, 2), np.float32)
+    _check(load().gala_rope_table(positions, rot_dim, base, scaling, factor, original, low, high,
+                                  out.ctypes.data_as(C.c_void_p)), "gala_rope_table")
+    return out
 
 
 def _rots(rots):
@@ -350,6 +413,24 @@ class Context:
 
     def fc_hybrid_plan(self, W):
         return FcHybridPlan(self, W)
+
+    # ---- a language model's last step
+    def sample_workspace_bytes(self, rows, vocab):
+        return int(self.lib.gala_sample_workspace(rows, vocab))
+
+    def sample(self, logits, u, tokens, workspace, workspace_bytes, temperature=None, top_k=None, top_p=None, min_p=None,
+               unit=1.0, stream=None):
+        """logits (rows, vocab) -> tokens (rows,) int32; the numbers a row are float32 tensors, top_k int32."""
+        rows, vocab = logits.shape
+        per_row = [("temperature", temperature, "torch.float32"), ("top_k", top_k, "torch.int32"),
+                   ("top_p", top_p, "torch.float32"), ("min_p", min_p, "torch.float32"), ("u", u, "torch.float32"),
+                   ("tokens", tokens, "torch.int32")]
+        for name, t, dtype in per_row:
+            if t is not None and t.numel() != rows:
+                raise ValueError(f"{name} has to have one number a row")
+        at = [None if t is None else _words(t, dtype, name) for name, t, dtype in per_row]
+        _check(self.lib.gala_sample(self.h, _stream(stream), C.byref(_values(logits, unit)), rows, vocab,
+                                    C.byref(SamplingArg(*at[:5])), at[5], _dev(workspace), workspace_bytes), "gala_sample")
 
 
 class SecretKey:
@@ -569,3 +650,66 @@ class ConvPlan:
         if getattr(self, "h", None):
             self.ctx.lib.gala_conv_plan_destroy(self.h)
             self.h = None
+
+
+class Rope:
+    """gala_rope: a (positions, rot_dim/2, 2) float32 table on the device and which channels make a pair."""
+
+    def __init__(self, table, interleaved=False):
+        self.table = table
+        self.arg = RopeArg(_words(table, "torch.float32", "the table"), table.shape[0], 2 * table.shape[1], int(interleaved), 0)
+        self.ref = C.byref(self.arg)
+
+
+class KvBatch:
+    """gala_kv_batch: the sequences of a call, int32 tensors on the device; max_new and max_len bound what they hold."""
+
+    def __init__(self, starts, lens, table, max_new, max_len):
+        self.tensors = starts, lens, table
+        if starts.numel() != lens.numel() + 1 or table.shape[0] != lens.numel():
+            raise ValueError("starts has one entry more than lens, and the table a row for each of them")
+        self.arg = KvBatchArg(lens.numel(), max_new, max_len, table.shape[1], _words(starts, "torch.int32", "starts"),
+                              _words(lens, "torch.int32", "lens"), _words(table, "torch.int32", "the table"))
+        self.ref = C.byref(self.arg)
+
+
+class KvCache:
+    """gala_kv_cache: 8-bit keys and values in pages of 64 tokens.  ``codes`` (pages, ...) int8 and ``scales``
+    (pages, heads, 2) float32 are the caller's, or are made here for ``pages`` pages."""
+
+    def __init__(self, ctx, heads, head_dim, codes=None, scales=None, pages=0):
+        import torch
+        self.ctx, self.heads, self.head_dim = ctx, heads, head_dim
+        if codes is None:
+            codes = torch.empty((pages, self.page_bytes(heads, head_dim)), dtype=torch.int8, device="cuda")
+            scales = torch.empty((pages, heads, 2), dtype=torch.float32, device="cuda")
+        if codes.numel() != codes.shape[0] * self.page_bytes(heads, head_dim) or scales.numel() != codes.shape[0] * heads * 2:
+            raise ValueError("codes and scales do not fit the heads and their dimension")
+        self.codes, self.scales = codes, scales
+        self.arg = KvCacheArg(heads, head_dim, codes.shape[0], 0, _words(codes, "torch.int8", "codes"),
+                              _words(scales, "torch.float32", "scales"))
+        self.ref = C.byref(self.arg)
+
+    @staticmethod
+    def page_bytes(heads, head_dim):
+        return int(load().gala_kv_cache_bytes(1, heads, head_dim))
+
+    def append(self, batch, k, v, q=None, q_out=None, rope=None, unit=1.0, stream=None):
+        """k, v (rows, heads, head_dim) into the cache; q (rows, heads_q, head_dim) rotated into q_out."""
+        heads_q = 0 if q is None else q[:1].numel() // self.head_dim
+        _check(self.ctx.lib.gala_kv_append(self.ctx.h, _stream(stream), self.ref, batch.ref, None if rope is None else rope.ref,
+                                           heads_q, *(None if t is None else C.byref(_values(t, unit)) for t in (q, q_out, k, v))),
+               "gala_kv_append")
+
+    def export(self, batch, k_out, v_out, unit=1.0, stream=None):
+        _check(self.ctx.lib.gala_kv_export(self.ctx.h, _stream(stream), self.ref, batch.ref, C.byref(_values(k_out, unit)),
+                                           C.byref(_values(v_out, unit))), "gala_kv_export")
+
+    def attention_workspace_bytes(self, batch, heads_q, window=0, sinks=0):
+        return int(self.ctx.lib.gala_kv_attention_workspace(self.ref, batch.ref, heads_q, window, sinks))
+
+    def attention(self, batch, q, out, scale, workspace, workspace_bytes, window=0, sinks=0, unit=1.0, stream=None):
+        """q (rows, heads_q, head_dim) -> out of the same shape."""
+        _check(self.ctx.lib.gala_kv_attention(self.ctx.h, _stream(stream), self.ref, batch.ref, q[:1].numel() // self.head_dim,
+                                              scale, window, sinks, C.byref(_values(q, unit)), C.byref(_values(out, unit)),
+                                              _dev(workspace), workspace_bytes), "gala_kv_attention")

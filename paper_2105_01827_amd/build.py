@@ -9,8 +9,9 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libgala_hip.so")
 SOURCES = ["gala_host.cpp", "gala_api.cpp", "gala_kernels.hip", "gala_conv_mfma.hip",
+           "gala_decode_api.cpp", "gala_kv.hip", "gala_attention.hip", "gala_sample.hip",
            "gala_ring1024.hip", "gala_ring2048.hip", "gala_ring4096.hip", "gala_ring8192.hip"]
-HEADERS = ["gala_internal.h", "gala_ring_impl.h", "modarith.h", os.path.join("..", "..", "include", "gala.h")]
+HEADERS = ["gala_internal.h", "gala_ring_impl.h", "gala_decode.h", "modarith.h", os.path.join("..", "..", "include", "gala.h")]
 # packed-FP32 instructions are switched off for every device compile on the test machines
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-pthread", "-Wno-unused-value", "-Wno-unused-command-line-argument",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops"]

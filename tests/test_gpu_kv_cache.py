@@ -1,0 +1,251 @@
+"""Appending to the paged 8-bit cache with positions rotated in, and reading it back, against the definition in 64 bits."""
+import numpy as np
+import pytest
+import torch
+
+from paper_2105_01827_amd import binding, workloads as wl
+from tests import decode_reference as ref
+
+pytestmark = pytest.mark.gpu
+TYPES = {"f32": torch.float32, "f16": torch.float16, "bf16": torch.bfloat16, "residue": torch.int64}
+UNIT = 2.0 ** -12
+
+
+@pytest.fixture(scope="module")
+def ctx():
+    par = wl.DEFAULT
+    return binding.Context(par.n, par.q, par.p, par.gadget_bits)
+
+
+def _values(gen, kind, *shape):
+    x = torch.randn(*shape, generator=gen)
+    if kind == "residue":
+        return torch.round(x / UNIT).to(torch.int64).remainder(wl.P).cuda()
+    return x.to(TYPES[kind]).cuda()
+
+
+def _plain(x):
+    return ref.centred(x.cpu().numpy(), wl.P, UNIT) if x.dtype == torch.int64 else x.cpu().double().numpy()
+
+
+def _int32(v):
+    return torch.tensor(v, dtype=torch.int32, device="cuda")
+
+
+class Sequences:
+    """A cache of its own, and what it should hold: codes and scales by the definition, in 64 bits."""
+
+    def __init__(self, ctx, heads, dim, batch, blocks, seed, spare=2):
+        self.gen = torch.Generator().manual_seed(seed)
+        self.heads, self.dim, self.batch = heads, dim, batch
+        pages = batch * blocks + spare
+        self.cache = binding.KvCache(ctx, heads, dim, pages=pages)
+        self.cache.codes.fill_(77)                       # what lies behind a sequence's end is nobody's
+        self.cache.scales.fill_(float("nan"))
+        self.table = torch.randperm(pages, generator=self.gen)[:batch * blocks].view(batch, blocks).to(torch.int32)
+        self.codes = np.zeros((2, batch, blocks * 64, heads, dim))
+        self.scales = np.zeros((2, batch, blocks, heads))
+        self.lens = [0] * batch
+
+    def step(self, new):
+        self.lens = [a + n for a, n in zip(self.lens, new)]
+        starts = np.concatenate([[0], np.cumsum(new)])
+        return starts, binding.KvBatch(_int32(starts.tolist()), _int32(self.lens), self.table.cuda(), max(new), max(self.lens))
+
+    def expect(self, starts, k, v):
+        """k (rotated) and v in 64 bits into the definition's own cache; checks the codes that the device has"""
+        places = ref.code_places(self.dim)
+        got = self.cache.codes.cpu().numpy().reshape(-1, self.heads, ref.head_bytes(self.dim))
+        scales = self.cache.scales.cpu().numpy().astype(np.float64)
+        for b in range(self.batch):
+            n = starts[b + 1] - starts[b]
+            first = self.lens[b] - n
+            for block in range(first // 64, -(-self.lens[b] // 64) if n else 0):
+                page = int(self.table[b, block])
+                lo, hi = max(first, block * 64), min(self.lens[b], block * 64 + 64)
+                for which, x in enumerate((k, v)):
+                    rows = x[starts[b] + lo - first:starts[b] + hi - first]
+                    for h in range(self.heads):
+                        old = self.scales[which, b, block, h] if lo > block * 64 else 0.0
+                        scale = max(old, np.abs(rows[:, h]).max() / 127)
+                        # rotations and the division by 127 in 32 bits
+                        assert abs(scales[page, h, which] - scale) <= 2.0 ** -20 * scale
+                        held = got[page, h][places[which]].astype(np.float64)
+                        if lo > block * 64:
+                            before = self.codes[which, b, block * 64:lo, h] * (old / scale if scale else 0)
+                            assert np.abs(held[:lo - block * 64] - before).max() <= 0.5 + 1e-3
+                            if scale == old:
+                                assert np.array_equal(held[:lo - block * 64], self.codes[which, b, block * 64:lo, h])
+                        if scale:
+                            assert np.abs(held[lo - block * 64:hi - block * 64] - rows[:, h] / scale).max() <= 0.5 + 1e-3
+                        assert np.abs(held[:hi - block * 64]).max() <= 127
+                        self.codes[which, b, block * 64:hi, h] = held[:hi - block * 64]
+                        self.scales[which, b, block, h] = scales[page, h, which]
+
+
+@pytest.mark.parametrize("kind,dim,rot,interleaved,heads,group", [
+    ("f32", 64, 64, False, 3, 2), ("bf16", 128, 128, False, 2, 4), ("f16", 80, 40, True, 5, 1), ("residue", 128, 64, True, 2, 3),
+    ("residue", 33, 32, False, 1, 1), ("bf16", 256, 256, True, 2, 2), ("f32", 200, 2, False, 1, 3), ("f16", 1, 0, False, 2, 1),
+    ("f16", 16, 16, False, 1, 8), ("bf16", 96, 96, False, 4, 5), ("residue", 64, 0, False, 7, 1), ("f16", 192, 96, False, 1, 2)])
+def test_append_and_export(ctx, kind, dim, rot, interleaved, heads, group):
+    """Prompts of several lengths, then single tokens, then a few at once, over block edges; part of a fused projection."""
+    s = Sequences(ctx, heads, dim, 3, 5, seed=dim + rot)
+    rope = table = None
+    if rot:
+        table = binding.rope_table(320, rot)
+        rope = binding.Rope(torch.from_numpy(table).cuda(), interleaved)
+    for new in [(70, 1, 64), (1, 1, 1), (0, 62, 3), (5, 64, 1), (1, 1, 130), (130, 0, 0)]:
+        before = list(s.lens)
+        starts, batch = s.step(new)
+        total = int(starts[-1])
+        fused = _values(s.gen, kind, total, group * heads + 2 * heads, dim)
+        fused[:, group * heads:] *= 1 if kind == "residue" else (3 if new[0] == 5 else 1)          # scales that grow
+        q, k, v = fused.split([group * heads, heads, heads], 1)
+        out = torch.float32 if kind == "residue" else TYPES[kind]
+        q_out = torch.full((total, group * heads, dim), 7.0, dtype=out, device="cuda")
+        s.cache.append(batch, k, v, q=q, q_out=q_out, rope=rope, unit=UNIT)
+        positions = np.concatenate([np.arange(a, a + n) for a, n in zip(before, new)])
+        plain = [_plain(x) for x in (q, k, v)]
+        turned = [ref.rotate(x, table, positions, interleaved) if rot else x for x in plain[:2]]
+        # two products and a sum in 32 bits, then one rounding to the output's type
+        eps = ref.UNIT_ROUNDOFF[str(out).replace("torch.", "")]
+        assert (np.abs(q_out.cpu().double().numpy() - turned[0]) <= 2.0 ** -21 * np.abs(plain[0]).max() + eps * np.abs(turned[0])).all()
+        s.expect(starts, turned[1], plain[2])
+    # everything back, whole sequences, as the values that codes and scales stand for
+    lens = s.lens
+    starts = np.concatenate([[0], np.cumsum(lens)])
+    whole = binding.KvBatch(_int32(starts.tolist()), _int32(lens), s.table.cuda(), max(lens), max(lens))
+    for kind_out in ("f32", "f16", "bf16", "residue"):
+        back = [torch.zeros(int(starts[-1]), heads, dim, dtype=TYPES[kind_out], device="cuda") for _ in range(2)]
+        s.cache.export(whole, *back, unit=UNIT)
+        for which, x in enumerate(back):
+            want = np.concatenate([(s.codes[which, b].reshape(-1, 64, heads, dim) * s.scales[which, b][:, None, :, None])
+                                   .reshape(-1, heads, dim)[:n] for b, n in enumerate(lens)])
+            got = _plain(x)
+            slack = UNIT / 2 if kind_out == "residue" else 0
+            eps = ref.UNIT_ROUNDOFF.get(str(x.dtype).replace("torch.", ""), 0) + 2.0 ** -23
+            tiny = 2.0 ** -24 if kind_out == "f16" else 0          # half's smallest step
+            assert (np.abs(got - want) <= eps * np.abs(want) + slack + tiny).all()
+
+
+def test_queries_alone_and_in_place(ctx):
+    heads, dim, group = 2, 64, 3
+    s = Sequences(ctx, heads, dim, 2, 3, seed=5)
+    starts, batch = s.step((90, 17))
+    rope = binding.Rope(torch.from_numpy(binding.rope_table(100, 32)).cuda(), True)
+    x = _values(s.gen, "bf16", 107, heads * group, dim)
+    out = torch.empty_like(x)
+    codes = s.cache.codes.clone()
+    s.cache.append(batch, None, None, q=x, q_out=out, rope=rope)
+    assert torch.equal(codes, s.cache.codes) and bool(s.cache.scales.isnan().all())
+    same = x.clone()
+    s.cache.append(batch, None, None, q=same, q_out=same, rope=rope)
+    assert torch.equal(same, out) and not torch.equal(same, x)
+
+
+def test_one_row_for_all_and_rows_apart(ctx):
+    """A row stride of zero repeats one row; a stride beyond the row leaves the gap alone."""
+    heads, dim = 2, 48
+    s = Sequences(ctx, heads, dim, 1, 2, seed=6)
+    starts, batch = s.step((70,))
+    one = _values(s.gen, "f32", 1, heads, dim)
+    wide = torch.full((70, heads * dim + 5), 3.0, device="cuda")
+    q_out = wide[:, :heads * dim].view(70, heads, dim)
+    s.cache.append(batch, one.expand(70, -1, -1), one.expand(70, -1, -1), q=one.expand(70, -1, -1), q_out=q_out)
+    s.expect(starts, *(_plain(one.expand(70, -1, -1)) for _ in range(2)))
+    assert torch.equal(q_out, one.expand(70, -1, -1)) and bool((wide[:, heads * dim:] == 3).all())
+
+
+def test_tokens_without_a_place_are_skipped(ctx):
+    """Pages that are not there, positions that the rope table does not have, rows beyond max_new, more rows than tokens."""
+    heads, dim = 1, 32
+    s = Sequences(ctx, heads, dim, 3, 3, seed=7)
+    s.table[0, 1], s.table[1, 0] = -1, s.cache.codes.shape[0]
+    starts, batch = s.step((150, 70, 100))
+    batch = binding.KvBatch(batch.tensors[0], _int32([150, 70, 90]), s.table.cuda(), 140, 150)
+    rope = binding.Rope(torch.from_numpy(binding.rope_table(60, 32)).cuda())
+    k, v = (_values(s.gen, "f32", 320, heads, dim) for _ in range(2))
+    q_out = torch.full((320, heads, dim), 7.0, device="cuda")
+    s.cache.append(batch, k, v, q=k, q_out=q_out, rope=rope)
+    got = q_out.cpu().numpy()
+    positions = np.concatenate([np.arange(150), np.arange(70), np.arange(-10, 90)])
+    inside = (positions >= 0) & (positions < 60)
+    taken = np.ones(320, bool)
+    taken[140:150] = False
+    assert np.isnan(got[~inside & taken]).all() and not np.isnan(got[inside]).any() and (got[140:150] == 7).all()
+    back = [torch.full((320, heads, dim), 7.0, device="cuda") for _ in range(2)]
+    s.cache.export(batch, *back)
+    vals = back[1].cpu().numpy()
+    plain = _plain(v)
+    absent = np.zeros(320, bool)
+    absent[64:128] = absent[150:150 + 64] = absent[220:230] = True
+    assert (vals[absent & taken] == 0).all() and (vals[140:150] == 7).all()
+    there = ~absent & taken
+    assert np.abs(vals[there] - plain[there]).max() <= np.abs(plain).max() / 127 * 0.51
+    untouched = [int(p) for p in set(range(s.cache.codes.shape[0])) - set(s.table.flatten().tolist())]
+    assert bool((s.cache.codes[untouched] == 77).all())
+
+
+def test_infinities_and_nan(ctx):
+    heads, dim = 2, 64
+    s = Sequences(ctx, heads, dim, 1, 1, seed=8)
+    starts, batch = s.step((20,))
+    k = _values(s.gen, "f32", 20, heads, dim)
+    k[3, 0, 5], k[4, 0, 6], k[5, 1, 7] = float("inf"), float("-inf"), float("nan")
+    v = torch.zeros_like(k)                               # a block of zeros: scale 0
+    v[7, 1, 2] = float("nan")
+    s.cache.append(batch, k, v)
+    want = k.clone()
+    finite = torch.where(k.isfinite(), k, 0.0).abs().amax((0, 2))
+    want[3, 0, 5], want[4, 0, 6], want[5, 1, 7] = finite[0], -finite[0], 0
+    back = [torch.empty_like(k) for _ in range(2)]
+    s.cache.export(batch, *back)
+    assert float((back[0] - want).abs().max()) <= float(finite.max()) / 127 * 0.51
+    assert bool((back[1] == 0).all())
+
+
+def test_a_block_that_begins_anew_forgets_its_scale(ctx):
+    s = Sequences(ctx, 1, 16, 1, 1, seed=9)
+    big, small = (torch.full((1, 1, 16), x, device="cuda") for x in (1000.0, 1.0))
+    for x in (big, small):                                # the sequence starts over in the same page
+        s.lens = [0]
+        starts, batch = s.step((1,))
+        s.cache.append(batch, x, x)
+    assert float(s.cache.scales[int(s.table[0, 0]), 0, 0]) == pytest.approx(1 / 127, rel=1e-6)
+
+
+def test_empty_calls(ctx):
+    s = Sequences(ctx, 1, 16, 2, 1, seed=10)
+    codes = s.cache.codes.clone()
+    starts, batch = s.step((0, 0))
+    none = torch.empty(0, 1, 16, device="cuda")
+    s.cache.append(batch, none, none) if none.data_ptr() else None
+    nobody = binding.KvBatch(_int32([0]), _int32([]), torch.empty(0, 1, dtype=torch.int32, device="cuda"), 0, 0)
+    one = torch.ones(1, 1, 16, device="cuda")
+    s.cache.append(nobody, one, one)
+    s.cache.append(batch, one, one)
+    assert torch.equal(codes, s.cache.codes)
+
+
+def test_another_stream_and_a_graph(ctx):
+    heads, dim = 4, 128
+    s = Sequences(ctx, heads, dim, 2, 2, seed=11)
+    starts, batch = s.step((65, 64))
+    rope = binding.Rope(torch.from_numpy(binding.rope_table(128, 128)).cuda())
+    x = _values(s.gen, "bf16", 129, 3 * heads, dim)
+    q, k, v = x.split(heads, 1)
+    out = torch.empty_like(q.contiguous())
+    s.cache.append(batch, k, v, q=q, q_out=out, rope=rope)
+    want, codes = out.clone(), s.cache.codes.clone()
+    stream = torch.cuda.Stream()
+    stream.wait_stream(torch.cuda.current_stream())
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=stream):
+        s.cache.append(batch, k, v, q=q, q_out=out, rope=rope, stream=torch.cuda.current_stream())
+    for _ in range(3):
+        out.zero_(), s.cache.codes.zero_()
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        live = codes != 77
+        assert torch.equal(out, want) and torch.equal(s.cache.codes[live], codes[live])
