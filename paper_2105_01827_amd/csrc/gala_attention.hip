@@ -1,6 +1,7 @@
 // Attention of a batch's queries over the paged 8-bit cache.
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
 #include <type_traits>
 
 #include "gala_decode.h"
@@ -9,78 +10,369 @@ using namespace gala;
 
 namespace {
 
-// One wavefront: one query head of one token.  A lane takes a token of a block for the scores, and channels for the sum.
-template <int TYPE, int OUT>
-__global__ __launch_bounds__(64) void kv_attention_kernel(KvArgs kv, int heads_q, float scale, int window, int sinks, Values q, Values out) {
-    __shared__ float qs[kMaxHeadDim], ps[64];
-    const int unit = blockIdx.x, hq = unit % heads_q, bi = unit / heads_q, b = bi / kv.max_new, i = bi % kv.max_new;
-    const int start = kv.starts[b], n = kv.starts[b + 1] - start, lane = threadIdx.x;
-    if (i >= n) return;
-    const int at = kv.lens[b] - n + i, h = hq / (heads_q / kv.heads), dim = kv.dim;
-    const long row = start + i;
-    bool bad = false;
-    for (int d = lane; d < kv.dim16 * 16; d += 64) {
-        const float x = d < dim ? load_value<TYPE>(q, row, hq * dim + d) : 0.0f;
-        bad |= !(fabsf(x) < INFINITY);
-        qs[d] = x;
+typedef int v4i __attribute__((ext_vector_type(4)));
+typedef float v4f __attribute__((ext_vector_type(4)));
+
+constexpr int kWaves = 4;            // of a workgroup
+constexpr int kColumns = 16;         // queries that a wavefront's products take at once
+constexpr float kLog2E = 1.4426950408889634f;
+
+struct Attention {
+    KvArgs kv;
+    Values q, out;
+    int heads_q, group;              // group: query heads of a head of the cache
+    float scale;
+    int window, sinks;
+    int tiles, splits, columns;      // column tiles of a head, shares of its keys, columns of a tile that are kept
+    float *sums, *stats;             // of every share: columns x dim, and columns x (largest, sum)
+};
+
+// The blocks that the queries of one column tile see: the first tokens', then the window's.
+struct Seen {
+    int start, n, col0, cols;        // first row, rows, first column and columns of the tile
+    int at_lo, at_hi;                // positions of the tile's queries
+    int first, begin, total;         // first: blocks of first tokens in front of `begin`
+
+    __device__ int block(int u) const { return u < first ? u : begin + (u - first); }
+};
+__device__ __forceinline__ Seen seen_by(const Attention &a, int b, int tile) {
+    Seen s;
+    s.start = a.kv.starts[b];
+    const int all = a.kv.starts[b + 1] - s.start, len = a.kv.lens[b];
+    s.n = min(all, a.kv.max_new);
+    s.col0 = tile * kColumns;
+    s.cols = max(0, min(kColumns, s.n * a.group - s.col0));
+    s.at_lo = len - all + s.col0 / a.group;
+    s.at_hi = len - all + (s.col0 + max(s.cols, 1) - 1) / a.group;
+    const int end = min(s.at_hi + 1, min(a.kv.max_len, a.kv.table_stride * kKvBlock));       // keys from here on are not seen
+    const int last = end > 0 ? (end + kKvBlock - 1) / kKvBlock : 0;
+    s.begin = a.window ? min(max(0, s.at_lo - a.window + 1) / kKvBlock, last) : 0;
+    s.first = min((int)min((long)a.sinks + kKvBlock - 1, 0x7fffffffl) / kKvBlock, s.begin);
+    s.total = s.cols ? s.first + last - s.begin : 0;
+    return s;
+}
+// blocks of a share
+__device__ __forceinline__ int share_of(int total, int splits) {
+    const int each = (total + splits - 1) / splits;
+    return (each + kWaves - 1) / kWaves * kWaves;
+}
+
+__device__ __forceinline__ float load_any(const Values &v, long row, int column) {
+    switch (v.type) {
+        case GALA_F32: return load_value<GALA_F32>(v, row, column);
+        case GALA_F16: return load_value<GALA_F16>(v, row, column);
+        case GALA_BF16: return load_value<GALA_BF16>(v, row, column);
+        default: return load_value<GALA_RESIDUE>(v, row, column);
     }
-    bad = __any(bad);
-    __syncthreads();
-    float top = -INFINITY, sum = 0, acc[4] = {0, 0, 0, 0};
-    const int end = min(at + 1, kv.max_len);
-    for (int block = 0; block * kKvBlock < end; ++block) {
-        const int t = block * kKvBlock + lane, last = block * kKvBlock + 63;
-        if (window && last <= at - window && block * kKvBlock >= sinks) continue;
-        const int page = page_of(kv, b, block);
+}
+__device__ __forceinline__ void store_any(const Values &v, long row, int column, float x) {
+    switch (v.type) {
+        case GALA_F32: store_value<GALA_F32>(v, row, column, x); break;
+        case GALA_F16: store_value<GALA_F16>(v, row, column, x); break;
+        case GALA_BF16: store_value<GALA_BF16>(v, row, column, x); break;
+        default: store_value<GALA_RESIDUE>(v, row, column, x); break;
+    }
+}
+
+// ND words -> ND planes of balanced base-256 digits of four numbers: the numbers come with 128 added to each digit but
+// the highest, as the low bytes of their words
+template <int ND>
+__device__ __forceinline__ void planes(const u32 (&w)[4], int at, v4i (&to)[ND]) {
+    const u32 ab = __builtin_amdgcn_perm(w[1], w[0], 0x05010400), cd = __builtin_amdgcn_perm(w[3], w[2], 0x05010400);
+    const u32 low = __builtin_amdgcn_perm(cd, ab, 0x05040100) ^ 0x80808080u, mid = __builtin_amdgcn_perm(cd, ab, 0x07060302);
+    to[0][at] = (int)low;
+    if constexpr (ND == 2) {
+        to[1][at] = (int)mid;
+    } else {
+        to[1][at] = (int)(mid ^ 0x80808080u);
+        const u32 ab2 = __builtin_amdgcn_perm(w[1], w[0], 0x0c0c0602), cd2 = __builtin_amdgcn_perm(w[3], w[2], 0x0c0c0602);
+        to[2][at] = (int)__builtin_amdgcn_perm(cd2, ab2, 0x05040100);
+    }
+}
+template <int ND>
+struct Digits;
+// the largest number, and 2^23 with 128 in every digit but the highest: added to a float below 2^23 it leaves the
+// float's nearest whole number, offset so, in the low bits
+template <>
+struct Digits<2> { static constexpr float most = 127 * 256.0f, offset = 8388608.0f + 128; };
+template <>
+struct Digits<3> { static constexpr float most = 127 * 65536.0f, offset = 8388608.0f + 128 * 257; };
+
+// the number whose digits' products were added up apart
+template <int ND>
+__device__ __forceinline__ float joined(const v4i (&acc)[ND], int r) {
+    const int low = acc[0][r] + (acc[1][r] << 8);
+    if constexpr (ND == 2)
+        return (float)low;
+    else
+        return fmaf((float)acc[ND - 1][r], 65536.0f, (float)low);
+}
+
+// Both products run on the matrix cores as exact sums of 8-bit products: the cache's codes as they lie in memory by
+// the base-256 digits of the queries and of the weights (NC x 64 channels; ND digits).  Of a block's scores a lane has
+// 16 of one column's, and they are the very weights that it hands to the second product, because the values' codes
+// lie in that order of tokens.  So a block goes from memory to the sums without LDS or an exchange between lanes, but
+// for the largest score.  A wavefront has blocks of its own; a workgroup's wavefronts are joined at the end.
+template <int NC, int ND>
+__global__ __launch_bounds__(64 * kWaves) void kv_attention_kernel(Attention a) {
+    constexpr int NV = 4 * NC;
+    __shared__ float sums[kWaves][kColumns][NV * 16 + 1];
+    __shared__ float stats[kWaves][kColumns][2];
+    const KvArgs &kv = a.kv;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 15, part = lane >> 4;
+    int unit = blockIdx.x;
+    const int split = unit % a.splits;
+    unit /= a.splits;
+    const int tile = unit % a.tiles;
+    unit /= a.tiles;
+    const int h = unit % kv.heads, b = unit / kv.heads;
+    const Seen s = seen_by(a, b, tile);
+    if (!s.cols) return;
+    const int share = share_of(s.total, a.splits), from = split * share, to = min(s.total, from + share);
+    if (split && from >= s.total) return;
+    // the column's query: digits, and what one unit of them is worth
+    const int c = s.col0 + min(col, s.cols - 1), qi = c / a.group, g = c % a.group;
+    const long row = s.start + qi;
+    const int at = s.at_lo - s.col0 / a.group + qi, hq = h * a.group + g;
+    v4i qd[NC][ND];
+    float unit_q;
+    bool bad;
+    {
+        float x[NC][16], most = 0;
+        bool fine = true;
+#pragma unroll
+        for (int k = 0; k < NC; ++k)
+#pragma unroll
+            for (int j = 0; j < 16; ++j) {
+                const int d = k * 64 + part * 16 + j;
+                x[k][j] = d < kv.dim ? load_any(a.q, row, hq * kv.dim + d) : 0.0f;
+                most = fmaxf(most, fabsf(x[k][j]));
+                fine &= fabsf(x[k][j]) < INFINITY;
+            }
+        most = fmaxf(most, __shfl_xor(most, 16));
+        most = fmaxf(most, __shfl_xor(most, 32));
+        int all = fine;
+        all &= __shfl_xor(all, 16);
+        all &= __shfl_xor(all, 32);
+        bad = !all;
+        const bool some = most > 0 && !bad;
+        // a power of two first: the reciprocal of a tiny number would be infinite
+        const int e = some ? ilogbf(most) : 0;
+        const float scaled = ldexpf(some ? most : 1.0f, -e), mul = Digits<ND>::most / scaled * (a.scale < 0 ? -1.0f : 1.0f);
+        unit_q = ldexpf(scaled / Digits<ND>::most, e) * fabsf(a.scale) * kLog2E;
+#pragma unroll
+        for (int k = 0; k < NC; ++k)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                u32 w[4];
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    const int v = some ? (int)rintf(ldexpf(x[k][4 * j + r], -e) * mul) : 0;
+                    w[r] = (u32)(v + (ND == 2 ? 128 : 128 * 257));
+                }
+                planes<ND>(w, j, qd[k]);
+            }
+    }
+    v4f o[NV];
+#pragma unroll
+    for (int j = 0; j < NV; ++j) o[j] = v4f{0, 0, 0, 0};
+    float top = -INFINITY, sum = 0;
+    const size_t head_bytes = kv_head_bytes(kv.dim16);
+    for (int u = from + wave; u < to; u += kWaves) {
+        const int block = s.block(u), page = page_of(kv, b, block);
         if (page < 0) continue;
-        const signed char *codes = kv.codes + ((long)page * kv.heads + h) * kv_head_bytes(kv.dim16);
-        const float *scales = kv.scales + ((long)page * kv.heads + h) * 2;
-        const bool seen = t < end && (!window || t > at - window || t < sinks);
-        float dot = 0;
-        for (int d = 0; d < kv.dim16 * 16; ++d)
-            dot += qs[d] * (float)codes[((lane >> 4) * kv.dim16 + (d >> 4)) * 256 + (lane & 15) * 16 + (d & 15)];
-        const float s = seen ? dot * scales[0] * scale : -INFINITY;
-        float m = s;
-        for (int k = 32; k; k >>= 1) m = fmaxf(m, __shfl_xor(m, k));
-        if (m == -INFINITY) continue;
-        m = fmaxf(m, top);
-        const float was = expf(top - m), p = expf(s - m);
-        float all = p;
-        for (int k = 32; k; k >>= 1) all += __shfl_xor(all, k);
-        sum = sum * was + all;
-        top = m;
-        __syncthreads();
-        ps[lane] = p * scales[1];
-        __syncthreads();
-        for (int k = 0; k < 4; ++k) {
-            const int d = lane + 64 * k;
-            if (d >= dim) break;
-            float a = 0;
-            for (int u = 0; u < 64; ++u)
-                a += ps[u] * (float)codes[kKvBlock * 16 * kv.dim16 + (d >> 4) * 1024 + ((u & 15) >> 2) * 256 + (d & 15) * 16 + (u >> 4) * 4 + (u & 3)];
-            acc[k] = acc[k] * was + a;
+        const signed char *codes = kv.codes + ((size_t)page * kv.heads + h) * head_bytes;
+        const float *scales = kv.scales + ((size_t)page * kv.heads + h) * 2;
+        const float unit_s = unit_q * scales[0], unit_v = scales[1] * (1.0f / Digits<ND>::most);
+        v4i keys[4][NC], values[NV];
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int k = 0; k < NC; ++k)       // channels beyond the head's meet digits of 0; what is read there is the head's
+                keys[i][k] = *(const v4i *)(codes + (size_t)(i * kv.dim16 + k * 4 + part) * 256 + col * 16);
+#pragma unroll
+        for (int j = 0; j < NV; ++j)
+            if (j < kv.dim16) values[j] = *(const v4i *)(codes + (size_t)kKvBlock * 16 * kv.dim16 + j * 1024 + lane * 16);
+        float t[16];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            v4i acc[ND];
+#pragma unroll
+            for (int n = 0; n < ND; ++n) {
+                acc[n] = v4i{0, 0, 0, 0};
+#pragma unroll
+                for (int k = 0; k < NC; ++k) acc[n] = __builtin_amdgcn_mfma_i32_16x16x64_i8(keys[i][k], qd[k][n], acc[n], 0, 0, 0);
+            }
+#pragma unroll
+            for (int r = 0; r < 4; ++r) t[4 * i + r] = joined<ND>(acc, r) * unit_s;
+        }
+        const int t0 = block * kKvBlock;
+        if (t0 + 63 > s.at_lo || t0 + 64 > kv.max_len || (a.window && t0 <= s.at_hi - a.window)) {
+            // keys of the block by their distance from the lane's first one; no branches between them
+            const int own = t0 + part * 4, hi = min(at, kv.max_len - 1) - own;
+            const int lo = a.window ? at - a.window + 1 - own : -kKvBlock, sinks = a.window ? a.sinks - own : 0;
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    const int e = i * 16 + r;
+                    t[4 * i + r] = (e <= hi) & ((e >= lo) | (e < sinks)) ? t[4 * i + r] : -INFINITY;
+                }
+        }
+        float most = t[0];
+#pragma unroll
+        for (int i = 1; i < 16; ++i) most = fmaxf(most, t[i]);
+        most = fmaxf(most, __shfl_xor(most, 16));
+        most = fmaxf(most, __shfl_xor(most, 32));
+        if (__any(most > top)) {
+            const float now = fmaxf(top, most), was = now > top ? __builtin_amdgcn_exp2f(top - now) : 1.0f;
+            top = now;
+            sum *= was;
+#pragma unroll
+            for (int j = 0; j < NV; ++j) o[j] *= was;
+        }
+        const float base = top == -INFINITY ? 0.0f : top;
+        v4i w[ND];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            u32 word[4];
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const float p = __builtin_amdgcn_exp2f(t[4 * i + r] - base);
+                sum += p;
+                word[r] = __float_as_uint(fmaf(p, Digits<ND>::most, Digits<ND>::offset));
+            }
+            planes<ND>(word, i, w);
+        }
+#pragma unroll
+        for (int j = 0; j < NV; ++j)
+            if (j < kv.dim16) {
+                v4i acc[ND];
+#pragma unroll
+                for (int n = 0; n < ND; ++n) acc[n] = __builtin_amdgcn_mfma_i32_16x16x64_i8(values[j], w[n], v4i{0, 0, 0, 0}, 0, 0, 0);
+#pragma unroll
+                for (int r = 0; r < 4; ++r) o[j][r] = fmaf(joined<ND>(acc, r), unit_v, o[j][r]);
+            }
+    }
+    // the wavefronts' sums in one
+    sum += __shfl_xor(sum, 16);
+    sum += __shfl_xor(sum, 32);
+#pragma unroll
+    for (int j = 0; j < NV; ++j)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) sums[wave][col][j * 16 + part * 4 + r] = o[j][r];
+    if (part == 0) stats[wave][col][0] = bad ? __builtin_nanf("") : top, stats[wave][col][1] = sum;
+    __syncthreads();
+    const long place = (((long)b * kv.heads + h) * a.tiles + tile) * a.splits + split;
+    for (int e = threadIdx.x; e < s.cols * kv.dim; e += 64 * kWaves) {
+        const int cc = e / kv.dim, d = e % kv.dim;
+        float most = -INFINITY, all = 0, x = 0;
+#pragma unroll
+        for (int k = 0; k < kWaves; ++k) most = fmaxf(most, stats[k][cc][0]);
+        const float base = most == -INFINITY ? 0.0f : most;
+#pragma unroll
+        for (int k = 0; k < kWaves; ++k) {
+            const float f = __builtin_amdgcn_exp2f(stats[k][cc][0] - base);       // NaN where the query is
+            all += f * stats[k][cc][1];
+            x += f * sums[k][cc][d];
+        }
+        if (a.splits == 1) {
+            const int column = s.col0 + cc;
+            store_any(a.out, s.start + column / a.group, (h * a.group + column % a.group) * kv.dim + d, all == 0 ? 0.0f : x / all);
+        } else {
+            a.sums[(place * a.columns + cc) * kv.dim + d] = x;
+            if (d == 0) a.stats[(place * a.columns + cc) * 2] = all != all ? __builtin_nanf("") : most, a.stats[(place * a.columns + cc) * 2 + 1] = all;
         }
     }
-    for (int k = 0; k < 4; ++k) {
-        const int d = lane + 64 * k;
-        if (d < dim) store_value<OUT>(out, row, hq * dim + d, bad ? __builtin_nanf("") : sum > 0 ? acc[k] / sum : 0.0f);
+}
+
+// The shares of one query's keys in one.
+__global__ __launch_bounds__(kMaxHeadDim) void kv_attention_join_kernel(Attention a) {
+    const KvArgs &kv = a.kv;
+    int unit = blockIdx.x;
+    const int cc = unit % a.columns;
+    unit /= a.columns;
+    const int tile = unit % a.tiles;
+    unit /= a.tiles;
+    const int h = unit % kv.heads, b = unit / kv.heads;
+    const Seen s = seen_by(a, b, tile);
+    if (cc >= s.cols) return;
+    const int share = share_of(s.total, a.splits), used = share ? max(1, (s.total + share - 1) / share) : 1;
+    const long place = (((long)b * kv.heads + h) * a.tiles + tile) * a.splits;
+    float most = -INFINITY, all = 0, x = 0;
+    for (int k = 0; k < used; ++k) {
+        const float t = a.stats[((place + k) * a.columns + cc) * 2];
+        most = t != t ? t : fmaxf(most, t);
     }
+    const float base = most == -INFINITY ? 0.0f : most;
+    const int d = threadIdx.x;
+    for (int k = 0; k < used; ++k) {
+        const long from = (place + k) * a.columns + cc;
+        const float f = __builtin_amdgcn_exp2f(a.stats[from * 2] - base);
+        all += f * a.stats[from * 2 + 1];
+        if (d < kv.dim) x += f * a.sums[from * kv.dim + d];
+    }
+    const int column = s.col0 + cc;
+    if (d < kv.dim) store_any(a.out, s.start + column / a.group, (h * a.group + column % a.group) * kv.dim + d, all == 0 ? 0.0f : x / all);
+}
+
+// How a call is cut up.
+struct Cut {
+    int tiles, splits, columns;
+    long places() const { return (long)tiles * splits * columns; }
+};
+Cut cut_of(const KvArgs &kv, int heads_q, int window, int sinks) {
+    Cut c;
+    const int group = heads_q / kv.heads;
+    const long columns = (long)kv.max_new * group;
+    c.tiles = (int)((columns + kColumns - 1) / kColumns);
+    c.columns = (int)std::min<long>(columns, kColumns);
+    const long reach = std::min<long>(kv.max_len, (long)kv.table_stride * kKvBlock);
+    const long keys = window ? std::min(reach, (long)window + kv.max_new + sinks + 2 * kKvBlock) : reach;
+    const long blocks = std::max(1l, (keys + kKvBlock - 1) / kKvBlock), units = std::max(1l, (long)kv.count * kv.heads * c.tiles);
+    c.splits = (int)std::max(1l, std::min((2048 + units - 1) / units, (blocks + 2 * kWaves - 1) / (2 * kWaves)));
+    return c;
 }
 
 }  // namespace
 
 namespace gala {
 
-size_t kv_attention_workspace(const KvArgs &, int, int, int) { return 0; }
+size_t kv_attention_workspace(const KvArgs &kv, int heads_q, int window, int sinks) {
+    const Cut c = cut_of(kv, heads_q, window, sinks);
+    return c.splits == 1 ? 0 : (size_t)kv.count * kv.heads * c.places() * (kv.dim + 2) * sizeof(float);
+}
 
 int launch_kv_attention(void *stream, const KvArgs &kv, int heads_q, float scale, int window, int sinks, const Values &q,
-                        const Values &out, void *) {
-    by_type(q.type, [&](auto type) {
-        by_type(out.type, [&](auto to) {
-            hipLaunchKernelGGL((kv_attention_kernel<decltype(type)::value, decltype(to)::value>), dim3(kv.count * kv.max_new * heads_q),
-                               dim3(64), 0, (hipStream_t)stream, kv, heads_q, scale, window, sinks, q, out);
-        });
-    });
+                        const Values &out, void *workspace) {
+    const Cut c = cut_of(kv, heads_q, window, sinks);
+    Attention a{};
+    a.kv = kv, a.q = q, a.out = out;
+    a.heads_q = heads_q, a.group = heads_q / kv.heads;
+    a.scale = scale, a.window = window, a.sinks = sinks;
+    a.tiles = c.tiles, a.splits = c.splits, a.columns = c.columns;
+    a.sums = (float *)workspace;
+    a.stats = a.sums + (size_t)kv.count * kv.heads * c.places() * kv.dim;
+    const bool fine = q.type == GALA_F32 || q.type == GALA_RESIDUE || out.type == GALA_F32 || out.type == GALA_RESIDUE;
+    const unsigned groups = (unsigned)((long)kv.count * kv.heads * c.tiles * c.splits);
+    auto launch = [&](auto nc) {
+        constexpr int NC = decltype(nc)::value;
+        if (fine)
+            hipLaunchKernelGGL((kv_attention_kernel<NC, 3>), dim3(groups), dim3(64 * kWaves), 0, (hipStream_t)stream, a);
+        else
+            hipLaunchKernelGGL((kv_attention_kernel<NC, 2>), dim3(groups), dim3(64 * kWaves), 0, (hipStream_t)stream, a);
+    };
+    switch ((kv.dim + 63) / 64) {
+        case 1: launch(std::integral_constant<int, 1>()); break;
+        case 2: launch(std::integral_constant<int, 2>()); break;
+        case 3: launch(std::integral_constant<int, 3>()); break;
+        default: launch(std::integral_constant<int, 4>()); break;
+    }
+    if (hipGetLastError() != hipSuccess) return 1;
+    if (c.splits > 1) {
+        const unsigned rows = (unsigned)((long)kv.count * kv.heads * c.tiles * c.columns);
+        hipLaunchKernelGGL(kv_attention_join_kernel, dim3(rows), dim3((kv.dim + 63) / 64 * 64), 0, (hipStream_t)stream, a);
+    }
     return hipGetLastError() != hipSuccess;
 }
 
