@@ -1,41 +1,273 @@
 // One token a row from logits and given uniform numbers.
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
 #include <type_traits>
 
 #include "gala_decode.h"
 
 using namespace gala;
 
+// A row's tokens are put into bins by how far their logit is below the largest, a cut is found from the bins' counts
+// and weights, and only the bin that the cut falls into is looked at token by token.  A row is shared by several
+// workgroups, and each step that needs all of them is a launch of its own:
+//   best    the largest logit of every chunk of the row;
+//   bins    counts and weights of the bins, where the row has a top-k or top-p;
+//   gather  of every chunk, the weight of the tokens that are kept for sure, and a list of those in the cut's bin;
+//   draw    the cut within its bin, the chunk that the uniform number falls into, and the token in it.
+// Weights are whole numbers, so the sums do not depend on who adds what first.
 namespace {
 
-constexpr int kThreads = 1024;
+constexpr int kThreads = 512, kDrawThreads = 1024;
 constexpr float kWeightOne = 1099511627776.0f;      // 2^40
+// 1/32 of a factor e each; from the last bin on weights are less than 2^-40 and count as nothing
+constexpr int kBins = 896;
+constexpr float kBinsPerUnit = 32.0f;
+constexpr int kListed = 2048;                       // tokens of a list; a row that needs more is searched as a whole
+constexpr int kMostChunks = 256;
 
 // A logit's place in descending order: the larger, the smaller; both zeros alike.
 __device__ __forceinline__ u32 descending(float z) {
     const u32 bits = __float_as_uint(z + 0.0f);
     return ~((bits & 0x80000000u) ? ~bits : bits | 0x80000000u);
 }
+__device__ __forceinline__ float logit_of(u64 key) {
+    const u32 bits = ~(u32)(key >> 32);
+    return __uint_as_float((bits & 0x80000000u) ? bits & 0x7fffffffu : ~bits);
+}
+__device__ __forceinline__ u64 key_of(float z, int i) { return (u64)descending(z == z ? z : -INFINITY) << 32 | (u32)i; }
 
-struct Shared {
+struct Workspace {
+    u64 *mass;               // rows x kBins: weights, and of every bin the count
+    u32 *count;
+    u32 *listed;             // rows: tokens of the list, those beyond its end included
+    u64 *list;               // rows x kListed keys
+    u64 *best, *sure;        // rows x chunks
+};
+struct Sample {
+    Values logits;
+    int rows, vocab, chunks, chunk;      // chunk: tokens of a chunk
+    gala_sampling how;
+    int *tokens;
+    Workspace ws;
+};
+
+// What a row asks for.
+struct Row {
+    float top, rate, share, least;
+    int first;               // the first token, -1 if the row has none
+    int most;                // top-k, 0: all
+    bool greedy;
+
+    __device__ float chance(float z) const {
+#pragma clang fp contract(off)
+        return z == top ? 1.0f : z > -INFINITY ? expf((z - top) * rate) : 0.0f;
+    }
+    __device__ u64 weight(float z) const { return (u64)(chance(z) * kWeightOne); }
+    __device__ int bin(float z) const { return z == top ? 0 : z == z ? (int)fminf((top - z) * rate * kBinsPerUnit, kBins - 1) : kBins - 1; }
+    // 0 where the token is not kept for its weight
+    __device__ u64 kept(float z) const {
+        const float w = chance(z);
+        return w >= least ? (u64)(w * kWeightOne) : (u64)0;
+    }
+    __device__ bool cuts() const { return !greedy && first >= 0 && (most > 0 || share < 1); }
+};
+__device__ __forceinline__ u64 wave_min(u64 v) {
+    for (int k = 32; k; k >>= 1) v = min(v, (u64)__shfl_xor(v, k));
+    return v;
+}
+__device__ __forceinline__ u64 wave_sum(u64 v) {
+    for (int k = 32; k; k >>= 1) v += __shfl_xor(v, k);
+    return v;
+}
+// by every wavefront for itself, from the chunks' largest logits
+__device__ __forceinline__ Row row_of(const Sample &a, int row) {
+    Row r;
+    u64 best = ~0ull;
+    for (int i = threadIdx.x & 63; i < a.chunks; i += 64) best = min(best, a.ws.best[(long)row * a.chunks + i]);
+    best = wave_min(best);
+    const float temperature = a.how.temperature ? a.how.temperature[row] : 1.0f, least = a.how.min_p ? a.how.min_p[row] : 0.0f;
+    r.top = logit_of(best);
+    r.first = r.top == -INFINITY ? -1 : (int)(u32)best;
+    r.greedy = temperature <= 0;
+    r.rate = r.greedy ? 1.0f : 1.0f / temperature;
+    r.share = a.how.top_p ? a.how.top_p[row] : 1.0f;
+    r.least = least == least ? fminf(least, 1.0f) : 0.0f;
+    const int most = a.how.top_k ? a.how.top_k[row] : 0;
+    r.most = most > 0 && most < a.vocab ? most : 0;
+    return r;
+}
+
+// f(logit, index) for the logits from `lo` to `hi`, eight loads of a thread under way together
+template <int TYPE, int THREADS, class F>
+__device__ __forceinline__ void for_each_logit(const Values &logits, int row, int lo, int hi, F f) {
+    constexpr int kLoads = 8;
+    for (int at = lo + threadIdx.x; at < hi; at += kLoads * THREADS) {
+        float z[kLoads];
+#pragma unroll
+        for (int k = 0; k < kLoads; ++k) z[k] = load_value<TYPE>(logits, row, min(at + k * THREADS, hi - 1));
+#pragma unroll
+        for (int k = 0; k < kLoads; ++k)
+            if (at + k * THREADS < hi) f(z[k], at + k * THREADS);
+    }
+}
+
+template <int TYPE>
+__global__ __launch_bounds__(kThreads) void sample_best_kernel(Sample a) {
+    __shared__ u64 part[kThreads / 64];
+    const int row = blockIdx.x / a.chunks, c = blockIdx.x % a.chunks, tid = threadIdx.x;
+    u64 best = ~0ull;
+    for_each_logit<TYPE, kThreads>(a.logits, row, c * a.chunk, min(a.vocab, c * a.chunk + a.chunk), [&](float z, int i) { best = min(best, key_of(z, i)); });
+    best = wave_min(best);
+    if ((tid & 63) == 0) part[tid >> 6] = best;
+    // what the next launches add to
+    for (int i = c * kThreads + tid; i < kBins; i += a.chunks * kThreads) a.ws.mass[(long)row * kBins + i] = 0, a.ws.count[(long)row * kBins + i] = 0;
+    if (c == 0 && tid == 0) a.ws.listed[row] = 0;
+    __syncthreads();
+    if (tid == 0) {
+        for (int k = 1; k < kThreads / 64; ++k) best = min(best, part[k]);
+        a.ws.best[(long)row * a.chunks + c] = best;
+    }
+}
+
+template <int TYPE>
+__global__ __launch_bounds__(kThreads) void sample_bins_kernel(Sample a) {
+    __shared__ u64 mass[kBins];
+    __shared__ u32 count[kBins];
+    const int row = blockIdx.x / a.chunks, c = blockIdx.x % a.chunks;
+    const Row r = row_of(a, row);
+    if (!r.cuts()) return;
+    for (int i = threadIdx.x; i < kBins; i += kThreads) mass[i] = 0, count[i] = 0;
+    __syncthreads();
+    const bool counts = r.most > 0, weighs = r.share < 1;
+    for_each_logit<TYPE, kThreads>(a.logits, row, c * a.chunk, min(a.vocab, c * a.chunk + a.chunk), [&](float z, int) {
+        const int bin = r.bin(z);
+        if (bin == kBins - 1) return;            // what is left over is in the last one
+        if (counts) atomicAdd(&count[bin], 1u);
+        if (weighs) atomicAdd((unsigned long long *)&mass[bin], (unsigned long long)r.weight(z));
+    });
+    __syncthreads();
+    for (int i = threadIdx.x; i < kBins; i += kThreads) {
+        if (count[i]) atomicAdd(&a.ws.count[(long)row * kBins + i], count[i]);
+        if (mass[i]) atomicAdd((unsigned long long *)&a.ws.mass[(long)row * kBins + i], (unsigned long long)mass[i]);
+    }
+}
+
+// The bins up to each, and the cuts as far as the bins tell.
+struct Bins {
+    u64 mass[kBins];         // of the bin and all before it
+    u32 count[kBins];
+    u64 part_mass[16];
+    u32 part_count[16];
+    int k_bin, p_low, p_high;
+};
+// Tokens of bins below `sure` are kept (min-p apart); those of bins in [low, high] and of k_bin are to be looked at.
+struct Cut {
+    int sure, low, high, k_bin;
+    bool by_k;
+    __device__ bool open(int bin) const { return (bin >= low && bin <= high) || (by_k && bin == k_bin); }
+};
+// the weight that is passed by the last token that top-p keeps
+__device__ __forceinline__ u64 passed(float share, u64 all) {
+    const double below = ceil((double)share * (double)all) - 1;
+    return below > 0 && all ? min((u64)below, all - 1) : 0;
+}
+template <int THREADS>
+__device__ Cut cut_of(const Sample &a, const Row &r, int row, Bins &bins) {
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    constexpr int kEach = (kBins + THREADS - 1) / THREADS;
+    u64 m[kEach], sum = 0;
+    u32 n[kEach], all = 0;
+#pragma unroll
+    for (int k = 0; k < kEach; ++k) {
+        const int i = tid * kEach + k;
+        sum += i < kBins ? a.ws.mass[(long)row * kBins + i] : 0, all += i < kBins ? a.ws.count[(long)row * kBins + i] : 0;
+        m[k] = sum, n[k] = all;
+    }
+    u64 before = sum;
+    u32 count = all;
+    for (int k = 1; k < 64; k <<= 1) {
+        const u64 x = __shfl_up(before, k);
+        const u32 y = __shfl_up(count, k);
+        if (lane >= k) before += x, count += y;
+    }
+    if (lane == 63) bins.part_mass[wave] = before, bins.part_count[wave] = count;
+    if (tid == 0) bins.k_bin = kBins - 1, bins.p_low = bins.p_high = kBins - 1;
+    __syncthreads();
+    before -= sum, count -= all;
+    for (int k = 0; k < wave; ++k) before += bins.part_mass[k], count += bins.part_count[k];
+#pragma unroll
+    for (int k = 0; k < kEach; ++k) {
+        const int i = tid * kEach + k;
+        if (i >= kBins) continue;
+        bins.mass[i] = before + m[k], bins.count[i] = count + n[k];
+        if (r.most > 0 && i < kBins - 1 && count + n[k] >= (u32)r.most && count + (k ? n[k - 1] : 0) < (u32)r.most) bins.k_bin = i;
+    }
+    __syncthreads();
+    Cut c;
+    c.k_bin = bins.k_bin, c.by_k = r.most > 0 && c.k_bin < kBins - 1;
+    c.low = kBins, c.high = -1;
+    c.sure = c.by_k ? c.k_bin : kBins;
+    if (r.share < 1) {
+        // what top-p takes its share of lies between these, and so do the bins of its cut
+        const u64 total = bins.mass[kBins - 1];
+        const u64 low = passed(r.share, c.by_k ? (c.k_bin ? bins.mass[c.k_bin - 1] : 0) : total), high = passed(r.share, c.by_k ? bins.mass[c.k_bin] : total);
+        for (int i = tid; i < kBins; i += THREADS) {
+            const u64 at = i ? bins.mass[i - 1] : 0;
+            if (at <= low && low < bins.mass[i]) bins.p_low = i;
+            if (at <= high && high < bins.mass[i]) bins.p_high = i;
+        }
+        __syncthreads();
+        c.low = min(bins.p_low, c.k_bin), c.high = min(bins.p_high, c.k_bin), c.sure = c.low;
+    }
+    return c;
+}
+
+template <int TYPE>
+__global__ __launch_bounds__(kThreads) void sample_gather_kernel(Sample a) {
+    __shared__ Bins bins;
+    __shared__ u64 part[kThreads / 64];
+    const int row = blockIdx.x / a.chunks, c = blockIdx.x % a.chunks, tid = threadIdx.x;
+    const Row r = row_of(a, row);
+    if (r.greedy || r.first < 0) return;
+    Cut cut{kBins, kBins, -1, kBins - 1, false};
+    if (r.cuts()) cut = cut_of<kThreads>(a, r, row, bins);
+    // tokens beyond this bin weigh nothing or less than min-p asks: their weights need not be computed
+    const int reach = min(cut.sure, r.least > 0 ? (int)fminf(-logf(r.least) * kBinsPerUnit + 2, kBins - 1) + 1 : kBins - 1);
+    u64 sum = 0;
+    for_each_logit<TYPE, kThreads>(a.logits, row, c * a.chunk, min(a.vocab, c * a.chunk + a.chunk), [&](float z, int i) {
+        const int bin = r.bin(z);
+        if (bin < reach) sum += r.kept(z);
+        if (cut.open(bin)) {
+            const u32 at = atomicAdd(&a.ws.listed[row], 1u);
+            if (at < kListed) a.ws.list[(long)row * kListed + at] = key_of(z, i);
+        }
+    });
+    sum = wave_sum(sum);
+    if ((tid & 63) == 0) part[tid >> 6] = sum;
+    __syncthreads();
+    if (tid == 0) {
+        for (int k = 1; k < kThreads / 64; ++k) sum += part[k];
+        a.ws.sure[(long)row * a.chunks + c] = sum;
+    }
+}
+
+struct Search {
     u64 bins[256];
     u64 carry, total;
     u32 digit;
-    float part[16];
 };
-
 // Of elements with keys and weights, given by each(f(key, weight)) over all threads together, the key at which the
 // weights added up in ascending order of keys first exceed `target`: digit by digit from the top, in sums of the
 // weights of all elements whose digits so far are the key's.  Needs target < the sum of all.
 template <class E>
-__device__ u64 weighted_select(Shared &sh, u64 target, int bits, E each) {
+__device__ u64 weighted_select(Search &sh, u64 target, E each) {
     u64 prefix = 0;
-    for (int shift = (bits + 7) / 8 * 8 - 8; shift >= 0; shift -= 8) {
-        for (int i = threadIdx.x; i < 256; i += kThreads) sh.bins[i] = 0;
+    for (int shift = 56; shift >= 0; shift -= 8) {
+        for (int i = threadIdx.x; i < 256; i += kDrawThreads) sh.bins[i] = 0;
         __syncthreads();
         each([&](u64 key, u64 weight) {
-            if (weight && (shift + 8 >= 64 || key >> (shift + 8) == prefix >> (shift + 8)))
+            if (weight && (shift == 56 || key >> (shift + 8) == prefix >> (shift + 8)))
                 atomicAdd((unsigned long long *)&sh.bins[key >> shift & 255], (unsigned long long)weight);
         });
         __syncthreads();
@@ -53,90 +285,223 @@ __device__ u64 weighted_select(Shared &sh, u64 target, int bits, E each) {
     return prefix;
 }
 
-// One workgroup a row.
 template <int TYPE>
-__global__ __launch_bounds__(kThreads) void sample_kernel(Values logits, int vocab, gala_sampling how, int *tokens) {
-#pragma clang fp contract(off)
-    __shared__ Shared sh;
-    const int row = blockIdx.x, tid = threadIdx.x;
-    auto logit = [&](int i) { return load_value<TYPE>(logits, row, i); };
-    const float temperature = how.temperature ? how.temperature[row] : 1.0f;
-    const bool greedy = temperature <= 0;
-    const float rate = greedy ? 1.0f : 1.0f / temperature;
-    float top = -INFINITY;
-    for (int i = tid; i < vocab; i += kThreads) top = fmaxf(top, logit(i));        // a NaN is never the larger
-    for (int k = 32; k; k >>= 1) top = fmaxf(top, __shfl_xor(top, k));
-    if ((tid & 63) == 0) sh.part[tid >> 6] = top;
-    __syncthreads();
-    for (int k = 0; k < kThreads / 64; ++k) top = fmaxf(top, sh.part[k]);
-    if (top == -INFINITY) {
-        if (tid == 0) tokens[row] = -1;
+__global__ __launch_bounds__(kDrawThreads) void sample_draw_kernel(Sample a) {
+    constexpr int kWaves = kDrawThreads / 64;
+    __shared__ Bins bins;
+    __shared__ union {
+        Search search;
+        u64 keys[kListed];
+    } sh;
+    __shared__ u64 chunk_mass[kMostChunks], part[kWaves], found_mass, found_key;
+    __shared__ int found;
+    const int row = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const Row r = row_of(a, row);
+    if (r.greedy || r.first < 0) {
+        if (tid == 0) a.tokens[row] = r.first;
         return;
     }
-    auto chance = [&](float z) { return z == top ? 1.0f : z == z ? expf((z - top) * rate) : 0.0f; };
-    auto weight = [&](float z) { return (u64)(chance(z) * kWeightOne); };
-    auto key = [&](float z, int i) { return (u64)descending(z) << 32 | (u32)i; };
-    auto sum_of = [&](auto f) {
-        if (tid == 0) sh.total = 0;
+    for (int i = tid; i < a.chunks; i += kDrawThreads) chunk_mass[i] = a.ws.sure[(long)row * a.chunks + i];
+    // sum over the workgroup's threads
+    auto sum_of = [&](u64 v) {
+        v = wave_sum(v);
         __syncthreads();
-        u64 sum = 0;
-        for (int i = tid; i < vocab; i += kThreads) sum += f(logit(i), i);
-        for (int k = 32; k; k >>= 1) sum += __shfl_xor(sum, k);
-        if ((tid & 63) == 0) atomicAdd((unsigned long long *)&sh.total, (unsigned long long)sum);
+        if (lane == 0) part[wave] = v;
         __syncthreads();
-        const u64 all = sh.total;
-        __syncthreads();
+        u64 all = 0;
+        for (int k = 0; k < kWaves; ++k) all += part[k];
         return all;
     };
-    u64 last = ~0ull;                                                             // the last key that is kept
-    const int most = greedy ? 1 : how.top_k ? how.top_k[row] : 0;
-    if (most > 0 && most < vocab) {
-        auto each = [&](auto f) {
-            for (int i = tid; i < vocab; i += kThreads) {
-                const float z = logit(i);
-                f(key(z == z ? z : -INFINITY, i), (u64)1);
+    u64 last = ~0ull;                                  // the last key that is kept
+    if (r.cuts()) {
+        const Cut cut = cut_of<kDrawThreads>(a, r, row, bins);
+        const int n = (int)a.ws.listed[row];
+        if (n > kListed) {
+            // more than a list holds: the cuts from the whole row, and the chunks' sums anew
+            auto each_of = [&](auto weight) {
+                return [&a, row, weight, &last](auto f) {
+                    for_each_logit<TYPE, kDrawThreads>(a.logits, row, 0, a.vocab, [&](float z, int i) {
+                        const u64 key = key_of(z, i);
+                        if (key <= last) f(key, weight(z));
+                    });
+                };
+            };
+            auto one = [](float) { return (u64)1; };
+            auto weight = [&](float z) { return r.weight(z); };
+            if (r.most > 0) last = weighted_select(sh.search, r.most - 1, each_of(one));
+            if (r.share < 1) {
+                u64 sum = 0;
+                each_of(weight)([&](u64, u64 w) { sum += w; });
+                last = weighted_select(sh.search, passed(r.share, sum_of(sum)), each_of(weight));
             }
-        };
-        last = weighted_select(sh, most - 1, 64, each);
-    }
-    const float share = how.top_p ? how.top_p[row] : 1.0f, given = how.min_p ? how.min_p[row] : 0.0f;
-    const float least = given == given ? fminf(given, 1.0f) : 0.0f;
-    if (share < 1) {
-        const u64 all = sum_of([&](float z, int i) { return key(z, i) <= last ? weight(z) : (u64)0; });
-        const double below = ceil((double)share * (double)all) - 1;
-        auto each = [&](auto f) {
-            for (int i = tid; i < vocab; i += kThreads) {
-                const float z = logit(i);
-                if (key(z, i) <= last) f(key(z, i), weight(z));
+            for (int c = wave; c < a.chunks; c += kWaves) {
+                u64 sum = 0;
+                for (int i = c * a.chunk + lane; i < min(a.vocab, c * a.chunk + a.chunk); i += 64) {
+                    const float z = load_value<TYPE>(a.logits, row, i);
+                    if (key_of(z, i) <= last) sum += r.kept(z);
+                }
+                sum = wave_sum(sum);
+                if (lane == 0) chunk_mass[c] = sum;
             }
-        };
-        last = weighted_select(sh, below > 0 ? min((u64)below, all - 1) : 0, 64, each);
+            __syncthreads();
+        } else {
+            int size = 64;
+            while (size < n) size *= 2;
+            for (int i = tid; i < size; i += kDrawThreads) sh.keys[i] = i < n ? a.ws.list[(long)row * kListed + i] : ~0ull;
+            // the list in order: a bitonic network
+            for (int run = 2; run <= size; run *= 2)
+                for (int step = run / 2; step; step /= 2) {
+                    __syncthreads();
+                    for (int p = tid; p < size / 2; p += kDrawThreads) {
+                        const int i = (p / step) * 2 * step + p % step, j = i + step;
+                        const u64 x = sh.keys[i], y = sh.keys[j];
+                        if ((x > y) == !(i & run)) sh.keys[i] = y, sh.keys[j] = x;
+                    }
+                }
+            __syncthreads();
+            // two neighbours a thread: their bins, weights, and the weight of the list before them
+            u64 key[2], w[2];
+            int bin[2];
+            for (int k = 0; k < 2; ++k) {
+                const int i = 2 * tid + k;
+                key[k] = i < n ? sh.keys[i] : ~0ull;
+                const float z = i < n ? logit_of(key[k]) : 0.0f;
+                bin[k] = i < n ? r.bin(z) : kBins;
+                w[k] = i < n ? r.weight(z) : 0;
+            }
+            u64 all = bins.mass[kBins - 1];
+            int below = 0;
+            if (cut.by_k) {
+                // of k_bin's tokens the first ones; other bins' come before them in the list
+                const int need = r.most - (cut.k_bin ? (int)bins.count[cut.k_bin - 1] : 0);
+                u64 at = 0;
+                for (int k = 0; k < 2; ++k) at += bin[k] < cut.k_bin;
+                below = (int)sum_of(at);
+                last = sh.keys[below + need - 1];
+                u64 mine = 0;
+                for (int k = 0; k < 2; ++k) mine += bin[k] == cut.k_bin && key[k] <= last ? w[k] : 0;
+                all = (cut.k_bin ? bins.mass[cut.k_bin - 1] : 0) + sum_of(mine);
+            }
+            if (r.share < 1) {
+                const u64 target = passed(r.share, all);
+                if (tid == 0) found = kBins - 1;
+                __syncthreads();
+                for (int i = tid; i < kBins; i += kDrawThreads)
+                    if ((i ? bins.mass[i - 1] : 0) <= target && target < bins.mass[i]) found = i;
+                __syncthreads();
+                const int p_bin = found;
+                const u64 rest = target - (p_bin ? bins.mass[p_bin - 1] : 0);
+                u64 mine = 0;
+                for (int k = 0; k < 2; ++k) mine += bin[k] == p_bin ? w[k] : 0;
+                u64 upto = mine;
+                for (int k = 1; k < 64; k <<= 1) {
+                    const u64 x = __shfl_up(upto, k);
+                    if (lane >= k) upto += x;
+                }
+                __syncthreads();
+                if (lane == 63) part[wave] = upto;
+                __syncthreads();
+                u64 at = upto - mine;
+                for (int k = 0; k < wave; ++k) at += part[k];
+                for (int k = 0; k < 2; ++k) {
+                    const u64 own = bin[k] == p_bin ? w[k] : 0;
+                    if (at <= rest && rest < at + own) found_key = key[k];
+                    at += own;
+                }
+                __syncthreads();
+                last = min(last, found_key);
+            }
+            // what the list adds to the chunks
+            for (int k = 0; k < 2; ++k)
+                if (key[k] <= last && 2 * tid + k < n && bin[k] >= cut.sure) {
+                    const u64 kept = r.kept(logit_of(key[k]));
+                    if (kept) atomicAdd((unsigned long long *)&chunk_mass[(u32)key[k] / a.chunk], (unsigned long long)kept);
+                }
+            __syncthreads();
+        }
+    } else {
+        __syncthreads();
     }
-    auto kept = [&](float z, int i) {
-        const float w = chance(z);
-        return key(z, i) <= last && w >= least ? (u64)(w * kWeightOne) : (u64)0;
+    // the chunk, then the wavefront's part of it, then the token
+    u64 sum = 0;
+    for (int i = tid; i < a.chunks; i += kDrawThreads) sum += chunk_mass[i];
+    const u64 all = sum_of(sum);
+    const double drawn = (double)a.how.u[row] * (double)all;
+    u64 target = drawn > 0 ? min((u64)drawn, all - 1) : 0;
+    if (tid == 0) {
+        int c = 0;
+        while (c < a.chunks - 1 && chunk_mass[c] <= target) target -= chunk_mass[c++];
+        found = c, found_mass = target;
+    }
+    __syncthreads();
+    target = found_mass;
+    const int lo = found * a.chunk, hi = min(a.vocab, lo + a.chunk), each = ((a.chunk + kWaves - 1) / kWaves + 63) / 64 * 64;
+    const int begin = lo + wave * each, end = min(hi, begin + each);
+    auto kept = [&](int i) {
+        if (i >= end) return (u64)0;
+        const float z = load_value<TYPE>(a.logits, row, i);
+        return key_of(z, i) <= last ? r.kept(z) : (u64)0;
     };
-    const u64 all = sum_of(kept);
-    const double drawn = (double)how.u[row] * (double)all;
-    const u64 target = drawn > 0 ? min((u64)drawn, all - 1) : 0;
-    auto each = [&](auto f) {
-        for (int i = tid; i < vocab; i += kThreads) f((u64)i, kept(logit(i), i));
-    };
-    const int bits = 32 - __clz(vocab);
-    const u64 token = weighted_select(sh, target, bits, each);
-    if (tid == 0) tokens[row] = (int)token;
+    sum = 0;
+    for (int i = begin + lane; i - lane < end; i += 64) sum += kept(i);
+    sum = wave_sum(sum);
+    __syncthreads();
+    if (lane == 0) part[wave] = sum;
+    __syncthreads();
+    u64 before = 0;
+    for (int k = 0; k < wave; ++k) before += part[k];
+    if (before <= target && target < before + part[wave]) {
+        for (int i = begin + lane; i - lane < end; i += 64) {
+            const u64 w = kept(i);
+            u64 upto = w;
+            for (int k = 1; k < 64; k <<= 1) {
+                const u64 x = __shfl_up(upto, k);
+                if (lane >= k) upto += x;
+            }
+            upto += before;
+            if (upto - w <= target && target < upto) a.tokens[row] = i;
+            before = __shfl(upto, 63);
+        }
+    }
+}
+
+// chunks of a row: enough workgroups for the card, none with fewer tokens than its threads load at once
+void chunks_of(int rows, int vocab, int *chunks, int *chunk) {
+    const int most = std::min(kMostChunks, (vocab + 2047) / 2048), wanted = (512 + rows - 1) / std::max(rows, 1);
+    *chunks = std::max(1, std::min(most, wanted));
+    *chunk = (int)(((long)vocab + *chunks - 1) / *chunks);
+    *chunks = (int)(((long)vocab + *chunk - 1) / *chunk);
 }
 
 }  // namespace
 
 namespace gala {
 
-size_t sample_workspace(int, int) { return 0; }
+size_t sample_workspace(int rows, int vocab) {
+    int chunks, chunk;
+    chunks_of(rows, vocab, &chunks, &chunk);
+    return (size_t)rows * (kBins * 12 + kListed * 8 + chunks * 16 + 8);
+}
 
-int launch_sample(void *stream, const Values &logits, int rows, int vocab, const gala_sampling &how, int *tokens, void *) {
+int launch_sample(void *stream, const Values &logits, int rows, int vocab, const gala_sampling &how, int *tokens, void *workspace) {
+    Sample a{};
+    a.logits = logits, a.rows = rows, a.vocab = vocab, a.how = how, a.tokens = tokens;
+    chunks_of(rows, vocab, &a.chunks, &a.chunk);
+    u64 *at = (u64 *)workspace;
+    a.ws.mass = at, at += (size_t)rows * kBins;
+    a.ws.list = at, at += (size_t)rows * kListed;
+    a.ws.best = at, at += (size_t)rows * a.chunks;
+    a.ws.sure = at, at += (size_t)rows * a.chunks;
+    a.ws.count = (u32 *)at;
+    a.ws.listed = a.ws.count + (size_t)rows * kBins;
+    const dim3 grid(rows * a.chunks);
+    hipStream_t st = (hipStream_t)stream;
     by_type(logits.type, [&](auto type) {
-        hipLaunchKernelGGL(sample_kernel<decltype(type)::value>, dim3(rows), dim3(kThreads), 0, (hipStream_t)stream, logits, vocab, how,
-                           tokens);
+        constexpr int T = decltype(type)::value;
+        hipLaunchKernelGGL(sample_best_kernel<T>, grid, dim3(kThreads), 0, st, a);
+        if (how.top_k || how.top_p) hipLaunchKernelGGL(sample_bins_kernel<T>, grid, dim3(kThreads), 0, st, a);
+        hipLaunchKernelGGL(sample_gather_kernel<T>, grid, dim3(kThreads), 0, st, a);
+        hipLaunchKernelGGL(sample_draw_kernel<T>, dim3(rows), dim3(kDrawThreads), 0, st, a);
     });
     return hipGetLastError() != hipSuccess;
 }
