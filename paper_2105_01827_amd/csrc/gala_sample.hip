@@ -18,12 +18,13 @@ using namespace gala;
 // Weights are whole numbers, so the sums do not depend on who adds what first.
 namespace {
 
-constexpr int kThreads = 512, kDrawThreads = 1024;
+constexpr int kThreads = 512, kDrawThreads = 512;
 constexpr float kWeightOne = 1099511627776.0f;      // 2^40
 // 1/32 of a factor e each; from the last bin on weights are less than 2^-40 and count as nothing
 constexpr int kBins = 896;
 constexpr float kBinsPerUnit = 32.0f;
 constexpr int kListed = 2048;                       // tokens of a list; a row that needs more is searched as a whole
+constexpr int kCounted = 128;                       // longest list that is put in order by counting
 constexpr int kMostChunks = 256;
 
 // A logit's place in descending order: the larger, the smaller; both zeros alike.
@@ -42,14 +43,26 @@ struct Workspace {
     u32 *count;
     u32 *listed;             // rows: tokens of the list, those beyond its end included
     u64 *list;               // rows x kListed keys
-    u64 *best, *sure;        // rows x chunks
+    u64 *best;               // rows x groups
+    u64 *sure;               // rows x chunks
 };
 struct Sample {
     Values logits;
-    int rows, vocab, chunks, chunk;      // chunk: tokens of a chunk
+    int rows, vocab;
+    int groups;              // workgroups of a row, each has `each` chunks
+    int each, chunks, chunk; // chunk: tokens of a chunk, 1 << shift
+    int shift;
     gala_sampling how;
     int *tokens;
     Workspace ws;
+    // a chunk's first token: chunks but the first begin on 16 bytes
+    template <int TYPE>
+    __device__ int from(int row, int c) const {
+        typedef typename Element<TYPE>::type E;
+        constexpr int kOf = 16 / sizeof(E);
+        const int off = (int)((uintptr_t)((const E *)logits.data + row * logits.stride) / sizeof(E) % kOf);
+        return c == 0 ? 0 : c >= chunks ? vocab : min(vocab, c * chunk + (off ? kOf - off : 0));
+    }
 };
 
 // What a row asks for.
@@ -64,7 +77,10 @@ struct Row {
         return z == top ? 1.0f : z > -INFINITY ? expf((z - top) * rate) : 0.0f;
     }
     __device__ u64 weight(float z) const { return (u64)(chance(z) * kWeightOne); }
-    __device__ int bin(float z) const { return z == top ? 0 : z == z ? (int)fminf((top - z) * rate * kBinsPerUnit, kBins - 1) : kBins - 1; }
+    __device__ int bin(float z) const { 
+#pragma clang fp contract(off)
+        return z == top ? 0 : z == z ? (int)fminf((z - top) * rate * -kBinsPerUnit, kBins - 1) : kBins - 1;
+    }
     // 0 where the token is not kept for its weight
     __device__ u64 kept(float z) const {
         const float w = chance(z);
@@ -80,11 +96,19 @@ __device__ __forceinline__ u64 wave_sum(u64 v) {
     for (int k = 32; k; k >>= 1) v += __shfl_xor(v, k);
     return v;
 }
+// over the wavefront's lanes up to the own one
+__device__ __forceinline__ u64 upto_of(u64 v) {
+    for (int k = 1; k < 64; k <<= 1) {
+        const u64 x = __shfl_up(v, k);
+        if ((threadIdx.x & 63) >= k) v += x;
+    }
+    return v;
+}
 // by every wavefront for itself, from the chunks' largest logits
 __device__ __forceinline__ Row row_of(const Sample &a, int row) {
     Row r;
     u64 best = ~0ull;
-    for (int i = threadIdx.x & 63; i < a.chunks; i += 64) best = min(best, a.ws.best[(long)row * a.chunks + i]);
+    for (int i = threadIdx.x & 63; i < a.groups; i += 64) best = min(best, a.ws.best[(long)row * a.groups + i]);
     best = wave_min(best);
     const float temperature = a.how.temperature ? a.how.temperature[row] : 1.0f, least = a.how.min_p ? a.how.min_p[row] : 0.0f;
     r.top = logit_of(best);
@@ -98,35 +122,60 @@ __device__ __forceinline__ Row row_of(const Sample &a, int row) {
     return r;
 }
 
-// f(logit, index) for the logits from `lo` to `hi`, eight loads of a thread under way together
-template <int TYPE, int THREADS, class F>
-__device__ __forceinline__ void for_each_logit(const Values &logits, int row, int lo, int hi, F f) {
-    constexpr int kLoads = 8;
-    for (int at = lo + threadIdx.x; at < hi; at += kLoads * THREADS) {
-        float z[kLoads];
+// f(logit, index) for the logits from `lo` to `hi`, a thread's in ascending order: 16 bytes a load where they lie on
+// 16 bytes, several loads under way together, and what is before and behind them one by one.  After each load
+// done(index, next): the first index of the wavefront's 64 loads and of its next ones, neither beyond the last logit;
+// behind the last load next is -1.
+struct Nothing {
+    __device__ void operator()(int, int) const {}
+};
+template <int TYPE, int THREADS, class F, class D = Nothing>
+__device__ __forceinline__ void for_each_logit(const Values &logits, int row, int lo, int hi, F f, D done = D()) {
+    typedef typename Element<TYPE>::type E;
+    constexpr int kOf = 16 / sizeof(E), kLoads = TYPE == GALA_RESIDUE ? 8 : 4;
+    const E *x = (const E *)logits.data + row * logits.stride;
+    const int tid = threadIdx.x, off = (int)((uintptr_t)(x + lo) / sizeof(E) % kOf), begin = min(hi, lo + (off ? kOf - off : 0));
+    const int vectors = (hi - begin) / kOf, behind = begin + vectors * kOf;
+    auto value = [&](E v) { return to_float<TYPE>(v, logits.unit, logits.p); };
+    if (lo + tid < begin) f(value(x[lo + tid]), lo + tid);
+    for (int at = tid; at - (tid & 63) < vectors; at += kLoads * THREADS) {
+        union {
+            int4 word;
+            E e[kOf];
+        } v[kLoads];
 #pragma unroll
-        for (int k = 0; k < kLoads; ++k) z[k] = load_value<TYPE>(logits, row, min(at + k * THREADS, hi - 1));
+        for (int k = 0; k < kLoads; ++k) v[k].word = *(const int4 *)(x + begin + (long)min(at + k * THREADS, vectors - 1) * kOf);
 #pragma unroll
-        for (int k = 0; k < kLoads; ++k)
-            if (at + k * THREADS < hi) f(z[k], at + k * THREADS);
+        for (int k = 0; k < kLoads; ++k) {
+            if (at + k * THREADS < vectors)
+#pragma unroll
+                for (int j = 0; j < kOf; ++j) f(value(v[k].e[j]), begin + (at + k * THREADS) * kOf + j);
+            const int here = begin + (at - (tid & 63) + k * THREADS) * kOf;
+            done(min(here, hi - 1), min(here + THREADS * kOf, hi - 1));
+        }
     }
+    if (behind + tid < hi) f(value(x[behind + tid]), behind + tid);
+    done(hi - 1, -1);
 }
 
 template <int TYPE>
 __global__ __launch_bounds__(kThreads) void sample_best_kernel(Sample a) {
     __shared__ u64 part[kThreads / 64];
-    const int row = blockIdx.x / a.chunks, c = blockIdx.x % a.chunks, tid = threadIdx.x;
-    u64 best = ~0ull;
-    for_each_logit<TYPE, kThreads>(a.logits, row, c * a.chunk, min(a.vocab, c * a.chunk + a.chunk), [&](float z, int i) { best = min(best, key_of(z, i)); });
-    best = wave_min(best);
+    const int row = blockIdx.x / a.groups, c = blockIdx.x % a.groups, tid = threadIdx.x;
+    float top = -INFINITY;
+    int first = -1;
+    for_each_logit<TYPE, kThreads>(a.logits, row, a.from<TYPE>(row, c * a.each), a.from<TYPE>(row, (c + 1) * a.each), [&](float z, int i) {
+        if (z > top) top = z, first = i;
+    });
+    u64 best = wave_min(key_of(top, first));
     if ((tid & 63) == 0) part[tid >> 6] = best;
     // what the next launches add to
-    for (int i = c * kThreads + tid; i < kBins; i += a.chunks * kThreads) a.ws.mass[(long)row * kBins + i] = 0, a.ws.count[(long)row * kBins + i] = 0;
+    for (int i = c * kThreads + tid; i < kBins; i += a.groups * kThreads) a.ws.mass[(long)row * kBins + i] = 0, a.ws.count[(long)row * kBins + i] = 0;
     if (c == 0 && tid == 0) a.ws.listed[row] = 0;
     __syncthreads();
     if (tid == 0) {
         for (int k = 1; k < kThreads / 64; ++k) best = min(best, part[k]);
-        a.ws.best[(long)row * a.chunks + c] = best;
+        a.ws.best[(long)row * a.groups + c] = best;
     }
 }
 
@@ -134,13 +183,13 @@ template <int TYPE>
 __global__ __launch_bounds__(kThreads) void sample_bins_kernel(Sample a) {
     __shared__ u64 mass[kBins];
     __shared__ u32 count[kBins];
-    const int row = blockIdx.x / a.chunks, c = blockIdx.x % a.chunks;
+    const int row = blockIdx.x / a.groups, c = blockIdx.x % a.groups;
     const Row r = row_of(a, row);
     if (!r.cuts()) return;
     for (int i = threadIdx.x; i < kBins; i += kThreads) mass[i] = 0, count[i] = 0;
     __syncthreads();
     const bool counts = r.most > 0, weighs = r.share < 1;
-    for_each_logit<TYPE, kThreads>(a.logits, row, c * a.chunk, min(a.vocab, c * a.chunk + a.chunk), [&](float z, int) {
+    for_each_logit<TYPE, kThreads>(a.logits, row, a.from<TYPE>(row, c * a.each), a.from<TYPE>(row, (c + 1) * a.each), [&](float z, int) {
         const int bin = r.bin(z);
         if (bin == kBins - 1) return;            // what is left over is in the last one
         if (counts) atomicAdd(&count[bin], 1u);
@@ -184,12 +233,11 @@ __device__ Cut cut_of(const Sample &a, const Row &r, int row, Bins &bins) {
         sum += i < kBins ? a.ws.mass[(long)row * kBins + i] : 0, all += i < kBins ? a.ws.count[(long)row * kBins + i] : 0;
         m[k] = sum, n[k] = all;
     }
-    u64 before = sum;
+    u64 before = upto_of(sum);
     u32 count = all;
     for (int k = 1; k < 64; k <<= 1) {
-        const u64 x = __shfl_up(before, k);
         const u32 y = __shfl_up(count, k);
-        if (lane >= k) before += x, count += y;
+        if (lane >= k) count += y;
     }
     if (lane == 63) bins.part_mass[wave] = before, bins.part_count[wave] = count;
     if (tid == 0) bins.k_bin = kBins - 1, bins.p_low = bins.p_high = kBins - 1;
@@ -226,30 +274,38 @@ __device__ Cut cut_of(const Sample &a, const Row &r, int row, Bins &bins) {
 template <int TYPE>
 __global__ __launch_bounds__(kThreads) void sample_gather_kernel(Sample a) {
     __shared__ Bins bins;
-    __shared__ u64 part[kThreads / 64];
-    const int row = blockIdx.x / a.chunks, c = blockIdx.x % a.chunks, tid = threadIdx.x;
+    __shared__ u64 sure[kMostChunks];
+    const int row = blockIdx.x / a.groups, group = blockIdx.x % a.groups, tid = threadIdx.x;
     const Row r = row_of(a, row);
     if (r.greedy || r.first < 0) return;
+    const int first = group * a.each, chunks = min(a.each, a.chunks - first);
+    for (int i = tid; i < chunks; i += kThreads) sure[i] = 0;
     Cut cut{kBins, kBins, -1, kBins - 1, false};
     if (r.cuts()) cut = cut_of<kThreads>(a, r, row, bins);
+    __syncthreads();
     // tokens beyond this bin weigh nothing or less than min-p asks: their weights need not be computed
     const int reach = min(cut.sure, r.least > 0 ? (int)fminf(-logf(r.least) * kBinsPerUnit + 2, kBins - 1) + 1 : kBins - 1);
+    const int lo = a.from<TYPE>(row, first), past = chunks > 1 ? a.from<TYPE>(row, first + 1) - a.chunk : lo;
     u64 sum = 0;
-    for_each_logit<TYPE, kThreads>(a.logits, row, c * a.chunk, min(a.vocab, c * a.chunk + a.chunk), [&](float z, int i) {
-        const int bin = r.bin(z);
-        if (bin < reach) sum += r.kept(z);
-        if (cut.open(bin)) {
-            const u32 at = atomicAdd(&a.ws.listed[row], 1u);
-            if (at < kListed) a.ws.list[(long)row * kListed + at] = key_of(z, i);
-        }
-    });
-    sum = wave_sum(sum);
-    if ((tid & 63) == 0) part[tid >> 6] = sum;
+    for_each_logit<TYPE, kThreads>(
+        a.logits, row, lo, a.from<TYPE>(row, first + chunks),
+        [&](float z, int i) {
+            const int bin = r.bin(z);
+            if (bin < reach) sum += r.kept(z);
+            if (cut.open(bin)) {
+                const u32 at = atomicAdd(&a.ws.listed[row], 1u);
+                if (at < kListed) a.ws.list[(long)row * kListed + at] = key_of(z, i);
+            }
+        },
+        [&](int i, int next) {
+            const int c = min(max(i - past, 0) >> a.shift, chunks - 1);
+            if (next >= 0 && min(max(next - past, 0) >> a.shift, chunks - 1) == c) return;
+            sum = wave_sum(sum);
+            if ((tid & 63) == 0 && sum) atomicAdd((unsigned long long *)&sure[c], (unsigned long long)sum);
+            sum = 0;
+        });
     __syncthreads();
-    if (tid == 0) {
-        for (int k = 1; k < kThreads / 64; ++k) sum += part[k];
-        a.ws.sure[(long)row * a.chunks + c] = sum;
-    }
+    for (int i = tid; i < chunks; i += kThreads) a.ws.sure[(long)row * a.chunks + first + i] = sure[i];
 }
 
 struct Search {
@@ -294,13 +350,16 @@ __global__ __launch_bounds__(kDrawThreads) void sample_draw_kernel(Sample a) {
         u64 keys[kListed];
     } sh;
     __shared__ u64 chunk_mass[kMostChunks], part[kWaves], found_mass, found_key;
-    __shared__ int found;
+    __shared__ u64 unsorted[kCounted];
+    __shared__ int found, place[kCounted];
     const int row = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const Row r = row_of(a, row);
     if (r.greedy || r.first < 0) {
         if (tid == 0) a.tokens[row] = r.first;
         return;
     }
+    // of a token's index: what its chunks' borders lie behind multiples of a chunk
+    const int past = a.chunks > 1 ? a.from<TYPE>(row, 1) - a.chunk : 0;
     for (int i = tid; i < a.chunks; i += kDrawThreads) chunk_mass[i] = a.ws.sure[(long)row * a.chunks + i];
     // sum over the workgroup's threads
     auto sum_of = [&](u64 v) {
@@ -308,10 +367,9 @@ __global__ __launch_bounds__(kDrawThreads) void sample_draw_kernel(Sample a) {
         __syncthreads();
         if (lane == 0) part[wave] = v;
         __syncthreads();
-        u64 all = 0;
-        for (int k = 0; k < kWaves; ++k) all += part[k];
-        return all;
+        return wave_sum(lane < kWaves ? part[lane] : 0);
     };
+    auto before_wave = [&]() { return wave_sum(lane < wave ? part[lane] : 0); };
     u64 last = ~0ull;                                  // the last key that is kept
     if (r.cuts()) {
         const Cut cut = cut_of<kDrawThreads>(a, r, row, bins);
@@ -336,7 +394,7 @@ __global__ __launch_bounds__(kDrawThreads) void sample_draw_kernel(Sample a) {
             }
             for (int c = wave; c < a.chunks; c += kWaves) {
                 u64 sum = 0;
-                for (int i = c * a.chunk + lane; i < min(a.vocab, c * a.chunk + a.chunk); i += 64) {
+                for (int i = a.from<TYPE>(row, c) + lane; i < a.from<TYPE>(row, c + 1); i += 64) {
                     const float z = load_value<TYPE>(a.logits, row, i);
                     if (key_of(z, i) <= last) sum += r.kept(z);
                 }
@@ -345,25 +403,43 @@ __global__ __launch_bounds__(kDrawThreads) void sample_draw_kernel(Sample a) {
             }
             __syncthreads();
         } else {
-            int size = 64;
-            while (size < n) size *= 2;
-            for (int i = tid; i < size; i += kDrawThreads) sh.keys[i] = i < n ? a.ws.list[(long)row * kListed + i] : ~0ull;
-            // the list in order: a bitonic network
-            for (int run = 2; run <= size; run *= 2)
-                for (int step = run / 2; step; step /= 2) {
-                    __syncthreads();
-                    for (int p = tid; p < size / 2; p += kDrawThreads) {
-                        const int i = (p / step) * 2 * step + p % step, j = i + step;
-                        const u64 x = sh.keys[i], y = sh.keys[j];
-                        if ((x > y) == !(i & run)) sh.keys[i] = y, sh.keys[j] = x;
+            const u64 *list = a.ws.list + (long)row * kListed;
+            if (n <= kCounted) {
+                // a short list in order: a token's place is the number of those before it
+                constexpr int kParts = kDrawThreads / kCounted;
+                const int c = tid % kCounted;
+                for (int i = tid; i < kCounted; i += kDrawThreads) unsorted[i] = i < n ? list[i] : ~0ull, place[i] = 0;
+                __syncthreads();
+                const u64 own = unsorted[c];
+                int before = 0;
+#pragma unroll 8
+                for (int i = tid / kCounted; i < n; i += kParts) before += unsorted[i] < own;
+                if (before) atomicAdd(&place[c], before);
+                __syncthreads();
+                if (tid < n) sh.keys[place[c]] = own;
+            } else {
+                int size = 2 * kCounted;
+                while (size < n) size *= 2;
+                for (int i = tid; i < size; i += kDrawThreads) sh.keys[i] = i < n ? list[i] : ~0ull;
+                // a bitonic network
+                for (int run = 2; run <= size; run *= 2)
+                    for (int step = run / 2; step; step /= 2) {
+                        __syncthreads();
+                        for (int p = tid; p < size / 2; p += kDrawThreads) {
+                            const int i = (p / step) * 2 * step + p % step, j = i + step;
+                            const u64 x = sh.keys[i], y = sh.keys[j];
+                            if ((x > y) == !(i & run)) sh.keys[i] = y, sh.keys[j] = x;
+                        }
                     }
-                }
+            }
             __syncthreads();
-            // two neighbours a thread: their bins, weights, and the weight of the list before them
-            u64 key[2], w[2];
-            int bin[2];
-            for (int k = 0; k < 2; ++k) {
-                const int i = 2 * tid + k;
+            // neighbours of the list by a thread: their bins, weights, and the weight of the list before them
+            constexpr int kOwn = kListed / kDrawThreads;
+            u64 key[kOwn], w[kOwn];
+            int bin[kOwn];
+#pragma unroll
+            for (int k = 0; k < kOwn; ++k) {
+                const int i = kOwn * tid + k;
                 key[k] = i < n ? sh.keys[i] : ~0ull;
                 const float z = i < n ? logit_of(key[k]) : 0.0f;
                 bin[k] = i < n ? r.bin(z) : kBins;
@@ -375,11 +451,11 @@ __global__ __launch_bounds__(kDrawThreads) void sample_draw_kernel(Sample a) {
                 // of k_bin's tokens the first ones; other bins' come before them in the list
                 const int need = r.most - (cut.k_bin ? (int)bins.count[cut.k_bin - 1] : 0);
                 u64 at = 0;
-                for (int k = 0; k < 2; ++k) at += bin[k] < cut.k_bin;
+                for (int k = 0; k < kOwn; ++k) at += bin[k] < cut.k_bin;
                 below = (int)sum_of(at);
                 last = sh.keys[below + need - 1];
                 u64 mine = 0;
-                for (int k = 0; k < 2; ++k) mine += bin[k] == cut.k_bin && key[k] <= last ? w[k] : 0;
+                for (int k = 0; k < kOwn; ++k) mine += bin[k] == cut.k_bin && key[k] <= last ? w[k] : 0;
                 all = (cut.k_bin ? bins.mass[cut.k_bin - 1] : 0) + sum_of(mine);
             }
             if (r.share < 1) {
@@ -392,18 +468,13 @@ __global__ __launch_bounds__(kDrawThreads) void sample_draw_kernel(Sample a) {
                 const int p_bin = found;
                 const u64 rest = target - (p_bin ? bins.mass[p_bin - 1] : 0);
                 u64 mine = 0;
-                for (int k = 0; k < 2; ++k) mine += bin[k] == p_bin ? w[k] : 0;
-                u64 upto = mine;
-                for (int k = 1; k < 64; k <<= 1) {
-                    const u64 x = __shfl_up(upto, k);
-                    if (lane >= k) upto += x;
-                }
+                for (int k = 0; k < kOwn; ++k) mine += bin[k] == p_bin ? w[k] : 0;
+                const u64 upto = upto_of(mine);
                 __syncthreads();
                 if (lane == 63) part[wave] = upto;
                 __syncthreads();
-                u64 at = upto - mine;
-                for (int k = 0; k < wave; ++k) at += part[k];
-                for (int k = 0; k < 2; ++k) {
+                u64 at = upto - mine + before_wave();
+                for (int k = 0; k < kOwn; ++k) {
                     const u64 own = bin[k] == p_bin ? w[k] : 0;
                     if (at <= rest && rest < at + own) found_key = key[k];
                     at += own;
@@ -412,65 +483,73 @@ __global__ __launch_bounds__(kDrawThreads) void sample_draw_kernel(Sample a) {
                 last = min(last, found_key);
             }
             // what the list adds to the chunks
-            for (int k = 0; k < 2; ++k)
-                if (key[k] <= last && 2 * tid + k < n && bin[k] >= cut.sure) {
+            for (int k = 0; k < kOwn; ++k)
+                if (key[k] <= last && kOwn * tid + k < n && bin[k] >= cut.sure) {
                     const u64 kept = r.kept(logit_of(key[k]));
-                    if (kept) atomicAdd((unsigned long long *)&chunk_mass[(u32)key[k] / a.chunk], (unsigned long long)kept);
+                    if (kept) atomicAdd((unsigned long long *)&chunk_mass[min(max((int)(u32)key[k] - past, 0) >> a.shift, a.chunks - 1)], (unsigned long long)kept);
                 }
             __syncthreads();
         }
     } else {
         __syncthreads();
     }
-    // the chunk, then the wavefront's part of it, then the token
+    // the chunk, then the token
     u64 sum = 0;
     for (int i = tid; i < a.chunks; i += kDrawThreads) sum += chunk_mass[i];
     const u64 all = sum_of(sum);
     const double drawn = (double)a.how.u[row] * (double)all;
     u64 target = drawn > 0 ? min((u64)drawn, all - 1) : 0;
-    if (tid == 0) {
-        int c = 0;
-        while (c < a.chunks - 1 && chunk_mass[c] <= target) target -= chunk_mass[c++];
-        found = c, found_mass = target;
+    if (wave == 0) {
+        constexpr int kOf = kMostChunks / 64;
+        u64 own[kOf], mine = 0;
+        for (int k = 0; k < kOf; ++k) mine += own[k] = lane * kOf + k < a.chunks ? chunk_mass[lane * kOf + k] : 0;
+        u64 at = upto_of(mine) - mine;
+        for (int k = 0; k < kOf; ++k) {
+            if (at <= target && target < at + own[k]) found = lane * kOf + k, found_mass = target - at;
+            at += own[k];
+        }
     }
     __syncthreads();
     target = found_mass;
-    const int lo = found * a.chunk, hi = min(a.vocab, lo + a.chunk), each = ((a.chunk + kWaves - 1) / kWaves + 63) / 64 * 64;
-    const int begin = lo + wave * each, end = min(hi, begin + each);
-    auto kept = [&](int i) {
-        if (i >= end) return (u64)0;
-        const float z = load_value<TYPE>(a.logits, row, i);
-        return key_of(z, i) <= last ? r.kept(z) : (u64)0;
-    };
-    sum = 0;
-    for (int i = begin + lane; i - lane < end; i += 64) sum += kept(i);
-    sum = wave_sum(sum);
-    __syncthreads();
-    if (lane == 0) part[wave] = sum;
-    __syncthreads();
-    u64 before = 0;
-    for (int k = 0; k < wave; ++k) before += part[k];
-    if (before <= target && target < before + part[wave]) {
-        for (int i = begin + lane; i - lane < end; i += 64) {
-            const u64 w = kept(i);
-            u64 upto = w;
-            for (int k = 1; k < 64; k <<= 1) {
-                const u64 x = __shfl_up(upto, k);
-                if (lane >= k) upto += x;
-            }
-            upto += before;
-            if (upto - w <= target && target < upto) a.tokens[row] = i;
-            before = __shfl(upto, 63);
+    // the chunk's tokens in runs of a thread each, all of them at once where a chunk is as usual
+    constexpr int kRun = 8;
+    const int hi = a.from<TYPE>(row, found + 1);
+    for (int lo = a.from<TYPE>(row, found); lo < hi; lo += kRun * kDrawThreads) {
+        float z[kRun];
+        u64 w[kRun], mine = 0;
+#pragma unroll
+        for (int k = 0; k < kRun; ++k) z[k] = load_value<TYPE>(a.logits, row, min(lo + tid * kRun + k, hi - 1));
+#pragma unroll
+        for (int k = 0; k < kRun; ++k) {
+            const int i = lo + tid * kRun + k;
+            mine += w[k] = i < hi && key_of(z[k], i) <= last ? r.kept(z[k]) : 0;
         }
+        const u64 upto = upto_of(mine);
+        __syncthreads();
+        if (lane == 63) part[wave] = upto;
+        __syncthreads();
+        u64 at = before_wave() + upto - mine;
+        if (at <= target && target < at + mine)
+            for (int k = 0; k < kRun; ++k) {
+                if (at <= target && target < at + w[k]) a.tokens[row] = lo + tid * kRun + k;
+                at += w[k];
+            }
+        const u64 run = wave_sum(lane < kWaves ? part[lane] : 0);
+        if (target < run) break;
+        target -= run;
     }
 }
 
-// chunks of a row: enough workgroups for the card, none with fewer tokens than its threads load at once
-void chunks_of(int rows, int vocab, int *chunks, int *chunk) {
-    const int most = std::min(kMostChunks, (vocab + 2047) / 2048), wanted = (512 + rows - 1) / std::max(rows, 1);
-    *chunks = std::max(1, std::min(most, wanted));
-    *chunk = (int)(((long)vocab + *chunks - 1) / *chunks);
-    *chunks = (int)(((long)vocab + *chunk - 1) / *chunk);
+// Chunks of a row: 4096 tokens, 2048 where rows alone do not fill the card, more where a row would have too many.  Workgroups of a row: enough for the card, with whole
+// chunks each.
+void cut_up(Sample &a) {
+    a.shift = a.rows < 32 ? 11 : 12;
+    while (((long)a.vocab + (1l << a.shift) - 1) >> a.shift > kMostChunks) ++a.shift;
+    a.chunk = 1 << a.shift;
+    a.chunks = (int)(((long)a.vocab + a.chunk - 1) / a.chunk);
+    const int wanted = std::max(1, std::min(a.chunks, (512 + a.rows - 1) / std::max(a.rows, 1)));
+    a.each = (a.chunks + wanted - 1) / wanted;
+    a.groups = (a.chunks + a.each - 1) / a.each;
 }
 
 }  // namespace
@@ -478,23 +557,24 @@ void chunks_of(int rows, int vocab, int *chunks, int *chunk) {
 namespace gala {
 
 size_t sample_workspace(int rows, int vocab) {
-    int chunks, chunk;
-    chunks_of(rows, vocab, &chunks, &chunk);
-    return (size_t)rows * (kBins * 12 + kListed * 8 + chunks * 16 + 8);
+    Sample a{};
+    a.rows = rows, a.vocab = vocab;
+    cut_up(a);
+    return (size_t)rows * (kBins * 12 + kListed * 8 + (a.chunks + a.groups) * 8 + 8);
 }
 
 int launch_sample(void *stream, const Values &logits, int rows, int vocab, const gala_sampling &how, int *tokens, void *workspace) {
     Sample a{};
     a.logits = logits, a.rows = rows, a.vocab = vocab, a.how = how, a.tokens = tokens;
-    chunks_of(rows, vocab, &a.chunks, &a.chunk);
+    cut_up(a);
     u64 *at = (u64 *)workspace;
     a.ws.mass = at, at += (size_t)rows * kBins;
     a.ws.list = at, at += (size_t)rows * kListed;
-    a.ws.best = at, at += (size_t)rows * a.chunks;
+    a.ws.best = at, at += (size_t)rows * a.groups;
     a.ws.sure = at, at += (size_t)rows * a.chunks;
     a.ws.count = (u32 *)at;
     a.ws.listed = a.ws.count + (size_t)rows * kBins;
-    const dim3 grid(rows * a.chunks);
+    const dim3 grid(rows * a.groups);
     hipStream_t st = (hipStream_t)stream;
     by_type(logits.type, [&](auto type) {
         constexpr int T = decltype(type)::value;
