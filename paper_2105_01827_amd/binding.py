@@ -7,7 +7,9 @@ device pointers and numpy ``uint64`` arrays for host pointers.  The library
 must be present: there is no fallback path.
 """
 import ctypes as C
+import math
 import os
+import struct
 
 import numpy as np
 
@@ -51,10 +53,6 @@ class ConvPolyphase(C.Structure):
                 [(k, C.c_int32) for k in ("c_i_poly", "k_h_poly", "k_w_poly", "out_h", "out_w")])
 
 
-class ValuesArg(C.Structure):
-    _fields_ = [("data", C.c_void_p), ("stride", C.c_int64), ("type", C.c_int32), ("unit", C.c_float)]
-
-
 class KvCacheArg(C.Structure):
     _fields_ = [(k, C.c_int32) for k in ("heads", "head_dim", "pages", "reserved")] + [("codes", C.c_void_p),
                                                                                       ("scales", C.c_void_p)]
@@ -67,10 +65,6 @@ class KvBatchArg(C.Structure):
 
 class RopeArg(C.Structure):
     _fields_ = [("table", C.c_void_p)] + [(k, C.c_int32) for k in ("positions", "rot_dim", "interleaved", "reserved")]
-
-
-class SamplingArg(C.Structure):
-    _fields_ = [(k, C.c_void_p) for k in ("temperature", "top_k", "top_p", "min_p", "u")]
 
 
 class OpCount(C.Structure):
@@ -208,6 +202,10 @@ def _dev(t):
     return C.c_void_p(t if isinstance(t, int) else t.data_ptr())
 
 
+def _at(t):
+    return t if isinstance(t, int) else t.data_ptr()
+
+
 def _stream(s):
     if s is None:
         return None
@@ -216,26 +214,33 @@ def _stream(s):
 
 _TYPES = {"torch.float32": 0, "torch.float16": 1, "torch.bfloat16": 2, "torch.int64": 3, "torch.uint64": 3}
 _types = {}                                    # the same by the dtype itself, filled as dtypes are met
+_named = {}                                    # dtypes by their names, likewise
+_pack_values = struct.Struct("Pqif").pack      # gala_values
+_pack_sampling = struct.Struct("PPPPP").pack   # gala_sampling
 
 
 def _values(t, unit):
-    """gala_values of a tensor: rows are its first dimension, the rest of a row has to be contiguous."""
+    """gala_values of a tensor, as bytes: rows are its first dimension, the rest of a row has to be contiguous."""
     kind = _types.get(t.dtype)
     if kind is None:
         if str(t.dtype) not in _TYPES:
             raise TypeError(f"values are float32, float16, bfloat16, or residues in 64-bit words: got {t.dtype}")
         kind = _types[t.dtype] = _TYPES[str(t.dtype)]
-    strides, step = t.stride(), 1
-    for size, stride in zip(reversed(t.shape[1:]), reversed(strides[1:])):
-        if size != 1 and stride != step:
+    strides, shape, step = t.stride(), t.shape, 1
+    for i in range(len(strides) - 1, 0, -1):
+        if strides[i] != step and shape[i] != 1:
             raise ValueError("the values of a row have to be contiguous")
-        step *= size
-    return ValuesArg(t.data_ptr(), strides[0], kind, unit)
+        step *= shape[i]
+    return _pack_values(t.data_ptr(), strides[0], kind, unit)
 
 
 def _words(t, dtype, what):
-    if str(t.dtype) != dtype or not t.is_contiguous():
-        raise TypeError(f"{what} has to be a contiguous {dtype} tensor")
+    if t.dtype is not _named.get(dtype):
+        if str(t.dtype) != dtype:
+            raise TypeError(f"{what} has to be a {dtype} tensor")
+        _named[dtype] = t.dtype
+    if not t.is_contiguous():
+        raise TypeError(f"{what} has to be contiguous")
     return t.data_ptr()
 
 
@@ -422,15 +427,21 @@ class Context:
                unit=1.0, stream=None):
         """logits (rows, vocab) -> tokens (rows,) int32; the numbers a row are float32 tensors, top_k int32."""
         rows, vocab = logits.shape
-        per_row = [("temperature", temperature, "torch.float32"), ("top_k", top_k, "torch.int32"),
-                   ("top_p", top_p, "torch.float32"), ("min_p", min_p, "torch.float32"), ("u", u, "torch.float32"),
-                   ("tokens", tokens, "torch.int32")]
-        for name, t, dtype in per_row:
-            if t is not None and t.numel() != rows:
-                raise ValueError(f"{name} has to have one number a row")
-        at = [None if t is None else _words(t, dtype, name) for name, t, dtype in per_row]
-        _check(self.lib.gala_sample(self.h, _stream(stream), C.byref(_values(logits, unit)), rows, vocab,
-                                    C.byref(SamplingArg(*at[:5])), at[5], _dev(workspace), workspace_bytes), "gala_sample")
+        at = [self._per_row(t, rows, "torch.float32", name) for t, name in
+              ((temperature, "temperature"), (top_p, "top_p"), (min_p, "min_p"), (u, "u"))]
+        top_k = self._per_row(top_k, rows, "torch.int32", "top_k")
+        _check(self.lib.gala_sample(self.h, _stream(stream), _values(logits, unit), rows, vocab,
+                                    _pack_sampling(at[0], top_k, at[1], at[2], at[3]),
+                                    self._per_row(tokens, rows, "torch.int32", "tokens"), _at(workspace), workspace_bytes),
+               "gala_sample")
+
+    @staticmethod
+    def _per_row(t, rows, dtype, name):
+        if t is None:
+            return 0
+        if t.numel() != rows:
+            raise ValueError(f"{name} has to have one number a row")
+        return _words(t, dtype, name)
 
 
 class SecretKey:
@@ -694,22 +705,25 @@ class KvCache:
     def page_bytes(heads, head_dim):
         return int(load().gala_kv_cache_bytes(1, heads, head_dim))
 
+    def _heads(self, q):
+        return math.prod(q.shape[1:]) // self.head_dim
+
     def append(self, batch, k, v, q=None, q_out=None, rope=None, unit=1.0, stream=None):
         """k, v (rows, heads, head_dim) into the cache; q (rows, heads_q, head_dim) rotated into q_out."""
-        heads_q = 0 if q is None else q[:1].numel() // self.head_dim
         _check(self.ctx.lib.gala_kv_append(self.ctx.h, _stream(stream), self.ref, batch.ref, None if rope is None else rope.ref,
-                                           heads_q, *(None if t is None else C.byref(_values(t, unit)) for t in (q, q_out, k, v))),
-               "gala_kv_append")
+                                           0 if q is None else self._heads(q), None if q is None else _values(q, unit),
+                                           None if q_out is None else _values(q_out, unit), None if k is None else _values(k, unit),
+                                           None if v is None else _values(v, unit)), "gala_kv_append")
 
     def export(self, batch, k_out, v_out, unit=1.0, stream=None):
-        _check(self.ctx.lib.gala_kv_export(self.ctx.h, _stream(stream), self.ref, batch.ref, C.byref(_values(k_out, unit)),
-                                           C.byref(_values(v_out, unit))), "gala_kv_export")
+        _check(self.ctx.lib.gala_kv_export(self.ctx.h, _stream(stream), self.ref, batch.ref, _values(k_out, unit),
+                                           _values(v_out, unit)), "gala_kv_export")
 
     def attention_workspace_bytes(self, batch, heads_q, window=0, sinks=0):
         return int(self.ctx.lib.gala_kv_attention_workspace(self.ref, batch.ref, heads_q, window, sinks))
 
     def attention(self, batch, q, out, scale, workspace, workspace_bytes, window=0, sinks=0, unit=1.0, stream=None):
         """q (rows, heads_q, head_dim) -> out of the same shape."""
-        _check(self.ctx.lib.gala_kv_attention(self.ctx.h, _stream(stream), self.ref, batch.ref, q[:1].numel() // self.head_dim,
-                                              scale, window, sinks, C.byref(_values(q, unit)), C.byref(_values(out, unit)),
-                                              _dev(workspace), workspace_bytes), "gala_kv_attention")
+        _check(self.ctx.lib.gala_kv_attention(self.ctx.h, _stream(stream), self.ref, batch.ref, self._heads(q), scale, window, sinks,
+                                              _values(q, unit), _values(out, unit), _at(workspace), workspace_bytes),
+               "gala_kv_attention")

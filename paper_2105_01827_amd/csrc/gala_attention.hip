@@ -20,6 +20,7 @@ constexpr float kLog2E = 1.4426950408889634f;
 struct Attention {
     KvArgs kv;
     Values q, out;
+    bool pieces;                     // rows of q lie on 16 bytes
     int heads_q, group;              // group: query heads of a head of the cache
     float scale;
     int window, sinks;
@@ -48,7 +49,7 @@ __device__ __forceinline__ Seen seen_by(const Attention &a, int b, int tile) {
     const int last = end > 0 ? (end + kKvBlock - 1) / kKvBlock : 0;
     s.begin = a.window ? min(max(0, s.at_lo - a.window + 1) / kKvBlock, last) : 0;
     s.first = min((int)min((long)a.sinks + kKvBlock - 1, 0x7fffffffl) / kKvBlock, s.begin);
-    s.total = s.cols ? s.first + last - s.begin : 0;
+    s.total = s.cols && a.kv.pages ? s.first + last - s.begin : 0;
     return s;
 }
 // blocks of a share
@@ -57,12 +58,30 @@ __device__ __forceinline__ int share_of(int total, int splits) {
     return (each + kWaves - 1) / kWaves * kWaves;
 }
 
-__device__ __forceinline__ float load_any(const Values &v, long row, int column) {
-    switch (v.type) {
-        case GALA_F32: return load_value<GALA_F32>(v, row, column);
-        case GALA_F16: return load_value<GALA_F16>(v, row, column);
-        case GALA_BF16: return load_value<GALA_BF16>(v, row, column);
-        default: return load_value<GALA_RESIDUE>(v, row, column);
+// 16 channels of a row from `column` on, 0 from `end` on; eight at a load where rows lie on 16 bytes
+template <int TYPE>
+__device__ __forceinline__ void load_channels(const Values &v, bool pieces, long row, int column, int end, float (&x)[16]) {
+    typedef typename Element<TYPE>::type E;
+    if (pieces) {
+#pragma unroll
+        for (int p = 0; p < 2; ++p) {
+            union {
+                int4 word[sizeof(E) / 2];
+                E e[8];
+            } u;
+#pragma unroll
+            for (int k = 0; k < (int)sizeof(E) / 2; ++k) u.word[k] = int4{0, 0, 0, 0};
+            if (column + 8 * p < end) {
+                const int4 *from = (const int4 *)((const E *)v.data + row * v.stride + column + 8 * p);
+#pragma unroll
+                for (int k = 0; k < (int)sizeof(E) / 2; ++k) u.word[k] = from[k];
+            }
+#pragma unroll
+            for (int k = 0; k < 8; ++k) x[8 * p + k] = to_float<TYPE>(u.e[k], v.unit, v.p);
+        }
+    } else {
+#pragma unroll
+        for (int k = 0; k < 16; ++k) x[k] = column + k < end ? load_value<TYPE>(v, row, column + k) : 0.0f;
     }
 }
 __device__ __forceinline__ void store_any(const Values &v, long row, int column, float x) {
@@ -114,7 +133,7 @@ __device__ __forceinline__ float joined(const v4i (&acc)[ND], int r) {
 // lie in that order of tokens.  So a block goes from memory to the sums without LDS or an exchange between lanes, but
 // for the largest score.  A wavefront has blocks of its own; a workgroup's wavefronts are joined at the end.
 template <int NC, int ND>
-__global__ __launch_bounds__(64 * kWaves) void kv_attention_kernel(Attention a) {
+__global__ __launch_bounds__(64 * kWaves, NC * ND <= 6 ? 2 : 1) void kv_attention_kernel(Attention a) {
     constexpr int NV = 4 * NC;
     __shared__ float sums[kWaves][kColumns][NV * 16 + 1];
     __shared__ float stats[kWaves][kColumns][2];
@@ -130,6 +149,31 @@ __global__ __launch_bounds__(64 * kWaves) void kv_attention_kernel(Attention a) 
     if (!s.cols) return;
     const int share = share_of(s.total, a.splits), from = split * share, to = min(s.total, from + share);
     if (split && from >= s.total) return;
+    // The next block's keys and scales are under way while this one's weights are made, the one after's page too.
+    const size_t head_bytes = kv_head_bytes(kv.dim16);
+    v4i keys[4][NC];
+    float scale_k = 0, scale_v = 0;
+    int u = from + wave, page, page_next;
+    auto page_at = [&](int v) { return v < to ? page_of(kv, b, s.block(v)) : -1; };
+    auto load_keys = [&]() __attribute__((always_inline)) {
+        // without a page the first one is read and not seen: no branch around what is under way
+        const size_t head = (size_t)max(page, 0) * kv.heads + h;
+        const signed char *codes = kv.codes + head * head_bytes;
+        scale_k = kv.scales[2 * head], scale_v = page < 0 ? 0.0f : kv.scales[2 * head + 1];
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int k = 0; k < NC; ++k)       // channels beyond the head's meet digits of 0; what is read there is the head's
+                keys[i][k] = *(const v4i *)(codes + (size_t)(i * kv.dim16 + k * 4 + part) * 256 + col * 16);
+    };
+    page = page_at(u), page_next = page_at(u + kWaves);
+    if (u < to) load_keys();
+    // from block u to the next one
+    auto step = [&]() __attribute__((always_inline)) {
+        page = page_next;
+        load_keys();
+        page_next = page_at(u + 2 * kWaves);
+    };
     // the column's query: digits, and what one unit of them is worth
     const int c = s.col0 + min(col, s.cols - 1), qi = c / a.group, g = c % a.group;
     const long row = s.start + qi;
@@ -140,12 +184,18 @@ __global__ __launch_bounds__(64 * kWaves) void kv_attention_kernel(Attention a) 
     {
         float x[NC][16], most = 0;
         bool fine = true;
+        auto load = [&](auto type) __attribute__((always_inline)) {
+#pragma unroll
+            for (int k = 0; k < NC; ++k) {
+                const int d = k * 64 + part * 16;
+                load_channels<decltype(type)::value>(a.q, a.pieces, row, hq * kv.dim + d, hq * kv.dim + kv.dim, x[k]);
+            }
+        };
+        by_type(a.q.type, load);
 #pragma unroll
         for (int k = 0; k < NC; ++k)
 #pragma unroll
             for (int j = 0; j < 16; ++j) {
-                const int d = k * 64 + part * 16 + j;
-                x[k][j] = d < kv.dim ? load_any(a.q, row, hq * kv.dim + d) : 0.0f;
                 most = fmaxf(most, fabsf(x[k][j]));
                 fine &= fabsf(x[k][j]) < INFINITY;
             }
@@ -157,8 +207,8 @@ __global__ __launch_bounds__(64 * kWaves) void kv_attention_kernel(Attention a) 
         bad = !all;
         const bool some = most > 0 && !bad;
         // a power of two first: the reciprocal of a tiny number would be infinite
-        const int e = some ? ilogbf(most) : 0;
-        const float scaled = ldexpf(some ? most : 1.0f, -e), mul = Digits<ND>::most / scaled * (a.scale < 0 ? -1.0f : 1.0f);
+        const int e = some ? min(max(ilogbf(most), -126), 126) : 0;
+        const float down = ldexpf(1.0f, -e), scaled = some ? most * down : 1.0f, mul = Digits<ND>::most / scaled * (a.scale < 0 ? -1.0f : 1.0f);
         unit_q = ldexpf(scaled / Digits<ND>::most, e) * fabsf(a.scale) * kLog2E;
 #pragma unroll
         for (int k = 0; k < NC; ++k)
@@ -167,7 +217,7 @@ __global__ __launch_bounds__(64 * kWaves) void kv_attention_kernel(Attention a) 
                 u32 w[4];
 #pragma unroll
                 for (int r = 0; r < 4; ++r) {
-                    const int v = some ? (int)rintf(ldexpf(x[k][4 * j + r], -e) * mul) : 0;
+                    const int v = some ? (int)rintf(x[k][4 * j + r] * down * mul) : 0;
                     w[r] = (u32)(v + (ND == 2 ? 128 : 128 * 257));
                 }
                 planes<ND>(w, j, qd[k]);
@@ -177,19 +227,11 @@ __global__ __launch_bounds__(64 * kWaves) void kv_attention_kernel(Attention a) 
 #pragma unroll
     for (int j = 0; j < NV; ++j) o[j] = v4f{0, 0, 0, 0};
     float top = -INFINITY, sum = 0;
-    const size_t head_bytes = kv_head_bytes(kv.dim16);
-    for (int u = from + wave; u < to; u += kWaves) {
-        const int block = s.block(u), page = page_of(kv, b, block);
-        if (page < 0) continue;
-        const signed char *codes = kv.codes + ((size_t)page * kv.heads + h) * head_bytes;
-        const float *scales = kv.scales + ((size_t)page * kv.heads + h) * 2;
-        const float unit_s = unit_q * scales[0], unit_v = scales[1] * (1.0f / Digits<ND>::most);
-        v4i keys[4][NC], values[NV];
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-#pragma unroll
-            for (int k = 0; k < NC; ++k)       // channels beyond the head's meet digits of 0; what is read there is the head's
-                keys[i][k] = *(const v4i *)(codes + (size_t)(i * kv.dim16 + k * 4 + part) * 256 + col * 16);
+    for (; u < to; u += kWaves) {
+        const int block = s.block(u), end = page < 0 ? 0 : kv.max_len;
+        const signed char *codes = kv.codes + ((size_t)max(page, 0) * kv.heads + h) * head_bytes;
+        const float unit_s = unit_q * scale_k, unit_v = scale_v * (1.0f / Digits<ND>::most);
+        v4i values[NV];
 #pragma unroll
         for (int j = 0; j < NV; ++j)
             if (j < kv.dim16) values[j] = *(const v4i *)(codes + (size_t)kKvBlock * 16 * kv.dim16 + j * 1024 + lane * 16);
@@ -206,10 +248,11 @@ __global__ __launch_bounds__(64 * kWaves) void kv_attention_kernel(Attention a) 
 #pragma unroll
             for (int r = 0; r < 4; ++r) t[4 * i + r] = joined<ND>(acc, r) * unit_s;
         }
+        step();
         const int t0 = block * kKvBlock;
-        if (t0 + 63 > s.at_lo || t0 + 64 > kv.max_len || (a.window && t0 <= s.at_hi - a.window)) {
+        if (t0 + 63 > s.at_lo || t0 + 64 > end || (a.window && t0 <= s.at_hi - a.window)) {
             // keys of the block by their distance from the lane's first one; no branches between them
-            const int own = t0 + part * 4, hi = min(at, kv.max_len - 1) - own;
+            const int own = t0 + part * 4, hi = min(at, end - 1) - own;
             const int lo = a.window ? at - a.window + 1 - own : -kKvBlock, sinks = a.window ? a.sinks - own : 0;
 #pragma unroll
             for (int i = 0; i < 4; ++i)
@@ -286,9 +329,13 @@ __global__ __launch_bounds__(64 * kWaves) void kv_attention_kernel(Attention a) 
     }
 }
 
-// The shares of one query's keys in one.
-__global__ __launch_bounds__(kMaxHeadDim) void kv_attention_join_kernel(Attention a) {
+// The shares of one query's keys in one: a wavefront takes every eighth share, a lane channels 64 apart.
+constexpr int kJoinWaves = 8;
+template <int NC>
+__global__ __launch_bounds__(64 * kJoinWaves) void kv_attention_join_kernel(Attention a) {
+    __shared__ float parts[kJoinWaves][NC * 64 + 1];
     const KvArgs &kv = a.kv;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     int unit = blockIdx.x;
     const int cc = unit % a.columns;
     unit /= a.columns;
@@ -299,21 +346,32 @@ __global__ __launch_bounds__(kMaxHeadDim) void kv_attention_join_kernel(Attentio
     if (cc >= s.cols) return;
     const int share = share_of(s.total, a.splits), used = share ? max(1, (s.total + share - 1) / share) : 1;
     const long place = (((long)b * kv.heads + h) * a.tiles + tile) * a.splits;
-    float most = -INFINITY, all = 0, x = 0;
-    for (int k = 0; k < used; ++k) {
-        const float t = a.stats[((place + k) * a.columns + cc) * 2];
-        most = t != t ? t : fmaxf(most, t);
-    }
+    const float *stats = a.stats + (place * a.columns + cc) * 2, *sums = a.sums + (place * a.columns + cc) * kv.dim;
+    const long next = a.columns;
+    float most = -INFINITY, all = 0, x[NC];
+    for (int k = lane; k < used; k += 64) most = fmaxf(most, stats[k * next * 2]);
+    for (int k = 32; k; k >>= 1) most = fmaxf(most, __shfl_xor(most, k));
     const float base = most == -INFINITY ? 0.0f : most;
-    const int d = threadIdx.x;
-    for (int k = 0; k < used; ++k) {
-        const long from = (place + k) * a.columns + cc;
-        const float f = __builtin_amdgcn_exp2f(a.stats[from * 2] - base);
-        all += f * a.stats[from * 2 + 1];
-        if (d < kv.dim) x += f * a.sums[from * kv.dim + d];
+#pragma unroll
+    for (int j = 0; j < NC; ++j) x[j] = 0;
+#pragma unroll 4
+    for (int k = wave; k < used; k += kJoinWaves) {
+        const float f = __builtin_amdgcn_exp2f(stats[k * next * 2] - base);           // NaN where the query is
+        all += f * stats[k * next * 2 + 1];
+#pragma unroll
+        for (int j = 0; j < NC; ++j) x[j] += f * sums[k * next * kv.dim + min(lane + 64 * j, kv.dim - 1)];
     }
-    const int column = s.col0 + cc;
-    if (d < kv.dim) store_any(a.out, s.start + column / a.group, (h * a.group + column % a.group) * kv.dim + d, all == 0 ? 0.0f : x / all);
+#pragma unroll
+    for (int j = 0; j < NC; ++j) parts[wave][lane + 64 * j] = x[j];
+    if (lane == 0) parts[wave][NC * 64] = all;
+    __syncthreads();
+    for (int d = threadIdx.x; d < kv.dim; d += 64 * kJoinWaves) {
+        float sum = 0, out = 0;
+#pragma unroll
+        for (int k = 0; k < kJoinWaves; ++k) sum += parts[k][NC * 64], out += parts[k][d];
+        const int column = s.col0 + cc;
+        store_any(a.out, s.start + column / a.group, (h * a.group + column % a.group) * kv.dim + d, sum == 0 ? 0.0f : out / sum);
+    }
 }
 
 // How a call is cut up.
@@ -330,7 +388,7 @@ Cut cut_of(const KvArgs &kv, int heads_q, int window, int sinks) {
     const long reach = std::min<long>(kv.max_len, (long)kv.table_stride * kKvBlock);
     const long keys = window ? std::min(reach, (long)window + kv.max_new + sinks + 2 * kKvBlock) : reach;
     const long blocks = std::max(1l, (keys + kKvBlock - 1) / kKvBlock), units = std::max(1l, (long)kv.count * kv.heads * c.tiles);
-    c.splits = (int)std::max(1l, std::min((2048 + units - 1) / units, (blocks + 2 * kWaves - 1) / (2 * kWaves)));
+    c.splits = (int)std::max(1l, std::min((512 + units - 1) / units, (blocks + 31) / 32));
     return c;
 }
 
@@ -348,6 +406,8 @@ int launch_kv_attention(void *stream, const KvArgs &kv, int heads_q, float scale
     const Cut c = cut_of(kv, heads_q, window, sinks);
     Attention a{};
     a.kv = kv, a.q = q, a.out = out;
+    const size_t size = q.type == GALA_F32 ? 4 : q.type == GALA_RESIDUE ? 8 : 2;
+    a.pieces = (uintptr_t)q.data % 16 == 0 && q.stride * size % 16 == 0 && kv.dim % 8 == 0;
     a.heads_q = heads_q, a.group = heads_q / kv.heads;
     a.scale = scale, a.window = window, a.sinks = sinks;
     a.tiles = c.tiles, a.splits = c.splits, a.columns = c.columns;
@@ -361,17 +421,15 @@ int launch_kv_attention(void *stream, const KvArgs &kv, int heads_q, float scale
             hipLaunchKernelGGL((kv_attention_kernel<NC, 3>), dim3(groups), dim3(64 * kWaves), 0, (hipStream_t)stream, a);
         else
             hipLaunchKernelGGL((kv_attention_kernel<NC, 2>), dim3(groups), dim3(64 * kWaves), 0, (hipStream_t)stream, a);
+        if (c.splits == 1) return;
+        const unsigned rows = (unsigned)((long)kv.count * kv.heads * c.tiles * c.columns);
+        hipLaunchKernelGGL(kv_attention_join_kernel<NC>, dim3(rows), dim3(64 * kJoinWaves), 0, (hipStream_t)stream, a);
     };
     switch ((kv.dim + 63) / 64) {
         case 1: launch(std::integral_constant<int, 1>()); break;
         case 2: launch(std::integral_constant<int, 2>()); break;
         case 3: launch(std::integral_constant<int, 3>()); break;
         default: launch(std::integral_constant<int, 4>()); break;
-    }
-    if (hipGetLastError() != hipSuccess) return 1;
-    if (c.splits > 1) {
-        const unsigned rows = (unsigned)((long)kv.count * kv.heads * c.tiles * c.columns);
-        hipLaunchKernelGGL(kv_attention_join_kernel, dim3(rows), dim3((kv.dim + 63) / 64 * 64), 0, (hipStream_t)stream, a);
     }
     return hipGetLastError() != hipSuccess;
 }

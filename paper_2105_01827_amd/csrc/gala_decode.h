@@ -93,7 +93,7 @@ __device__ __forceinline__ void store_value(const Values &v, long row, int colum
 }
 // f with the type as a constant
 template <class F>
-inline void by_type(int type, F f) {
+__host__ __device__ inline void by_type(int type, F f) {
     switch (type) {
         case GALA_F32: f(std::integral_constant<int, GALA_F32>()); break;
         case GALA_F16: f(std::integral_constant<int, GALA_F16>()); break;

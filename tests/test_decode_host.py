@@ -81,6 +81,14 @@ def _args(**change):
     return a
 
 
+class ValuesArg(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("stride", C.c_int64), ("type", C.c_int32), ("unit", C.c_float)]
+
+
+class SamplingArg(C.Structure):
+    _fields_ = [(k, C.c_void_p) for k in ("temperature", "top_k", "top_p", "min_p", "u")]
+
+
 def _struct(cls, fields):
     return None if fields is None else C.byref(cls(**fields))
 
@@ -88,7 +96,7 @@ def _struct(cls, fields):
 def _append(ctx, a):
     return ctx.lib.gala_kv_append(ctx.h, None, _struct(binding.KvCacheArg, a["cache"]), _struct(binding.KvBatchArg, a["batch"]),
                                   _struct(binding.RopeArg, a["rope"]), a["heads_q"],
-                                  *(_struct(binding.ValuesArg, a[k]) for k in ("q", "q_out", "k", "v")))
+                                  *(_struct(ValuesArg, a[k]) for k in ("q", "q_out", "k", "v")))
 
 
 BAD_CACHE = [dict(cache=None), dict(cache__heads=0), dict(cache__head_dim=0), dict(cache__head_dim=257), dict(cache__pages=-1),
@@ -114,7 +122,7 @@ def test_append_refuses(ctx, change):
 def test_export_refuses(ctx, change):
     a = _args(**change)
     assert ctx.lib.gala_kv_export(ctx.h, None, _struct(binding.KvCacheArg, a["cache"]), _struct(binding.KvBatchArg, a["batch"]),
-                                  _struct(binding.ValuesArg, a["k"]), _struct(binding.ValuesArg, a["v"])) == EARG
+                                  _struct(ValuesArg, a["k"]), _struct(ValuesArg, a["v"])) == EARG
 
 
 @pytest.mark.parametrize("change", BAD_CACHE + BAD_BATCH + BAD_GRID + [
@@ -129,7 +137,7 @@ def test_attention_refuses(ctx, change):
     if "workspace" in change and not need:
         pytest.skip("no workspace is needed")
     got = ctx.lib.gala_kv_attention(ctx.h, None, cache, batch, a["heads_q"], a["scale"], a["window"], a["sinks"],
-                                    _struct(binding.ValuesArg, a["q"]), _struct(binding.ValuesArg, a["q_out"]), a["workspace"], 1 << 40)
+                                    _struct(ValuesArg, a["q"]), _struct(ValuesArg, a["q_out"]), a["workspace"], 1 << 40)
     assert got == EARG
 
 
@@ -139,16 +147,16 @@ def test_attention_wants_its_workspace(ctx):
     need = ctx.lib.gala_kv_attention_workspace(cache, batch, 4, 0, 0)
     if not need:
         pytest.skip("no workspace is needed")
-    assert ctx.lib.gala_kv_attention(ctx.h, None, cache, batch, 4, 1.0, 0, 0, _struct(binding.ValuesArg, a["q"]),
-                                     _struct(binding.ValuesArg, a["q_out"]), AT, need - 1) == ENOMEM
+    assert ctx.lib.gala_kv_attention(ctx.h, None, cache, batch, 4, 1.0, 0, 0, _struct(ValuesArg, a["q"]),
+                                     _struct(ValuesArg, a["q_out"]), AT, need - 1) == ENOMEM
 
 
 @pytest.mark.parametrize("change", [dict(logits=None), dict(rows=-1), dict(vocab=0), dict(how=None), dict(tokens=0), dict(u=0),
                                     dict(type=9), dict(type=3, unit=0.0), dict(stride=-5), dict(data=AT + 2)])
 def test_sample_refuses(ctx, change):
     a = dict(data=AT, stride=100, type=0, unit=1.0, rows=3, vocab=100, u=AT, tokens=AT) | change
-    logits = None if "logits" in change else C.byref(binding.ValuesArg(a["data"], a["stride"], a["type"], a["unit"]))
-    how = None if "how" in change else C.byref(binding.SamplingArg(0, 0, 0, 0, a["u"]))
+    logits = None if "logits" in change else C.byref(ValuesArg(a["data"], a["stride"], a["type"], a["unit"]))
+    how = None if "how" in change else C.byref(SamplingArg(0, 0, 0, 0, a["u"]))
     assert ctx.lib.gala_sample(ctx.h, None, logits, a["rows"], a["vocab"], how, a["tokens"], AT, 1 << 40) == EARG
 
 
@@ -158,8 +166,8 @@ def test_binding_refuses_tensors_that_do_not_fit(ctx):
         binding._values(torch.zeros(4, 8, dtype=torch.float64), 1.0)
     with pytest.raises(ValueError):
         binding._values(torch.zeros(4, 8, 6).transpose(1, 2), 1.0)
-    v = binding._values(torch.zeros(4, 24)[:, 8:16].view(4, 2, 4), 1.0)
-    assert (v.stride, v.type) == (24, 0)
+    v = ValuesArg.from_buffer_copy(binding._values(torch.zeros(4, 24)[:, 8:16].view(4, 2, 4), 0.5))
+    assert (v.stride, v.type, v.unit) == (24, 0, 0.5)
     with pytest.raises(TypeError):
         binding.KvBatch(torch.zeros(3, dtype=torch.int64), torch.zeros(2, dtype=torch.int32), torch.zeros(2, 1, dtype=torch.int32), 1, 1)
     with pytest.raises(ValueError):

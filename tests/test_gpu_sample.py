@@ -175,9 +175,8 @@ def test_no_rows(ctx):
     ws = torch.zeros(16, dtype=torch.uint8, device="cuda")
     t = torch.zeros(1, dtype=torch.int32, device="cuda")
     z = torch.zeros(1, 10, device="cuda")
-    how = binding.SamplingArg(0, 0, 0, 0, z.data_ptr())
-    import ctypes as C
-    assert ctx.lib.gala_sample(ctx.h, None, C.byref(binding._values(z, 1.0)), 0, 10, C.byref(how), t.data_ptr(), ws.data_ptr(), 16) == 0
+    how = binding._pack_sampling(0, 0, 0, 0, z.data_ptr())
+    assert ctx.lib.gala_sample(ctx.h, None, binding._values(z, 1.0), 0, 10, how, t.data_ptr(), ws.data_ptr(), 16) == 0
 
 
 def test_another_stream_and_a_graph(ctx):
