@@ -20,7 +20,7 @@ constexpr float kLog2E = 1.4426950408889634f;
 struct Attention {
     KvArgs kv;
     Values q, out;
-    bool pieces;                     // rows of q lie on 16 bytes
+    bool pieces, out_quads;          // rows of q lie on 16 bytes, those of out on four values
     int heads_q, group;              // group: query heads of a head of the cache
     float scale;
     int window, sinks;
@@ -36,13 +36,13 @@ struct Seen {
 
     __device__ int block(int u) const { return u < first ? u : begin + (u - first); }
 };
-__device__ __forceinline__ Seen seen_by(const Attention &a, int b, int tile) {
+__device__ __forceinline__ Seen seen_by(const Attention &a, int b, int tile, int columns = kColumns) {
     Seen s;
     s.start = a.kv.starts[b];
     const int all = a.kv.starts[b + 1] - s.start, len = a.kv.lens[b];
     s.n = min(all, a.kv.max_new);
-    s.col0 = tile * kColumns;
-    s.cols = max(0, min(kColumns, s.n * a.group - s.col0));
+    s.col0 = tile * columns;
+    s.cols = max(0, min(columns, s.n * a.group - s.col0));
     s.at_lo = len - all + s.col0 / a.group;
     s.at_hi = len - all + (s.col0 + max(s.cols, 1) - 1) / a.group;
     const int end = min(s.at_hi + 1, min(a.kv.max_len, a.kv.table_stride * kKvBlock));       // keys from here on are not seen
@@ -58,13 +58,13 @@ __device__ __forceinline__ int share_of(int total, int splits) {
     return (each + kWaves - 1) / kWaves * kWaves;
 }
 
-// 16 channels of a row from `column` on, 0 from `end` on; eight at a load where rows lie on 16 bytes
-template <int TYPE>
-__device__ __forceinline__ void load_channels(const Values &v, bool pieces, long row, int column, int end, float (&x)[16]) {
+// 8 x N channels of a row from `column` on, 0 from `end` on; eight at a load where rows lie on 16 bytes
+template <int TYPE, int N>
+__device__ __forceinline__ void load_channels(const Values &v, bool pieces, long row, int column, int end, float (&x)[8 * N]) {
     typedef typename Element<TYPE>::type E;
     if (pieces) {
 #pragma unroll
-        for (int p = 0; p < 2; ++p) {
+        for (int p = 0; p < N; ++p) {
             union {
                 int4 word[sizeof(E) / 2];
                 E e[8];
@@ -81,7 +81,7 @@ __device__ __forceinline__ void load_channels(const Values &v, bool pieces, long
         }
     } else {
 #pragma unroll
-        for (int k = 0; k < 16; ++k) x[k] = column + k < end ? load_value<TYPE>(v, row, column + k) : 0.0f;
+        for (int k = 0; k < 8 * N; ++k) x[k] = column + k < end ? load_value<TYPE>(v, row, column + k) : 0.0f;
     }
 }
 __device__ __forceinline__ void store_any(const Values &v, long row, int column, float x) {
@@ -188,7 +188,7 @@ __global__ __launch_bounds__(64 * kWaves, NC * ND <= 6 ? 2 : 1) void kv_attentio
 #pragma unroll
             for (int k = 0; k < NC; ++k) {
                 const int d = k * 64 + part * 16;
-                load_channels<decltype(type)::value>(a.q, a.pieces, row, hq * kv.dim + d, hq * kv.dim + kv.dim, x[k]);
+                load_channels<decltype(type)::value, 2>(a.q, a.pieces, row, hq * kv.dim + d, hq * kv.dim + kv.dim, x[k]);
             }
         };
         by_type(a.q.type, load);
@@ -374,15 +374,272 @@ __global__ __launch_bounds__(64 * kJoinWaves) void kv_attention_join_kernel(Atte
     }
 }
 
+// ---- many queries of a sequence ---------------------------------------------------------------------------------------
+// Here the products and the weights count, not the cache's bytes.  The codes are whole numbers that half precision holds
+// exactly, so a workgroup turns a block into half-precision fragments in LDS once, for kGroup wavefronts of kTiles
+// column tiles each; both products run on the matrix cores in half precision with 32-bit sums, queries scaled to their
+// row's largest (11 bits of each channel), weights in 11 bits.  A weight carries its block's scale of values, so that the
+// sums need no work between blocks: w = 2^(t + log2(scale) - base), base within 2^8 of the largest so far.
+constexpr int kGroup = 4;
+typedef _Float16 v8h __attribute__((ext_vector_type(8)));
+typedef _Float16 v2h __attribute__((ext_vector_type(2)));
+
+// 16 codes -> 16 half-precision numbers: 1024 + 128 + code is a bit pattern, 1152 is taken off
+__device__ __forceinline__ void halves_of(const v4i &codes, v8h (&to)[2]) {
+    union {
+        u32 word[8];
+        v2h pair[8];
+        v8h out[2];
+    } u;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        const u32 w = (u32)codes[k] ^ 0x80808080u;
+        u.word[2 * k] = __builtin_amdgcn_perm(0x64646464u, w, 0x04010400);
+        u.word[2 * k + 1] = __builtin_amdgcn_perm(0x64646464u, w, 0x04030402);
+    }
+#pragma unroll
+    for (int k = 0; k < 8; ++k) u.pair[k] -= v2h{1152, 1152};
+    to[0] = u.out[0], to[1] = u.out[1];
+}
+
+template <int NC, int TILES>
+__global__ __launch_bounds__(64 * kGroup, NC * TILES <= 4 ? 2 : 1) void kv_attention_many_kernel(Attention a) {
+    constexpr int NV = 4 * NC, NK = 2 * NC;          // tiles of 16 channels, products of 32 channels
+    constexpr int kBuffer = NC * 8192 * 2;           // keys, then values
+    constexpr int kLoads = 4 * NC / kGroup;          // pieces of 16 codes a thread loads, of keys and of values
+    extern __shared__ __attribute__((aligned(16))) char lds[];
+    const KvArgs &kv = a.kv;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 15, part = lane >> 4, tid = threadIdx.x;
+    int unit = blockIdx.x;
+    // the last queries see most keys: they go first
+    const int group = a.tiles - 1 - unit % a.tiles;
+    unit /= a.tiles;
+    const int h = unit % kv.heads, b = unit / kv.heads;
+    constexpr int kColumnsOf = kGroup * TILES * kColumns;
+    const Seen s = seen_by(a, b, group, kColumnsOf);
+    if (!s.cols) return;
+    // the wavefront's queries
+    const int c0 = s.col0 + wave * TILES * kColumns, c1 = min(c0 + TILES * kColumns, s.col0 + s.cols) - 1;
+    const int base_at = s.at_lo - s.col0 / a.group, at_lo = base_at + min(c0, c1) / a.group, at_hi = base_at + c1 / a.group;
+    const bool idle = c0 > c1;
+    int at[TILES];
+    v8h qf[TILES][NK];
+    float unit_q[TILES];
+    bool bad[TILES];
+#pragma unroll
+    for (int m = 0; m < TILES; ++m) {
+        const int c = min(c0 + m * kColumns + col, s.col0 + s.cols - 1), qi = c / a.group, hq = h * a.group + c % a.group;
+        const long row = s.start + qi;
+        at[m] = base_at + qi;
+        float most = 0;
+        bool fine = true;
+        float x[NK][8];
+#pragma unroll
+        for (int k = 0; k < NK; ++k) {
+            auto load = [&](auto type) __attribute__((always_inline)) {
+                load_channels<decltype(type)::value, 1>(a.q, a.pieces, row, hq * kv.dim + k * 32 + part * 8, hq * kv.dim + kv.dim, x[k]);
+            };
+            by_type(a.q.type, load);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) most = fmaxf(most, fabsf(x[k][j])), fine &= fabsf(x[k][j]) < INFINITY;
+        }
+        most = fmaxf(most, __shfl_xor(most, 16));
+        most = fmaxf(most, __shfl_xor(most, 32));
+        int all = fine;
+        all &= __shfl_xor(all, 16);
+        all &= __shfl_xor(all, 32);
+        bad[m] = !all;
+        const bool some = most > 0 && all;
+        const int e = some ? min(max(ilogbf(most), -126), 126) : 0;
+        const float down = some ? ldexpf(a.scale < 0 ? -1.0f : 1.0f, -e) : 0.0f;
+        unit_q[m] = ldexpf(fabsf(a.scale) * kLog2E, e);
+#pragma unroll
+        for (int k = 0; k < NK; ++k)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) qf[m][k][j] = some ? (_Float16)(x[k][j] * down) : (_Float16)0;
+    }
+    v4f o[TILES][NV];
+    float base[TILES], sum[TILES];
+#pragma unroll
+    for (int m = 0; m < TILES; ++m) {
+        base[m] = -INFINITY, sum[m] = 0;
+#pragma unroll
+        for (int j = 0; j < NV; ++j) o[m][j] = v4f{0, 0, 0, 0};
+    }
+    // channels that fill up a product of 32 are zero in both buffers from here on
+    if (kv.dim16 & 1)
+        for (int i = tid; i < 2 * 4 * 32; i += 64 * kGroup)
+            *(v4i *)(lds + (i >> 7) * kBuffer + (i >> 5 & 3) * NC * 2048 + (kv.dim16 >> 1) * 1024 + 512 + (i & 31) * 16) = v4i{0, 0, 0, 0};
+    // a block's pieces on their way from the cache to LDS
+    const size_t head_bytes = kv_head_bytes(kv.dim16);
+    const int pieces = kv.dim16 * 64;
+    v4i staged[2][kLoads];
+    int key_at[kLoads];          // piece (16 tokens, 16 channels, token)
+#pragma unroll
+    for (int k = 0; k < kLoads; ++k) {
+        const int i = tid + k * 64 * kGroup, t16 = (i >> 4) / kv.dim16, d16 = (i >> 4) - t16 * kv.dim16;
+        key_at[k] = (t16 * NK + (d16 >> 1)) * 1024 + (d16 & 1) * 512 + (i & 15) * 16;
+    }
+    float scale_k = 0, scale_v = 0;
+    int page = -1;
+    auto fetch = [&](int u) __attribute__((always_inline)) {
+        page = page_of(kv, b, s.block(u));
+        const size_t head = (size_t)max(page, 0) * kv.heads + h;
+        const signed char *codes = kv.codes + head * head_bytes;
+        scale_k = kv.scales[2 * head], scale_v = kv.scales[2 * head + 1];
+#pragma unroll
+        for (int k = 0; k < kLoads; ++k) {
+            const int i = min(tid + k * 64 * kGroup, pieces - 1);
+            staged[0][k] = ((const v4i *)codes)[i];
+            staged[1][k] = ((const v4i *)codes)[pieces + i];
+        }
+    };
+    if (s.total) fetch(0);
+    for (int u = 0; u < s.total; ++u) {
+        char *keys = lds + (u & 1) * kBuffer, *values = keys + NC * 8192;
+#pragma unroll
+        for (int k = 0; k < kLoads; ++k) {
+            if (tid + k * 64 * kGroup < pieces) {
+                v8h x[2];
+                // keys: of a product of 32 channels a lane has eight of a token
+                halves_of(staged[0][k], x);
+                *(v8h *)(keys + key_at[k]) = x[0], *(v8h *)(keys + key_at[k] + 256) = x[1];
+                // values: the first and the last 32 tokens of a channel
+                halves_of(staged[1][k], x);
+                char *to = values + (tid + k * 64 * kGroup) * 16;
+                *(v8h *)to = x[0], *(v8h *)(to + NV * 1024) = x[1];
+            }
+        }
+        const int block = s.block(u), t0 = block * kKvBlock, end = page < 0 ? 0 : kv.max_len;
+        const float now_k = scale_k, now_v = page < 0 ? 1.0f : fmaxf(scale_v, 0x1p-100f);
+        if (u + 1 < s.total) fetch(u + 1);
+        __syncthreads();
+        if (idle || t0 > at_hi || t0 >= end || (a.window && t0 + 63 <= at_lo - a.window && t0 >= a.sinks)) continue;
+        const bool edge = t0 + 63 > at_lo || t0 + 64 > end || (a.window && t0 <= at_hi - a.window);
+        const float log_v = __builtin_amdgcn_logf(now_v), unit_l = 1.0f / now_v;
+        v4f acc[TILES][4];
+#pragma unroll
+        for (int m = 0; m < TILES; ++m)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) acc[m][i] = v4f{0, 0, 0, 0};
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int k = 0; k < NK; ++k)
+                if (k * 2 < kv.dim16) {
+                const v8h x = *(const v8h *)(keys + (i * NK + k) * 1024 + lane * 16);
+#pragma unroll
+                for (int m = 0; m < TILES; ++m) acc[m][i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(x, qf[m][k], acc[m][i], 0, 0, 0);
+            }
+        v8h w[TILES][2];
+#pragma unroll
+        for (int m = 0; m < TILES; ++m) {
+            const float unit_s = fmaxf(unit_q[m] * now_k, 0x1p-126f);      // not 0: what is not seen stays at -infinity
+            if (edge) {
+                const int own = t0 + part * 4, hi = min(at[m], end - 1) - own;
+                const int lo = a.window ? at[m] - a.window + 1 - own : -kKvBlock, sinks = a.window ? a.sinks - own : 0;
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) {
+                        const int e = i * 16 + r;
+                        acc[m][i][r] = (e <= hi) & ((e >= lo) | (e < sinks)) ? acc[m][i][r] : -INFINITY;
+                    }
+            }
+            float most = -INFINITY;
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) most = fmaxf(most, acc[m][i][r]);
+            most = fmaf(most, unit_s, log_v);
+            if (__any(most > base[m] + 8)) {
+                most = fmaxf(most, __shfl_xor(most, 16));
+                most = fmaxf(most, __shfl_xor(most, 32));
+                if (most > base[m]) {
+                    const float was = __builtin_amdgcn_exp2f(base[m] - most);
+                    base[m] = most;
+                    sum[m] *= was;
+#pragma unroll
+                    for (int j = 0; j < NV; ++j) o[m][j] *= was;
+                }
+            }
+            const float off = base[m] == -INFINITY ? -INFINITY : log_v - base[m];
+            float part_sum = 0;
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    const float x = __builtin_amdgcn_exp2f(fmaf(acc[m][i][r], unit_s, off));
+                    part_sum += x;
+                    w[m][i >> 1][(i & 1) * 4 + r] = (_Float16)x;
+                }
+            sum[m] = fmaf(part_sum, unit_l, sum[m]);
+        }
+#pragma unroll
+        for (int j = 0; j < NV; ++j)
+            if (j < kv.dim16)
+#pragma unroll
+            for (int n = 0; n < 2; ++n) {
+                const v8h x = *(const v8h *)(values + (n * NV + j) * 1024 + lane * 16);
+#pragma unroll
+                for (int m = 0; m < TILES; ++m) o[m][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(x, w[m][n], o[m][j], 0, 0, 0);
+            }
+    }
+#pragma unroll
+    for (int m = 0; m < TILES; ++m) {
+        float all = sum[m];
+        all += __shfl_xor(all, 16);
+        all += __shfl_xor(all, 32);
+        const float f = bad[m] ? __builtin_nanf("") : all > 0 ? 1.0f / all : 0.0f;
+        const int c = c0 + m * kColumns + col;
+        if (c > c1) continue;
+        const long row = s.start + c / a.group;
+        const int column = (h * a.group + c % a.group) * kv.dim + part * 4;
+#pragma unroll
+        for (int j = 0; j < NV; ++j) {
+            const int d = j * 16 + part * 4;
+            if (d + 4 <= kv.dim && a.out_quads) {
+                auto store = [&](auto type) __attribute__((always_inline)) {
+                    typedef typename Element<decltype(type)::value>::type E;
+                    struct alignas(4 * sizeof(E) < 16 ? 4 * sizeof(E) : 16) Quad {
+                        E e[4];
+                    } quad;
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) quad.e[r] = from_float<decltype(type)::value>(o[m][j][r] * f, a.out.unit, a.out.p);
+                    *(Quad *)((E *)a.out.data + row * a.out.stride + column + j * 16) = quad;
+                };
+                by_type(a.out.type, store);
+            } else {
+#pragma unroll
+                for (int r = 0; r < 4; ++r)
+                    if (d + r < kv.dim) store_any(a.out, row, column + j * 16 + r, o[m][j][r] * f);
+            }
+        }
+    }
+}
+
+#ifndef MANY
+#define MANY 64
+#endif
+// Column tiles of a wavefront, for head sizes of NC x 64 channels.
+constexpr int many_tiles(int nc) { return nc <= 2 ? 2 : 1; }
+
 // How a call is cut up.
 struct Cut {
+    bool many;
     int tiles, splits, columns;
     long places() const { return (long)tiles * splits * columns; }
 };
-Cut cut_of(const KvArgs &kv, int heads_q, int window, int sinks) {
+Cut cut_of(const KvArgs &kv, int heads_q, int window, int sinks, bool fine) {
     Cut c;
     const int group = heads_q / kv.heads;
     const long columns = (long)kv.max_new * group;
+    const int of_group = kGroup * kColumns * many_tiles((kv.dim + 63) / 64);
+    c.many = !fine && columns >= of_group && (columns + of_group - 1) / of_group * kv.count * kv.heads >= MANY;
+    if (c.many) {
+        c.tiles = (int)((columns + of_group - 1) / of_group), c.splits = 1, c.columns = 0;
+        return c;
+    }
     c.tiles = (int)((columns + kColumns - 1) / kColumns);
     c.columns = (int)std::min<long>(columns, kColumns);
     const long reach = std::min<long>(kv.max_len, (long)kv.table_stride * kKvBlock);
@@ -397,26 +654,32 @@ Cut cut_of(const KvArgs &kv, int heads_q, int window, int sinks) {
 namespace gala {
 
 size_t kv_attention_workspace(const KvArgs &kv, int heads_q, int window, int sinks) {
-    const Cut c = cut_of(kv, heads_q, window, sinks);
+    const Cut c = cut_of(kv, heads_q, window, sinks, true);          // the other way needs none
     return c.splits == 1 ? 0 : (size_t)kv.count * kv.heads * c.places() * (kv.dim + 2) * sizeof(float);
 }
 
 int launch_kv_attention(void *stream, const KvArgs &kv, int heads_q, float scale, int window, int sinks, const Values &q,
                         const Values &out, void *workspace) {
-    const Cut c = cut_of(kv, heads_q, window, sinks);
+    const bool fine = q.type == GALA_F32 || q.type == GALA_RESIDUE || out.type == GALA_F32 || out.type == GALA_RESIDUE;
+    const Cut c = cut_of(kv, heads_q, window, sinks, fine);
     Attention a{};
     a.kv = kv, a.q = q, a.out = out;
     const size_t size = q.type == GALA_F32 ? 4 : q.type == GALA_RESIDUE ? 8 : 2;
     a.pieces = (uintptr_t)q.data % 16 == 0 && q.stride * size % 16 == 0 && kv.dim % 8 == 0;
+    const size_t of_out = out.type == GALA_F32 ? 4 : out.type == GALA_RESIDUE ? 8 : 2, quad = std::min<size_t>(4 * of_out, 16);
+    a.out_quads = (uintptr_t)out.data % quad == 0 && out.stride * of_out % quad == 0 && kv.dim % 4 == 0;
     a.heads_q = heads_q, a.group = heads_q / kv.heads;
     a.scale = scale, a.window = window, a.sinks = sinks;
     a.tiles = c.tiles, a.splits = c.splits, a.columns = c.columns;
     a.sums = (float *)workspace;
     a.stats = a.sums + (size_t)kv.count * kv.heads * c.places() * kv.dim;
-    const bool fine = q.type == GALA_F32 || q.type == GALA_RESIDUE || out.type == GALA_F32 || out.type == GALA_RESIDUE;
     const unsigned groups = (unsigned)((long)kv.count * kv.heads * c.tiles * c.splits);
     auto launch = [&](auto nc) {
         constexpr int NC = decltype(nc)::value;
+        if (c.many) {
+            hipLaunchKernelGGL((kv_attention_many_kernel<NC, many_tiles(NC)>), dim3(groups), dim3(64 * kGroup), NC * 32768, (hipStream_t)stream, a);
+            return;
+        }
         if (fine)
             hipLaunchKernelGGL((kv_attention_kernel<NC, 3>), dim3(groups), dim3(64 * kWaves), 0, (hipStream_t)stream, a);
         else

@@ -99,3 +99,20 @@ def kept_tokens(z, temperature, top_k, top_p, min_p):
         kept &= w >= min(min_p, 1.0)
     kept[order[0]] = True
     return kept, w, margin
+
+
+def attention_in_halves(q, k, v, scales, seen, scale):
+    """The same with half-precision operands: each channel of the query and each weight times its block's scale of values
+    (`scales`, a token each) rounded to 11 bits, such a weight to 2^-25 of the largest of them at least; sums in 32 bits."""
+    dim = len(q)
+    if not seen.any():
+        return np.zeros(dim), np.zeros(dim)
+    k, v, scales = k[seen], v[seen], scales[seen]
+    s = scale * (k @ q)
+    w = np.exp(s - s.max())
+    out = (w[:, None] * v).sum(0) / w.sum()
+    size = abs(scale) * (np.abs(k) @ np.abs(q))
+    slack = (2.0 ** -11 + 2.0 ** -20) * size + 2.0 ** -20 * (np.abs(s) + np.abs(s).max() + 1)
+    rel = np.expm1(2 * slack.max()) + 2.0 ** -11
+    spread = (w[:, None] * np.abs(v)).sum(0) / w.sum()
+    return out, 2 * rel * spread + len(w) * 127 * 2.0 ** -25 * (w * scales).max() / w.sum() + 2.0 ** -18 * spread

@@ -88,7 +88,10 @@ class Case:
                     if not np.isfinite(q[row, h]).all():
                         assert np.isnan(got[row, h]).all()
                         continue
-                    want, bound = ref.attention(q[row, h], k[h // self.group, :tokens], v[h // self.group, :tokens], seen, self.scale,
+                    at_scale = np.repeat(scales[at][:, h // self.group, 1], 64)[:tokens]
+                    halves = not fine and min(max(self.new), max_new) * self.group >= 64
+                    want, bound = ref.attention_in_halves(q[row, h], k[h // self.group, :tokens], v[h // self.group, :tokens], at_scale, seen,
+                                                          self.scale) if halves else ref.attention(q[row, h], k[h // self.group, :tokens], v[h // self.group, :tokens], seen, self.scale,
                                                 *((24, 23) if fine else (16, 15)))
                     eps = ref.UNIT_ROUNDOFF.get({"f16": "float16", "bf16": "bfloat16", "f32": "float32"}.get(self.out_kind), 0)
                     bound = bound + eps * (np.abs(want) + bound) + (UNIT / 2 if self.out_kind == "residue" else 0) + 2.0 ** -24
@@ -279,3 +282,48 @@ def test_after_append(ctx):
     codes = c.cache.codes.cpu().numpy().reshape(c.cache.codes.shape[0], heads, -1)
     c.k, c.v = (codes[:, :, p] for p in ref.code_places(dim))
     c.check(c.run(), {(0, i) for i in (0, 1, 64, 100, 149)})
+
+
+@pytest.mark.parametrize("dim", [1, 16, 40, 64, 72, 80, 96, 112, 128, 160, 192, 200, 256])
+@pytest.mark.parametrize("kind,group", [("bf16", 3), ("f16", 8)])
+def test_prompts_of_every_head_size(ctx, dim, kind, group):
+    c = Case(ctx, [180, 1, 77], [180, 300, 200], 32, group, dim, kind, seed=dim, spread=1.0)
+    out = c.run()
+    c.check(out, {(0, 0), (0, 63), (0, 179), (1, 0), (2, 5), (2, 76)} if dim < 100 else {(0, 179), (2, 5)})
+
+
+@pytest.mark.parametrize("window,sinks", [(1, 0), (16, 4), (100, 0), (65, 70), (1000, 4)])
+def test_windows_of_prompts(ctx, window, sinks):
+    c = Case(ctx, [200, 50, 130], [500, 50, 131], 32, 4, 64, "bf16", seed=window)
+    c.check(c.run(window=window, sinks=sinks), {(0, i) for i in (0, 17, 199)} | {(1, 0), (1, 49), (2, 0), (2, 129)})
+
+
+def test_prompts_with_scales_far_apart(ctx):
+    c = Case(ctx, [150, 3], [400, 90], 32, 4, 64, "f16", seed=41)
+    n = c.cache.scales.numel()
+    c.cache.scales.mul_(torch.logspace(-2, 2, n, device="cuda")[torch.randperm(n, device="cuda")].view_as(c.cache.scales))
+    rows = {(0, 0), (0, 70), (0, 149), (1, 2)}
+    c.check(c.run(scale=0.02), rows)
+    c.check(c.run(scale=-0.02), rows)
+    c.check(c.run(scale=0.0), rows)
+    c.cache.scales[::2, :, 0] = 0
+    c.cache.scales[::3, :, 1] = 0
+    c.check(c.run(scale=0.02), rows)
+
+
+def test_prompts_that_see_little(ctx):
+    """Rows before the first token, pages given back, bounds of the host, rows apart, a NaN in one head's query."""
+    c = Case(ctx, [140, 200, 10], [100, 260, 300], 32, 4, 64, "bf16", seed=42, layout_gap=1, most=(180, 250))
+    c.table[1, 1], c.table[2, :] = -1, c.cache.codes.shape[0]
+    c.q[150, 7, 3], c.q[151, 8, 0] = float("nan"), float("inf")
+    out = c.run()
+    c.check(out, {(0, 0), (0, 39), (0, 40), (0, 139), (1, 0), (1, 10), (1, 11), (1, 179), (1, 199), (2, 4)})
+    assert bool((out[:40] == 0).all()) and bool((out[340:] == 0).all())
+    again = c.run()
+    assert torch.equal(out.nan_to_num(9), again.nan_to_num(9))
+
+
+def test_prompts_into_other_types(ctx):
+    for kind, out in (("bf16", "f16"), ("f16", "bf16")):
+        c = Case(ctx, [130], [300], 64, 2, 96, kind, out, seed=43)
+        c.check(c.run(), {(0, 0), (0, 77), (0, 129)})
