@@ -132,9 +132,9 @@ __device__ __forceinline__ float joined(const v4i (&acc)[ND], int r) {
 // 16 of one column's, and they are the very weights that it hands to the second product, because the values' codes
 // lie in that order of tokens.  So a block goes from memory to the sums without LDS or an exchange between lanes, but
 // for the largest score.  A wavefront has blocks of its own; a workgroup's wavefronts are joined at the end.
-template <int NC, int ND>
-__global__ __launch_bounds__(64 * kWaves, NC * ND <= 6 ? 2 : 1) void kv_attention_kernel(Attention a) {
-    constexpr int NV = 4 * NC;
+template <int N32, int ND>
+__global__ __launch_bounds__(64 * kWaves, N32 * ND <= 12 ? 2 : 1) void kv_attention_kernel(Attention a) {
+    constexpr int NC = (N32 + 1) / 2, NV = 2 * N32;          // products of 64 channels, tiles of 16
     __shared__ float sums[kWaves][kColumns][NV * 16 + 1];
     __shared__ float stats[kWaves][kColumns][2];
     const KvArgs &kv = a.kv;
@@ -234,7 +234,7 @@ __global__ __launch_bounds__(64 * kWaves, NC * ND <= 6 ? 2 : 1) void kv_attentio
         v4i values[NV];
 #pragma unroll
         for (int j = 0; j < NV; ++j)
-            if (j < kv.dim16) values[j] = *(const v4i *)(codes + (size_t)kKvBlock * 16 * kv.dim16 + j * 1024 + lane * 16);
+            values[j] = *(const v4i *)(codes + (size_t)kKvBlock * 16 * kv.dim16 + min(j, kv.dim16 - 1) * 1024 + lane * 16);
         float t[16];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
@@ -288,14 +288,13 @@ __global__ __launch_bounds__(64 * kWaves, NC * ND <= 6 ? 2 : 1) void kv_attentio
             planes<ND>(word, i, w);
         }
 #pragma unroll
-        for (int j = 0; j < NV; ++j)
-            if (j < kv.dim16) {
-                v4i acc[ND];
+        for (int j = 0; j < NV; ++j) {
+            v4i acc[ND];
 #pragma unroll
-                for (int n = 0; n < ND; ++n) acc[n] = __builtin_amdgcn_mfma_i32_16x16x64_i8(values[j], w[n], v4i{0, 0, 0, 0}, 0, 0, 0);
+            for (int n = 0; n < ND; ++n) acc[n] = __builtin_amdgcn_mfma_i32_16x16x64_i8(values[j], w[n], v4i{0, 0, 0, 0}, 0, 0, 0);
 #pragma unroll
-                for (int r = 0; r < 4; ++r) o[j][r] = fmaf(joined<ND>(acc, r), unit_v, o[j][r]);
-            }
+            for (int r = 0; r < 4; ++r) o[j][r] = fmaf(joined<ND>(acc, r), unit_v, o[j][r]);
+        }
     }
     // the wavefronts' sums in one
     sum += __shfl_xor(sum, 16);
@@ -376,11 +375,11 @@ __global__ __launch_bounds__(64 * kJoinWaves) void kv_attention_join_kernel(Atte
 
 // ---- many queries of a sequence ---------------------------------------------------------------------------------------
 // Here the products and the weights count, not the cache's bytes.  The codes are whole numbers that half precision holds
-// exactly, so a workgroup turns a block into half-precision fragments in LDS once, for kGroup wavefronts of kTiles
-// column tiles each; both products run on the matrix cores in half precision with 32-bit sums, queries scaled to their
+// exactly, so a workgroup turns a block into half-precision fragments in LDS once, for kGroup wavefronts of a
+// column tile each; both products run on the matrix cores in half precision with 32-bit sums, queries scaled to their
 // row's largest (11 bits of each channel), weights in 11 bits.  A weight carries its block's scale of values, so that the
 // sums need no work between blocks: w = 2^(t + log2(scale) - base), base within 2^8 of the largest so far.
-constexpr int kGroup = 4;
+constexpr int kGroup = 8;
 typedef _Float16 v8h __attribute__((ext_vector_type(8)));
 typedef _Float16 v2h __attribute__((ext_vector_type(2)));
 
@@ -402,11 +401,11 @@ __device__ __forceinline__ void halves_of(const v4i &codes, v8h (&to)[2]) {
     to[0] = u.out[0], to[1] = u.out[1];
 }
 
-template <int NC, int TILES>
-__global__ __launch_bounds__(64 * kGroup, NC * TILES <= 4 ? 2 : 1) void kv_attention_many_kernel(Attention a) {
-    constexpr int NV = 4 * NC, NK = 2 * NC;          // tiles of 16 channels, products of 32 channels
-    constexpr int kBuffer = NC * 8192 * 2;           // keys, then values
-    constexpr int kLoads = 4 * NC / kGroup;          // pieces of 16 codes a thread loads, of keys and of values
+template <int NK>
+__global__ __launch_bounds__(64 * kGroup, NK <= 4 ? 4 : 2) void kv_attention_many_kernel(Attention a) {
+    constexpr int NV = 2 * NK;                       // tiles of 16 channels, beside NK products of 32
+    constexpr int kHalf = NK * 4096, kBuffer = 2 * kHalf;           // keys, then values
+    constexpr int kLoads = (2 * NK + kGroup - 1) / kGroup;          // pieces of 16 codes a thread loads, of keys and of values
     extern __shared__ __attribute__((aligned(16))) char lds[];
     const KvArgs &kv = a.kv;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 15, part = lane >> 4, tid = threadIdx.x;
@@ -415,22 +414,21 @@ __global__ __launch_bounds__(64 * kGroup, NC * TILES <= 4 ? 2 : 1) void kv_atten
     const int group = a.tiles - 1 - unit % a.tiles;
     unit /= a.tiles;
     const int h = unit % kv.heads, b = unit / kv.heads;
-    constexpr int kColumnsOf = kGroup * TILES * kColumns;
+    constexpr int kColumnsOf = kGroup * kColumns;
     const Seen s = seen_by(a, b, group, kColumnsOf);
     if (!s.cols) return;
     // the wavefront's queries
-    const int c0 = s.col0 + wave * TILES * kColumns, c1 = min(c0 + TILES * kColumns, s.col0 + s.cols) - 1;
+    const int c0 = s.col0 + wave * kColumns, c1 = min(c0 + kColumns, s.col0 + s.cols) - 1;
     const int base_at = s.at_lo - s.col0 / a.group, at_lo = base_at + min(c0, c1) / a.group, at_hi = base_at + c1 / a.group;
     const bool idle = c0 > c1;
-    int at[TILES];
-    v8h qf[TILES][NK];
-    float unit_q[TILES];
-    bool bad[TILES];
-#pragma unroll
-    for (int m = 0; m < TILES; ++m) {
-        const int c = min(c0 + m * kColumns + col, s.col0 + s.cols - 1), qi = c / a.group, hq = h * a.group + c % a.group;
+    int at;
+    v8h qf[NK];
+    float unit_q;
+    bool bad;
+    {
+        const int c = min(c0 + col, s.col0 + s.cols - 1), qi = c / a.group, hq = h * a.group + c % a.group;
         const long row = s.start + qi;
-        at[m] = base_at + qi;
+        at = base_at + qi;
         float most = 0;
         bool fine = true;
         float x[NK][8];
@@ -448,28 +446,27 @@ __global__ __launch_bounds__(64 * kGroup, NC * TILES <= 4 ? 2 : 1) void kv_atten
         int all = fine;
         all &= __shfl_xor(all, 16);
         all &= __shfl_xor(all, 32);
-        bad[m] = !all;
+        bad = !all;
         const bool some = most > 0 && all;
         const int e = some ? min(max(ilogbf(most), -126), 126) : 0;
         const float down = some ? ldexpf(a.scale < 0 ? -1.0f : 1.0f, -e) : 0.0f;
-        unit_q[m] = ldexpf(fabsf(a.scale) * kLog2E, e);
+        unit_q = ldexpf(fabsf(a.scale) * kLog2E, e);
 #pragma unroll
         for (int k = 0; k < NK; ++k)
 #pragma unroll
-            for (int j = 0; j < 8; ++j) qf[m][k][j] = some ? (_Float16)(x[k][j] * down) : (_Float16)0;
+            for (int j = 0; j < 8; ++j) qf[k][j] = some ? (_Float16)(x[k][j] * down) : (_Float16)0;
     }
-    v4f o[TILES][NV];
-    float base[TILES], sum[TILES];
+    v4f o[NV];
+    float base = 0, limit = -INFINITY, sum = 0;      // limit: what an exponent may be before the base is raised
 #pragma unroll
-    for (int m = 0; m < TILES; ++m) {
-        base[m] = -INFINITY, sum[m] = 0;
-#pragma unroll
-        for (int j = 0; j < NV; ++j) o[m][j] = v4f{0, 0, 0, 0};
-    }
+    for (int j = 0; j < NV; ++j) o[j] = v4f{0, 0, 0, 0};
     // channels that fill up a product of 32 are zero in both buffers from here on
     if (kv.dim16 & 1)
-        for (int i = tid; i < 2 * 4 * 32; i += 64 * kGroup)
-            *(v4i *)(lds + (i >> 7) * kBuffer + (i >> 5 & 3) * NC * 2048 + (kv.dim16 >> 1) * 1024 + 512 + (i & 31) * 16) = v4i{0, 0, 0, 0};
+        for (int i = tid; i < 2 * 128; i += 64 * kGroup) {
+            char *to = lds + (i >> 7) * kBuffer;
+            *(v4i *)(to + ((i >> 5 & 3) * NK + NK - 1) * 1024 + 512 + (i & 31) * 16) = v4i{0, 0, 0, 0};
+            *(v4i *)(to + kHalf + ((i >> 6 & 1) * NV + NV - 1) * 1024 + (i & 63) * 16) = v4i{0, 0, 0, 0};
+        }
     // a block's pieces on their way from the cache to LDS
     const size_t head_bytes = kv_head_bytes(kv.dim16);
     const int pieces = kv.dim16 * 64;
@@ -481,22 +478,27 @@ __global__ __launch_bounds__(64 * kGroup, NC * TILES <= 4 ? 2 : 1) void kv_atten
         key_at[k] = (t16 * NK + (d16 >> 1)) * 1024 + (d16 & 1) * 512 + (i & 15) * 16;
     }
     float scale_k = 0, scale_v = 0;
-    int page = -1;
+    int page = -1, page_next = 0;
+    // the page of block u has to be there when its codes are asked for: it is asked for a block earlier
+    auto page_at = [&](int u) __attribute__((always_inline)) { return u < s.total ? page_of(kv, b, s.block(u)) : -1; };
     auto fetch = [&](int u) __attribute__((always_inline)) {
-        page = page_of(kv, b, s.block(u));
+        page = __builtin_amdgcn_readfirstlane(page_next);
         const size_t head = (size_t)max(page, 0) * kv.heads + h;
         const signed char *codes = kv.codes + head * head_bytes;
-        scale_k = kv.scales[2 * head], scale_v = kv.scales[2 * head + 1];
+        const float2 scales = *(const float2 *)(kv.scales + 2 * head);
+        scale_k = scales.x, scale_v = scales.y;
 #pragma unroll
         for (int k = 0; k < kLoads; ++k) {
             const int i = min(tid + k * 64 * kGroup, pieces - 1);
             staged[0][k] = ((const v4i *)codes)[i];
             staged[1][k] = ((const v4i *)codes)[pieces + i];
         }
+        page_next = page_at(u + 1);
     };
+    page_next = page_at(0);
     if (s.total) fetch(0);
     for (int u = 0; u < s.total; ++u) {
-        char *keys = lds + (u & 1) * kBuffer, *values = keys + NC * 8192;
+        char *keys = lds + (u & 1) * kBuffer, *values = keys + kHalf;
 #pragma unroll
         for (int k = 0; k < kLoads; ++k) {
             if (tid + k * 64 * kGroup < pieces) {
@@ -517,112 +519,103 @@ __global__ __launch_bounds__(64 * kGroup, NC * TILES <= 4 ? 2 : 1) void kv_atten
         if (idle || t0 > at_hi || t0 >= end || (a.window && t0 + 63 <= at_lo - a.window && t0 >= a.sinks)) continue;
         const bool edge = t0 + 63 > at_lo || t0 + 64 > end || (a.window && t0 <= at_hi - a.window);
         const float log_v = __builtin_amdgcn_logf(now_v), unit_l = 1.0f / now_v;
-        v4f acc[TILES][4];
+        v4f acc[4];
 #pragma unroll
-        for (int m = 0; m < TILES; ++m)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) acc[m][i] = v4f{0, 0, 0, 0};
+        for (int i = 0; i < 4; ++i) acc[i] = v4f{0, 0, 0, 0};
 #pragma unroll
         for (int i = 0; i < 4; ++i)
 #pragma unroll
-            for (int k = 0; k < NK; ++k)
-                if (k * 2 < kv.dim16) {
+            for (int k = 0; k < NK; ++k) {
                 const v8h x = *(const v8h *)(keys + (i * NK + k) * 1024 + lane * 16);
-#pragma unroll
-                for (int m = 0; m < TILES; ++m) acc[m][i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(x, qf[m][k], acc[m][i], 0, 0, 0);
+                acc[i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(x, qf[k], acc[i], 0, 0, 0);
             }
-        v8h w[TILES][2];
-#pragma unroll
-        for (int m = 0; m < TILES; ++m) {
-            const float unit_s = fmaxf(unit_q[m] * now_k, 0x1p-126f);      // not 0: what is not seen stays at -infinity
-            if (edge) {
-                const int own = t0 + part * 4, hi = min(at[m], end - 1) - own;
-                const int lo = a.window ? at[m] - a.window + 1 - own : -kKvBlock, sinks = a.window ? a.sinks - own : 0;
-#pragma unroll
-                for (int i = 0; i < 4; ++i)
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) {
-                        const int e = i * 16 + r;
-                        acc[m][i][r] = (e <= hi) & ((e >= lo) | (e < sinks)) ? acc[m][i][r] : -INFINITY;
-                    }
-            }
-            float most = -INFINITY;
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-#pragma unroll
-                for (int r = 0; r < 4; ++r) most = fmaxf(most, acc[m][i][r]);
-            most = fmaf(most, unit_s, log_v);
-            if (__any(most > base[m] + 8)) {
-                most = fmaxf(most, __shfl_xor(most, 16));
-                most = fmaxf(most, __shfl_xor(most, 32));
-                if (most > base[m]) {
-                    const float was = __builtin_amdgcn_exp2f(base[m] - most);
-                    base[m] = most;
-                    sum[m] *= was;
-#pragma unroll
-                    for (int j = 0; j < NV; ++j) o[m][j] *= was;
-                }
-            }
-            const float off = base[m] == -INFINITY ? -INFINITY : log_v - base[m];
-            float part_sum = 0;
+        v8h w[2];
+        const float unit_s = fmaxf(unit_q * now_k, 0x1p-126f);      // not 0: what is not seen stays at -infinity
+        if (edge) {
+            const int own = t0 + part * 4, hi = min(at, end - 1) - own;
+            const int lo = a.window ? at - a.window + 1 - own : -kKvBlock, sinks = a.window ? a.sinks - own : 0;
 #pragma unroll
             for (int i = 0; i < 4; ++i)
 #pragma unroll
                 for (int r = 0; r < 4; ++r) {
-                    const float x = __builtin_amdgcn_exp2f(fmaf(acc[m][i][r], unit_s, off));
-                    part_sum += x;
-                    w[m][i >> 1][(i & 1) * 4 + r] = (_Float16)x;
+                    const int e = i * 16 + r;
+                    acc[i][r] = (e <= hi) & ((e >= lo) | (e < sinks)) ? acc[i][r] : -INFINITY;
                 }
-            sum[m] = fmaf(part_sum, unit_l, sum[m]);
         }
+        // exponents below the base so far
+        const float off = log_v - base;
+        float most = -INFINITY;
 #pragma unroll
-        for (int j = 0; j < NV; ++j)
-            if (j < kv.dim16)
+        for (int i = 0; i < 4; ++i)
 #pragma unroll
-            for (int n = 0; n < 2; ++n) {
-                const v8h x = *(const v8h *)(values + (n * NV + j) * 1024 + lane * 16);
-#pragma unroll
-                for (int m = 0; m < TILES; ++m) o[m][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(x, w[m][n], o[m][j], 0, 0, 0);
+            for (int r = 0; r < 4; ++r) {
+                acc[i][r] = fmaf(acc[i][r], unit_s, off);
+                most = fmaxf(most, acc[i][r]);
             }
+        if (__any(most > limit)) {
+            most = fmaxf(most, __shfl_xor(most, 16));
+            most = fmaxf(most, __shfl_xor(most, 32));
+            if (most > limit || most > 0) {
+                const float was = limit == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(-most);          // nothing yet with the first base
+                base += most;
+                limit = 8;
+                sum *= was;
+#pragma unroll
+                for (int j = 0; j < NV; ++j) o[j] *= was;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) acc[i] -= most;
+            }
+        }
+        // the values' fragments four ahead of the products
+        auto fragment = [&](int f) __attribute__((always_inline)) { return *(const v8h *)(values + ((f & 1) * NV + (f >> 1)) * 1024 + lane * 16); };
+        v8h ahead[4];
+#pragma unroll
+        for (int f = 0; f < 4; ++f) ahead[f] = fragment(f);
+        float part_sum = 0;
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const float x = __builtin_amdgcn_exp2f(acc[i][r]);
+                part_sum += x;
+                w[i >> 1][(i & 1) * 4 + r] = (_Float16)x;
+            }
+        sum = fmaf(part_sum, unit_l, sum);
+#pragma unroll
+        for (int f = 0; f < 2 * NV; ++f) {
+            o[f >> 1] = __builtin_amdgcn_mfma_f32_16x16x32_f16(ahead[f & 3], w[f & 1], o[f >> 1], 0, 0, 0);
+            if (f + 4 < 2 * NV) ahead[f & 3] = fragment(f + 4);
+        }
     }
+    float all = sum;
+    all += __shfl_xor(all, 16);
+    all += __shfl_xor(all, 32);
+    const float f = bad ? __builtin_nanf("") : all > 0 ? 1.0f / all : 0.0f;
+    const int c = c0 + col;
+    if (c > c1) return;
+    const long row = s.start + c / a.group;
+    const int column = (h * a.group + c % a.group) * kv.dim + part * 4;
 #pragma unroll
-    for (int m = 0; m < TILES; ++m) {
-        float all = sum[m];
-        all += __shfl_xor(all, 16);
-        all += __shfl_xor(all, 32);
-        const float f = bad[m] ? __builtin_nanf("") : all > 0 ? 1.0f / all : 0.0f;
-        const int c = c0 + m * kColumns + col;
-        if (c > c1) continue;
-        const long row = s.start + c / a.group;
-        const int column = (h * a.group + c % a.group) * kv.dim + part * 4;
+    for (int j = 0; j < NV; ++j) {
+        const int d = j * 16 + part * 4;
+        if (d + 4 <= kv.dim && a.out_quads) {
+            auto store = [&](auto type) __attribute__((always_inline)) {
+                typedef typename Element<decltype(type)::value>::type E;
+                struct alignas(4 * sizeof(E) < 16 ? 4 * sizeof(E) : 16) Quad {
+                    E e[4];
+                } quad;
 #pragma unroll
-        for (int j = 0; j < NV; ++j) {
-            const int d = j * 16 + part * 4;
-            if (d + 4 <= kv.dim && a.out_quads) {
-                auto store = [&](auto type) __attribute__((always_inline)) {
-                    typedef typename Element<decltype(type)::value>::type E;
-                    struct alignas(4 * sizeof(E) < 16 ? 4 * sizeof(E) : 16) Quad {
-                        E e[4];
-                    } quad;
+                for (int r = 0; r < 4; ++r) quad.e[r] = from_float<decltype(type)::value>(o[j][r] * f, a.out.unit, a.out.p);
+                *(Quad *)((E *)a.out.data + row * a.out.stride + column + j * 16) = quad;
+            };
+            by_type(a.out.type, store);
+        } else {
 #pragma unroll
-                    for (int r = 0; r < 4; ++r) quad.e[r] = from_float<decltype(type)::value>(o[m][j][r] * f, a.out.unit, a.out.p);
-                    *(Quad *)((E *)a.out.data + row * a.out.stride + column + j * 16) = quad;
-                };
-                by_type(a.out.type, store);
-            } else {
-#pragma unroll
-                for (int r = 0; r < 4; ++r)
-                    if (d + r < kv.dim) store_any(a.out, row, column + j * 16 + r, o[m][j][r] * f);
-            }
+            for (int r = 0; r < 4; ++r)
+                if (d + r < kv.dim) store_any(a.out, row, column + j * 16 + r, o[j][r] * f);
         }
     }
 }
-
-#ifndef MANY
-#define MANY 64
-#endif
-// Column tiles of a wavefront, for head sizes of NC x 64 channels.
-constexpr int many_tiles(int nc) { return nc <= 2 ? 2 : 1; }
 
 // How a call is cut up.
 struct Cut {
@@ -634,17 +627,24 @@ Cut cut_of(const KvArgs &kv, int heads_q, int window, int sinks, bool fine) {
     Cut c;
     const int group = heads_q / kv.heads;
     const long columns = (long)kv.max_new * group;
-    const int of_group = kGroup * kColumns * many_tiles((kv.dim + 63) / 64);
-    c.many = !fine && columns >= of_group && (columns + of_group - 1) / of_group * kv.count * kv.heads >= MANY;
+    const int of_group = kGroup * kColumns;
+    const long reach = std::min<long>(kv.max_len, (long)kv.table_stride * kKvBlock);
+    const long keys = window ? std::min(reach, (long)window + kv.max_new + sinks + 2 * kKvBlock) : reach;
+    const long blocks = std::max(1l, (keys + kKvBlock - 1) / kKvBlock);
+    // Whole prompts in half precision, where they fill the card or have few keys: 8 x 128 queries of 32 heads over 4000
+    // tokens (256 workgroups) take 110 us so and 142 us as exact sums, 4 x 300 over 300 14 and 30 us; but 4 x 128 over
+    // 4000 (128 workgroups) 108 and 69 us, because exact sums can share a tile's keys.
+    const long groups = (columns + of_group - 1) / of_group * kv.count * kv.heads;
+    c.many = !fine && columns >= of_group && (groups >= 192 || blocks <= 16);
     if (c.many) {
         c.tiles = (int)((columns + of_group - 1) / of_group), c.splits = 1, c.columns = 0;
         return c;
     }
     c.tiles = (int)((columns + kColumns - 1) / kColumns);
     c.columns = (int)std::min<long>(columns, kColumns);
-    const long reach = std::min<long>(kv.max_len, (long)kv.table_stride * kKvBlock);
-    const long keys = window ? std::min(reach, (long)window + kv.max_new + sinks + 2 * kKvBlock) : reach;
-    const long blocks = std::max(1l, (keys + kKvBlock - 1) / kKvBlock), units = std::max(1l, (long)kv.count * kv.heads * c.tiles);
+    // Workgroups for one round of the card, with 32 blocks at least: 64 sequences of 8192 tokens take 161 us in 512 workgroups,
+    // 191 us in 1024 and 208 us in 4096.
+    const long units = std::max(1l, (long)kv.count * kv.heads * c.tiles);
     c.splits = (int)std::max(1l, std::min((512 + units - 1) / units, (blocks + 31) / 32));
     return c;
 }
@@ -674,25 +674,29 @@ int launch_kv_attention(void *stream, const KvArgs &kv, int heads_q, float scale
     a.sums = (float *)workspace;
     a.stats = a.sums + (size_t)kv.count * kv.heads * c.places() * kv.dim;
     const unsigned groups = (unsigned)((long)kv.count * kv.heads * c.tiles * c.splits);
-    auto launch = [&](auto nc) {
-        constexpr int NC = decltype(nc)::value;
+    auto launch = [&](auto n32) {
+        constexpr int N32 = decltype(n32)::value, NC = (N32 + 1) / 2;
         if (c.many) {
-            hipLaunchKernelGGL((kv_attention_many_kernel<NC, many_tiles(NC)>), dim3(groups), dim3(64 * kGroup), NC * 32768, (hipStream_t)stream, a);
+            hipLaunchKernelGGL((kv_attention_many_kernel<N32>), dim3(groups), dim3(64 * kGroup), N32 * 16384, (hipStream_t)stream, a);
             return;
         }
         if (fine)
-            hipLaunchKernelGGL((kv_attention_kernel<NC, 3>), dim3(groups), dim3(64 * kWaves), 0, (hipStream_t)stream, a);
+            hipLaunchKernelGGL((kv_attention_kernel<N32, 3>), dim3(groups), dim3(64 * kWaves), 0, (hipStream_t)stream, a);
         else
-            hipLaunchKernelGGL((kv_attention_kernel<NC, 2>), dim3(groups), dim3(64 * kWaves), 0, (hipStream_t)stream, a);
+            hipLaunchKernelGGL((kv_attention_kernel<N32, 2>), dim3(groups), dim3(64 * kWaves), 0, (hipStream_t)stream, a);
         if (c.splits == 1) return;
         const unsigned rows = (unsigned)((long)kv.count * kv.heads * c.tiles * c.columns);
         hipLaunchKernelGGL(kv_attention_join_kernel<NC>, dim3(rows), dim3(64 * kJoinWaves), 0, (hipStream_t)stream, a);
     };
-    switch ((kv.dim + 63) / 64) {
+    switch ((kv.dim + 31) / 32) {
         case 1: launch(std::integral_constant<int, 1>()); break;
         case 2: launch(std::integral_constant<int, 2>()); break;
         case 3: launch(std::integral_constant<int, 3>()); break;
-        default: launch(std::integral_constant<int, 4>()); break;
+        case 4: launch(std::integral_constant<int, 4>()); break;
+        case 5: launch(std::integral_constant<int, 5>()); break;
+        case 6: launch(std::integral_constant<int, 6>()); break;
+        case 7: launch(std::integral_constant<int, 7>()); break;
+        default: launch(std::integral_constant<int, 8>()); break;
     }
     return hipGetLastError() != hipSuccess;
 }
