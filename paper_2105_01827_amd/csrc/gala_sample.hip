@@ -88,21 +88,34 @@ struct Row {
     }
     __device__ bool cuts() const { return !greedy && first >= 0 && (most > 0 || share < 1); }
 };
-__device__ __forceinline__ u64 wave_min(u64 v) {
-    for (int k = 32; k; k >>= 1) v = min(v, (u64)__shfl_xor(v, k));
+// Reductions over a wavefront's lanes by data-parallel moves: within rows of 16 lanes, then from row to row.  The
+// exchange through LDS that shuffles take is ten times the latency, and these kernels are chains of such steps.
+template <int CTRL, int ROWS>
+__device__ __forceinline__ u64 moved(u64 v, u64 none) {
+    const u32 low = __builtin_amdgcn_update_dpp((int)none, (int)v, CTRL, ROWS, 0xf, false);
+    const u32 high = __builtin_amdgcn_update_dpp((int)(none >> 32), (int)(v >> 32), CTRL, ROWS, 0xf, false);
+    return (u64)high << 32 | low;
+}
+template <class F>
+__device__ __forceinline__ u64 scanned(u64 v, u64 none, F f) {
+    v = f(v, moved<0x111, 0xf>(v, none));        // from 1, 2, 4 and 8 lanes below in the row
+    v = f(v, moved<0x112, 0xf>(v, none));
+    v = f(v, moved<0x114, 0xf>(v, none));
+    v = f(v, moved<0x118, 0xf>(v, none));
+    v = f(v, moved<0x142, 0xa>(v, none));        // rows 1 and 3 from the last lane of the row below
+    v = f(v, moved<0x143, 0xc>(v, none));        // rows 2 and 3 from lane 31
     return v;
 }
-__device__ __forceinline__ u64 wave_sum(u64 v) {
-    for (int k = 32; k; k >>= 1) v += __shfl_xor(v, k);
-    return v;
+__device__ __forceinline__ u64 from_lane(u64 v, int lane) {
+    return (u64)(u32)__builtin_amdgcn_readlane((int)(v >> 32), lane) << 32 | (u32)__builtin_amdgcn_readlane((int)v, lane);
 }
 // over the wavefront's lanes up to the own one
 __device__ __forceinline__ u64 upto_of(u64 v) {
-    for (int k = 1; k < 64; k <<= 1) {
-        const u64 x = __shfl_up(v, k);
-        if ((threadIdx.x & 63) >= k) v += x;
-    }
-    return v;
+    return scanned(v, 0, [](u64 a, u64 b) { return a + b; });
+}
+__device__ __forceinline__ u64 wave_sum(u64 v) { return from_lane(upto_of(v), 63); }
+__device__ __forceinline__ u64 wave_min(u64 v) {
+    return from_lane(scanned(v, ~0ull, [](u64 a, u64 b) { return min(a, b); }), 63);
 }
 // by every wavefront for itself, from the chunks' largest logits
 __device__ __forceinline__ Row row_of(const Sample &a, int row) {
@@ -234,11 +247,7 @@ __device__ Cut cut_of(const Sample &a, const Row &r, int row, Bins &bins) {
         m[k] = sum, n[k] = all;
     }
     u64 before = upto_of(sum);
-    u32 count = all;
-    for (int k = 1; k < 64; k <<= 1) {
-        const u32 y = __shfl_up(count, k);
-        if (lane >= k) count += y;
-    }
+    u32 count = (u32)upto_of(all);
     if (lane == 63) bins.part_mass[wave] = before, bins.part_count[wave] = count;
     if (tid == 0) bins.k_bin = kBins - 1, bins.p_low = bins.p_high = kBins - 1;
     __syncthreads();
