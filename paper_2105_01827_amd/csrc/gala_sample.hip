@@ -135,41 +135,52 @@ __device__ __forceinline__ Row row_of(const Sample &a, int row) {
     return r;
 }
 
-// f(logit, index) for the logits from `lo` to `hi`, a thread's in ascending order: 16 bytes a load where they lie on
-// 16 bytes, several loads under way together, and what is before and behind them one by one.  After each load
-// done(index, next): the first index of the wavefront's 64 loads and of its next ones, neither beyond the last logit;
-// behind the last load next is -1.
+// The logits of a row from `lo` to `hi`: 16 bytes a load where they lie on 16 bytes, several loads under way together,
+// and what is before and behind them one by one.
 struct Nothing {
     __device__ void operator()(int, int) const {}
 };
-template <int TYPE, int THREADS, class F, class D = Nothing>
-__device__ __forceinline__ void for_each_logit(const Values &logits, int row, int lo, int hi, F f, D done = D()) {
+template <int TYPE, int THREADS>
+struct Logits {
     typedef typename Element<TYPE>::type E;
-    constexpr int kOf = 16 / sizeof(E), kLoads = TYPE == GALA_RESIDUE ? 8 : 4;
-    const E *x = (const E *)logits.data + row * logits.stride;
-    const int tid = threadIdx.x, off = (int)((uintptr_t)(x + lo) / sizeof(E) % kOf), begin = min(hi, lo + (off ? kOf - off : 0));
-    const int vectors = (hi - begin) / kOf, behind = begin + vectors * kOf;
-    auto value = [&](E v) { return to_float<TYPE>(v, logits.unit, logits.p); };
-    if (lo + tid < begin) f(value(x[lo + tid]), lo + tid);
-    for (int at = tid; at - (tid & 63) < vectors; at += kLoads * THREADS) {
-        union {
-            int4 word;
-            E e[kOf];
-        } v[kLoads];
-#pragma unroll
-        for (int k = 0; k < kLoads; ++k) v[k].word = *(const int4 *)(x + begin + (long)min(at + k * THREADS, vectors - 1) * kOf);
-#pragma unroll
-        for (int k = 0; k < kLoads; ++k) {
-            if (at + k * THREADS < vectors)
-#pragma unroll
-                for (int j = 0; j < kOf; ++j) f(value(v[k].e[j]), begin + (at + k * THREADS) * kOf + j);
-            const int here = begin + (at - (tid & 63) + k * THREADS) * kOf;
-            done(min(here, hi - 1), min(here + THREADS * kOf, hi - 1));
-        }
+    static constexpr int kOf = 16 / sizeof(E), kLoads = TYPE == GALA_RESIDUE ? 8 : 4;
+    union Vector {
+        int4 word;
+        E e[kOf];
+    };
+    const Values &logits;
+    const E *x;
+    int lo, hi, begin, vectors, behind;
+
+    __device__ __forceinline__ Logits(const Values &logits, int row, int lo, int hi) : logits(logits), lo(lo), hi(hi) {
+        x = (const E *)logits.data + row * logits.stride;
+        const int off = (int)((uintptr_t)(x + lo) / sizeof(E) % kOf);
+        begin = min(hi, lo + (off ? kOf - off : 0)), vectors = (hi - begin) / kOf, behind = begin + vectors * kOf;
     }
-    if (behind + tid < hi) f(value(x[behind + tid]), behind + tid);
-    done(hi - 1, -1);
-}
+    // f(logit, index), a thread's in ascending order.  After each load done(index, next): the first index of the
+    // wavefront's 64 loads and of its next ones, neither beyond the last logit; behind the last load next is -1.
+    template <class F, class D = Nothing>
+    __device__ __forceinline__ void each(F f, D done = D()) {
+        const int tid = threadIdx.x;
+        auto value = [&](E e) { return to_float<TYPE>(e, logits.unit, logits.p); };
+        if (lo + tid < begin) f(value(x[lo + tid]), lo + tid);
+        for (int at = tid; at - (tid & 63) < vectors; at += kLoads * THREADS) {
+            Vector v[kLoads];
+#pragma unroll
+            for (int k = 0; k < kLoads; ++k) v[k].word = *(const int4 *)(x + begin + (long)min(at + k * THREADS, vectors - 1) * kOf);
+#pragma unroll
+            for (int k = 0; k < kLoads; ++k) {
+                if (at + k * THREADS < vectors)
+#pragma unroll
+                    for (int j = 0; j < kOf; ++j) f(value(v[k].e[j]), begin + (at + k * THREADS) * kOf + j);
+                const int here = begin + (at - (tid & 63) + k * THREADS) * kOf;
+                done(min(here, hi - 1), min(here + THREADS * kOf, hi - 1));
+            }
+        }
+        if (behind + tid < hi) f(value(x[behind + tid]), behind + tid);
+        done(hi - 1, -1);
+    }
+};
 
 template <int TYPE>
 __global__ __launch_bounds__(kThreads) void sample_best_kernel(Sample a) {
@@ -177,7 +188,8 @@ __global__ __launch_bounds__(kThreads) void sample_best_kernel(Sample a) {
     const int row = blockIdx.x / a.groups, c = blockIdx.x % a.groups, tid = threadIdx.x;
     float top = -INFINITY;
     int first = -1;
-    for_each_logit<TYPE, kThreads>(a.logits, row, a.from<TYPE>(row, c * a.each), a.from<TYPE>(row, (c + 1) * a.each), [&](float z, int i) {
+    Logits<TYPE, kThreads> logits(a.logits, row, a.from<TYPE>(row, c * a.each), a.from<TYPE>(row, (c + 1) * a.each));
+    logits.each([&](float z, int i) {
         if (z > top) top = z, first = i;
     });
     u64 best = wave_min(key_of(top, first));
@@ -192,17 +204,23 @@ __global__ __launch_bounds__(kThreads) void sample_best_kernel(Sample a) {
     }
 }
 
+__device__ __forceinline__ bool asks_to_cut(const Sample &a, int row) {
+    const int most = a.how.top_k ? a.how.top_k[row] : 0;
+    return (most > 0 && most < a.vocab) || (a.how.top_p && a.how.top_p[row] < 1);
+}
 template <int TYPE>
 __global__ __launch_bounds__(kThreads) void sample_bins_kernel(Sample a) {
     __shared__ u64 mass[kBins];
     __shared__ u32 count[kBins];
     const int row = blockIdx.x / a.groups, c = blockIdx.x % a.groups;
+    if (!asks_to_cut(a, row)) return;
+    Logits<TYPE, kThreads> logits(a.logits, row, a.from<TYPE>(row, c * a.each), a.from<TYPE>(row, (c + 1) * a.each));
     const Row r = row_of(a, row);
     if (!r.cuts()) return;
     for (int i = threadIdx.x; i < kBins; i += kThreads) mass[i] = 0, count[i] = 0;
     __syncthreads();
     const bool counts = r.most > 0, weighs = r.share < 1;
-    for_each_logit<TYPE, kThreads>(a.logits, row, a.from<TYPE>(row, c * a.each), a.from<TYPE>(row, (c + 1) * a.each), [&](float z, int) {
+    logits.each([&](float z, int) {
         const int bin = r.bin(z);
         if (bin == kBins - 1) return;            // what is left over is in the last one
         if (counts) atomicAdd(&count[bin], 1u);
@@ -234,16 +252,31 @@ __device__ __forceinline__ u64 passed(float share, u64 all) {
     const double below = ceil((double)share * (double)all) - 1;
     return below > 0 && all ? min((u64)below, all - 1) : 0;
 }
+// the bins that a thread adds up
+struct Filled {
+    u64 mass[2];
+    u32 count[2];
+};
 template <int THREADS>
-__device__ Cut cut_of(const Sample &a, const Row &r, int row, Bins &bins) {
+__device__ __forceinline__ Filled filled_of(const Sample &a, int row) {
+    static_assert(2 * THREADS >= kBins);
+    Filled f;
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+        const int i = 2 * (int)threadIdx.x + k;
+        f.mass[k] = i < kBins ? a.ws.mass[(long)row * kBins + i] : 0, f.count[k] = i < kBins ? a.ws.count[(long)row * kBins + i] : 0;
+    }
+    return f;
+}
+template <int THREADS>
+__device__ Cut cut_of(const Row &r, const Filled &filled, Bins &bins) {
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    constexpr int kEach = (kBins + THREADS - 1) / THREADS;
+    constexpr int kEach = 2;
     u64 m[kEach], sum = 0;
     u32 n[kEach], all = 0;
 #pragma unroll
     for (int k = 0; k < kEach; ++k) {
-        const int i = tid * kEach + k;
-        sum += i < kBins ? a.ws.mass[(long)row * kBins + i] : 0, all += i < kBins ? a.ws.count[(long)row * kBins + i] : 0;
+        sum += filled.mass[k], all += filled.count[k];
         m[k] = sum, n[k] = all;
     }
     u64 before = upto_of(sum);
@@ -285,19 +318,20 @@ __global__ __launch_bounds__(kThreads) void sample_gather_kernel(Sample a) {
     __shared__ Bins bins;
     __shared__ u64 sure[kMostChunks];
     const int row = blockIdx.x / a.groups, group = blockIdx.x % a.groups, tid = threadIdx.x;
+    const int first = group * a.each, chunks = min(a.each, a.chunks - first);
+    Logits<TYPE, kThreads> logits(a.logits, row, a.from<TYPE>(row, first), a.from<TYPE>(row, first + chunks));
+    const Filled filled = filled_of<kThreads>(a, row);
     const Row r = row_of(a, row);
     if (r.greedy || r.first < 0) return;
-    const int first = group * a.each, chunks = min(a.each, a.chunks - first);
     for (int i = tid; i < chunks; i += kThreads) sure[i] = 0;
     Cut cut{kBins, kBins, -1, kBins - 1, false};
-    if (r.cuts()) cut = cut_of<kThreads>(a, r, row, bins);
+    if (r.cuts()) cut = cut_of<kThreads>(r, filled, bins);
     __syncthreads();
     // tokens beyond this bin weigh nothing or less than min-p asks: their weights need not be computed
     const int reach = min(cut.sure, r.least > 0 ? (int)fminf(-logf(r.least) * kBinsPerUnit + 2, kBins - 1) + 1 : kBins - 1);
     const int lo = a.from<TYPE>(row, first), past = chunks > 1 ? a.from<TYPE>(row, first + 1) - a.chunk : lo;
     u64 sum = 0;
-    for_each_logit<TYPE, kThreads>(
-        a.logits, row, lo, a.from<TYPE>(row, first + chunks),
+    logits.each(
         [&](float z, int i) {
             const int bin = r.bin(z);
             if (bin < reach) sum += r.kept(z);
@@ -362,6 +396,14 @@ __global__ __launch_bounds__(kDrawThreads) void sample_draw_kernel(Sample a) {
     __shared__ u64 unsorted[kCounted];
     __shared__ int found, place[kCounted];
     const int row = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    // all that does not depend on the cut is asked for at once
+    static_assert(kMostChunks <= kDrawThreads);
+    const float u = a.how.u[row];
+    const u64 sure = tid < a.chunks ? a.ws.sure[(long)row * a.chunks + tid] : 0;
+    const int n = (int)a.ws.listed[row];
+    const u64 *list = a.ws.list + (long)row * kListed;
+    const u64 early = list[tid % kCounted];
+    const Filled filled = filled_of<kDrawThreads>(a, row);
     const Row r = row_of(a, row);
     if (r.greedy || r.first < 0) {
         if (tid == 0) a.tokens[row] = r.first;
@@ -369,7 +411,7 @@ __global__ __launch_bounds__(kDrawThreads) void sample_draw_kernel(Sample a) {
     }
     // of a token's index: what its chunks' borders lie behind multiples of a chunk
     const int past = a.chunks > 1 ? a.from<TYPE>(row, 1) - a.chunk : 0;
-    for (int i = tid; i < a.chunks; i += kDrawThreads) chunk_mass[i] = a.ws.sure[(long)row * a.chunks + i];
+    if (tid < a.chunks) chunk_mass[tid] = sure;
     // sum over the workgroup's threads
     auto sum_of = [&](u64 v) {
         v = wave_sum(v);
@@ -381,13 +423,12 @@ __global__ __launch_bounds__(kDrawThreads) void sample_draw_kernel(Sample a) {
     auto before_wave = [&]() { return wave_sum(lane < wave ? part[lane] : 0); };
     u64 last = ~0ull;                                  // the last key that is kept
     if (r.cuts()) {
-        const Cut cut = cut_of<kDrawThreads>(a, r, row, bins);
-        const int n = (int)a.ws.listed[row];
+        const Cut cut = cut_of<kDrawThreads>(r, filled, bins);
         if (n > kListed) {
             // more than a list holds: the cuts from the whole row, and the chunks' sums anew
             auto each_of = [&](auto weight) {
                 return [&a, row, weight, &last](auto f) {
-                    for_each_logit<TYPE, kDrawThreads>(a.logits, row, 0, a.vocab, [&](float z, int i) {
+                    Logits<TYPE, kDrawThreads>(a.logits, row, 0, a.vocab).each([&](float z, int i) {
                         const u64 key = key_of(z, i);
                         if (key <= last) f(key, weight(z));
                     });
@@ -412,12 +453,11 @@ __global__ __launch_bounds__(kDrawThreads) void sample_draw_kernel(Sample a) {
             }
             __syncthreads();
         } else {
-            const u64 *list = a.ws.list + (long)row * kListed;
             if (n <= kCounted) {
                 // a short list in order: a token's place is the number of those before it
                 constexpr int kParts = kDrawThreads / kCounted;
                 const int c = tid % kCounted;
-                for (int i = tid; i < kCounted; i += kDrawThreads) unsorted[i] = i < n ? list[i] : ~0ull, place[i] = 0;
+                if (tid < kCounted) unsorted[tid] = tid < n ? early : ~0ull, place[tid] = 0;
                 __syncthreads();
                 const u64 own = unsorted[c];
                 int before = 0;
@@ -506,7 +546,7 @@ __global__ __launch_bounds__(kDrawThreads) void sample_draw_kernel(Sample a) {
     u64 sum = 0;
     for (int i = tid; i < a.chunks; i += kDrawThreads) sum += chunk_mass[i];
     const u64 all = sum_of(sum);
-    const double drawn = (double)a.how.u[row] * (double)all;
+    const double drawn = (double)u * (double)all;
     u64 target = drawn > 0 ? min((u64)drawn, all - 1) : 0;
     if (wave == 0) {
         constexpr int kOf = kMostChunks / 64;
