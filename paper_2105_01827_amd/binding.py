@@ -226,11 +226,13 @@ def _values(t, unit):
         if str(t.dtype) not in _TYPES:
             raise TypeError(f"values are float32, float16, bfloat16, or residues in 64-bit words: got {t.dtype}")
         kind = _types[t.dtype] = _TYPES[str(t.dtype)]
-    strides, shape, step = t.stride(), t.shape, 1
-    for i in range(len(strides) - 1, 0, -1):
-        if strides[i] != step and shape[i] != 1:
-            raise ValueError("the values of a row have to be contiguous")
-        step *= shape[i]
+    strides = t.stride()
+    if len(strides) != 3 or strides[2] != 1 or strides[1] != t.size(2):        # not heads x head_dim as they mostly lie
+        step = 1
+        for i in range(len(strides) - 1, 0, -1):
+            if strides[i] != step and t.size(i) != 1:
+                raise ValueError("the values of a row have to be contiguous")
+            step *= t.size(i)
     return _pack_values(t.data_ptr(), strides[0], kind, unit)
 
 
@@ -697,6 +699,7 @@ class KvCache:
         if codes.numel() != codes.shape[0] * self.page_bytes(heads, head_dim) or scales.numel() != codes.shape[0] * heads * 2:
             raise ValueError("codes and scales do not fit the heads and their dimension")
         self.codes, self.scales = codes, scales
+        self._lib, self._ctx = ctx.lib, ctx.h
         self.arg = KvCacheArg(heads, head_dim, codes.shape[0], 0, _words(codes, "torch.int8", "codes"),
                               _words(scales, "torch.float32", "scales"))
         self.ref = C.byref(self.arg)
@@ -706,24 +709,24 @@ class KvCache:
         return int(load().gala_kv_cache_bytes(1, heads, head_dim))
 
     def _heads(self, q):
-        return math.prod(q.shape[1:]) // self.head_dim
+        return q.size(1) if q.dim() == 3 else math.prod(q.shape[1:]) // self.head_dim
 
     def append(self, batch, k, v, q=None, q_out=None, rope=None, unit=1.0, stream=None):
         """k, v (rows, heads, head_dim) into the cache; q (rows, heads_q, head_dim) rotated into q_out."""
-        _check(self.ctx.lib.gala_kv_append(self.ctx.h, _stream(stream), self.ref, batch.ref, None if rope is None else rope.ref,
+        _check(self._lib.gala_kv_append(self._ctx, _stream(stream), self.ref, batch.ref, None if rope is None else rope.ref,
                                            0 if q is None else self._heads(q), None if q is None else _values(q, unit),
                                            None if q_out is None else _values(q_out, unit), None if k is None else _values(k, unit),
                                            None if v is None else _values(v, unit)), "gala_kv_append")
 
     def export(self, batch, k_out, v_out, unit=1.0, stream=None):
-        _check(self.ctx.lib.gala_kv_export(self.ctx.h, _stream(stream), self.ref, batch.ref, _values(k_out, unit),
+        _check(self._lib.gala_kv_export(self._ctx, _stream(stream), self.ref, batch.ref, _values(k_out, unit),
                                            _values(v_out, unit)), "gala_kv_export")
 
     def attention_workspace_bytes(self, batch, heads_q, window=0, sinks=0):
-        return int(self.ctx.lib.gala_kv_attention_workspace(self.ref, batch.ref, heads_q, window, sinks))
+        return int(self._lib.gala_kv_attention_workspace(self.ref, batch.ref, heads_q, window, sinks))
 
     def attention(self, batch, q, out, scale, workspace, workspace_bytes, window=0, sinks=0, unit=1.0, stream=None):
         """q (rows, heads_q, head_dim) -> out of the same shape."""
-        _check(self.ctx.lib.gala_kv_attention(self.ctx.h, _stream(stream), self.ref, batch.ref, self._heads(q), scale, window, sinks,
+        _check(self._lib.gala_kv_attention(self._ctx, _stream(stream), self.ref, batch.ref, self._heads(q), scale, window, sinks,
                                               _values(q, unit), _values(out, unit), _at(workspace), workspace_bytes),
                "gala_kv_attention")
