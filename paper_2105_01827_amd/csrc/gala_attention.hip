@@ -13,7 +13,6 @@ namespace {
 typedef int v4i __attribute__((ext_vector_type(4)));
 typedef float v4f __attribute__((ext_vector_type(4)));
 
-constexpr int kWaves = 4;            // of a workgroup
 constexpr int kColumns = 16;         // queries that a wavefront's products take at once
 constexpr float kLog2E = 1.4426950408889634f;
 
@@ -24,6 +23,7 @@ struct Attention {
     int heads_q, group;              // group: query heads of a head of the cache
     float scale;
     int window, sinks;
+    int waves;                       // wavefronts of a workgroup
     int tiles, splits, columns;      // column tiles of a head, shares of its keys, columns of a tile that are kept
     float *sums, *stats;             // of every share: columns x dim, and columns x (largest, sum)
 };
@@ -53,9 +53,9 @@ __device__ __forceinline__ Seen seen_by(const Attention &a, int b, int tile, int
     return s;
 }
 // blocks of a share
-__device__ __forceinline__ int share_of(int total, int splits) {
-    const int each = (total + splits - 1) / splits;
-    return (each + kWaves - 1) / kWaves * kWaves;
+__device__ __forceinline__ int share_of(const Attention &a, int total) {
+    const int each = (total + a.splits - 1) / a.splits;
+    return (each + a.waves - 1) / a.waves * a.waves;
 }
 
 // 8 x N channels of a row from `column` on, 0 from `end` on; eight at a load where rows lie on 16 bytes
@@ -132,7 +132,7 @@ __device__ __forceinline__ float joined(const v4i (&acc)[ND], int r) {
 // 16 of one column's, and they are the very weights that it hands to the second product, because the values' codes
 // lie in that order of tokens.  So a block goes from memory to the sums without LDS or an exchange between lanes, but
 // for the largest score.  A wavefront has blocks of its own; a workgroup's wavefronts are joined at the end.
-template <int N32, int ND>
+template <int N32, int ND, int kWaves>
 __global__ __launch_bounds__(64 * kWaves, N32 * ND <= 12 ? 2 : 1) void kv_attention_kernel(Attention a) {
     constexpr int NC = (N32 + 1) / 2, NV = 2 * N32;          // products of 64 channels, tiles of 16
     __shared__ float sums[kWaves][kColumns][NV * 16 + 1];
@@ -147,7 +147,7 @@ __global__ __launch_bounds__(64 * kWaves, N32 * ND <= 12 ? 2 : 1) void kv_attent
     const int h = unit % kv.heads, b = unit / kv.heads;
     const Seen s = seen_by(a, b, tile);
     if (!s.cols) return;
-    const int share = share_of(s.total, a.splits), from = split * share, to = min(s.total, from + share);
+    const int share = share_of(a, s.total), from = split * share, to = min(s.total, from + share);
     if (split && from >= s.total) return;
     // The next block's keys and scales are under way while this one's weights are made, the one after's page too.
     const size_t head_bytes = kv_head_bytes(kv.dim16);
@@ -343,7 +343,7 @@ __global__ __launch_bounds__(64 * kJoinWaves) void kv_attention_join_kernel(Atte
     const int h = unit % kv.heads, b = unit / kv.heads;
     const Seen s = seen_by(a, b, tile);
     if (cc >= s.cols) return;
-    const int share = share_of(s.total, a.splits), used = share ? max(1, (s.total + share - 1) / share) : 1;
+    const int share = share_of(a, s.total), used = share ? max(1, (s.total + share - 1) / share) : 1;
     const long place = (((long)b * kv.heads + h) * a.tiles + tile) * a.splits;
     const float *stats = a.stats + (place * a.columns + cc) * 2, *sums = a.sums + (place * a.columns + cc) * kv.dim;
     const long next = a.columns;
@@ -680,10 +680,24 @@ int launch_kv_attention(void *stream, const KvArgs &kv, int heads_q, float scale
             hipLaunchKernelGGL((kv_attention_many_kernel<N32>), dim3(groups), dim3(64 * kGroup), N32 * 16384, (hipStream_t)stream, a);
             return;
         }
-        if (fine)
-            hipLaunchKernelGGL((kv_attention_kernel<N32, 3>), dim3(groups), dim3(64 * kWaves), 0, (hipStream_t)stream, a);
-        else
-            hipLaunchKernelGGL((kv_attention_kernel<N32, 2>), dim3(groups), dim3(64 * kWaves), 0, (hipStream_t)stream, a);
+        // A launch that leaves CUs with one workgroup gets eight wavefronts in each: 32 windows of 1024 tokens take 12.0 us with
+        // eight and 14.0 with four; 64 sequences of 500 tokens in 512 workgroups 16.9 and 13.4.
+        auto waves = [&](auto w) {
+            constexpr int W = decltype(w)::value;
+            a.waves = W;
+            if (fine)
+                hipLaunchKernelGGL((kv_attention_kernel<N32, 3, W>), dim3(groups), dim3(64 * W), 0, (hipStream_t)stream, a);
+            else
+                hipLaunchKernelGGL((kv_attention_kernel<N32, 2, W>), dim3(groups), dim3(64 * W), 0, (hipStream_t)stream, a);
+        };
+        if constexpr (N32 <= 4) {
+            if (groups <= 256)
+                waves(std::integral_constant<int, 8>());
+            else
+                waves(std::integral_constant<int, 4>());
+        } else {
+            waves(std::integral_constant<int, 4>());
+        }
         if (c.splits == 1) return;
         const unsigned rows = (unsigned)((long)kv.count * kv.heads * c.tiles * c.columns);
         hipLaunchKernelGGL(kv_attention_join_kernel<NC>, dim3(rows), dim3(64 * kJoinWaves), 0, (hipStream_t)stream, a);
