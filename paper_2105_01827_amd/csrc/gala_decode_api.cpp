@@ -2,6 +2,7 @@
 // happens here, and nothing waits.
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
 #include <cmath>
 
 #include "gala_decode.h"
@@ -10,6 +11,7 @@ using namespace gala;
 
 namespace {
 
+constexpr int kFarthest = 1 << 30;      // no sequence is longer: distances beyond it are cut to it
 constexpr double kTwoPi = 6.283185307179586476925286766559;
 
 size_t type_size(int type) { return type == GALA_F32 ? 4 : type == GALA_RESIDUE ? 8 : 2; }
@@ -32,7 +34,7 @@ bool batch_ok(const gala_kv_batch *b) {
     if (!b || b->count < 0 || b->max_new < 0 || b->max_len < 0 || b->table_stride < 0) return false;
     if (b->count && (!b->starts || !b->lens || (b->table_stride && !b->table))) return false;
     // positions and tokens fit 32 bits with room for a block
-    return b->max_new <= (1 << 30) && b->max_len <= (1 << 30) && b->table_stride <= (1 << 24);
+    return b->max_new <= kFarthest && b->max_len <= kFarthest && b->table_stride <= (1 << 24);
 }
 KvArgs kv_args(const gala_kv_cache *k, const gala_kv_batch *b) {
     KvArgs a{};
@@ -124,7 +126,7 @@ extern "C" int gala_kv_export(const gala_ctx *c, void *stream, const gala_kv_cac
 extern "C" size_t gala_kv_attention_workspace(const gala_kv_cache *cache, const gala_kv_batch *batch, int heads_q, int window,
                                               int sinks) {
     if (!attention_ok(cache, batch, heads_q, window, sinks)) return 0;
-    return kv_attention_workspace(kv_args(cache, batch), heads_q, window, sinks);
+    return kv_attention_workspace(kv_args(cache, batch), heads_q, std::min(window, kFarthest), std::min(sinks, kFarthest));
 }
 
 extern "C" int gala_kv_attention(const gala_ctx *c, void *stream, const gala_kv_cache *cache, const gala_kv_batch *batch,
@@ -135,6 +137,7 @@ extern "C" int gala_kv_attention(const gala_ctx *c, void *stream, const gala_kv_
     if (!values_ok(q, row, false) || !values_ok(out, row, true)) return GALA_EARG;
     if (out->data == q->data && (out->type != q->type || out->stride != q->stride)) return GALA_EARG;
     const KvArgs kv = kv_args(cache, batch);
+    window = std::min(window, kFarthest), sinks = std::min(sinks, kFarthest);
     const size_t need = kv_attention_workspace(kv, heads_q, window, sinks);
     if (need && (!workspace || (uintptr_t)workspace % 16)) return GALA_EARG;
     if (workspace_bytes < need) return GALA_ENOMEM;

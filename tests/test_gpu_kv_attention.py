@@ -327,3 +327,35 @@ def test_prompts_into_other_types(ctx):
     for kind, out in (("bf16", "f16"), ("f16", "bf16")):
         c = Case(ctx, [130], [300], 64, 2, 96, kind, out, seed=43)
         c.check(c.run(), {(0, 0), (0, 77), (0, 129)})
+
+
+@pytest.mark.parametrize("kind,new", [("bf16", 1), ("f32", 3), ("f16", 150), ("residue", 2)])
+def test_rows_that_begin_anywhere(ctx, kind, new):
+    """Rows on 16 bytes, and the same rows an element further on: the same bits."""
+    c = Case(ctx, [new, 1], [300, 90], 32, 4, 64, kind, seed=50)
+    want, q = c.run(), c.q
+    c.q = torch.empty(q.numel() + 8, dtype=q.dtype, device="cuda")[1:1 + q.numel()].view(q.shape).copy_(q)
+    out = torch.empty(q.numel() + 8, dtype=want.dtype, device="cuda")[3:3 + q.numel()].view(q.shape)
+    assert torch.equal(c.run(out=out), want)
+
+
+@pytest.mark.parametrize("window,sinks", [(2 ** 31 - 1, 0), (2 ** 31 - 1, 2 ** 31 - 1), (5, 2 ** 31 - 1), (2 ** 30, 3)])
+def test_windows_without_end(ctx, window, sinks):
+    for new in (2, 130):
+        c = Case(ctx, [new, 10], [200, 4], 32, 4, 64, seed=51)
+        want = c.run()
+        assert torch.equal(c.run(window=window, sinks=sinks), want)
+
+
+def test_in_place_for_prompts(ctx):
+    c = Case(ctx, [150, 1], [300, 90], 32, 4, 64, "bf16", seed=52)
+    want = c.run()
+    c.q = c.q.clone()
+    assert torch.equal(c.run(out=c.q), want)
+
+
+def test_prompts_are_the_same_bits_again(ctx):
+    c = Case(ctx, [300, 200], [400, 200], 32, 4, 96, "f16", seed=53)
+    want = c.run()
+    for _ in range(3):
+        assert torch.equal(c.run(), want)

@@ -249,3 +249,41 @@ def test_another_stream_and_a_graph(ctx):
         torch.cuda.synchronize()
         live = codes != 77
         assert torch.equal(out, want) and torch.equal(s.cache.codes[live], codes[live])
+
+
+@pytest.mark.parametrize("kind", ["f32", "f16", "bf16", "residue"])
+@pytest.mark.parametrize("new", [(70, 3), (1, 1)])
+def test_rows_that_begin_anywhere(ctx, kind, new):
+    """Rows on 16 bytes, and the same rows an element further on: the same bits."""
+    heads, dim = 2, 64
+    results = []
+    for shift in (0, 1):
+        s = Sequences(ctx, heads, dim, 2, 2, seed=12)
+        rope = binding.Rope(torch.from_numpy(binding.rope_table(128, 64)).cuda())
+        out = torch.float32 if kind == "residue" else TYPES[kind]
+        for step in (new, (2, 5)):
+            starts, batch = s.step(step)
+            total = int(starts[-1])
+            row = 4 * heads * dim
+            wide = torch.zeros(total * (row + 1) + 8, dtype=TYPES[kind], device="cuda")
+            rows = wide[shift:shift + total * (row + shift)].view(total, row + shift)[:, :row].view(total, 4 * heads, dim)
+            rows.copy_(_values(s.gen, kind, total, 4 * heads, dim))
+            q, k, v = rows.split([2 * heads, heads, heads], 1)
+            q_out = torch.zeros(total * 2 * heads * dim + 8, dtype=out, device="cuda")[shift:shift + total * 2 * heads * dim].view(total, 2 * heads, dim)
+            s.cache.append(batch, k, v, q=q, q_out=q_out, rope=rope, unit=UNIT)
+        back = [torch.zeros(total * heads * dim + 8, dtype=out, device="cuda")[shift:shift + total * heads * dim].view(total, heads, dim) for _ in range(2)]
+        s.cache.export(batch, *back)
+        results.append([q_out.clone()] + [b.clone() for b in back])
+    for a, b in zip(*results):
+        assert torch.equal(a, b)
+
+
+def test_interleaved_pairs_of_odd_counts(ctx):
+    """Rotations that end inside a piece of eight channels."""
+    for rot, interleaved in ((6, True), (12, True), (24, False), (40, False), (8, True)):
+        s = Sequences(ctx, 1, 48, 1, 2, seed=rot)
+        table = binding.rope_table(100, rot)
+        starts, batch = s.step((70,))
+        k, v = (_values(s.gen, "f32", 70, 1, 48) for _ in range(2))
+        s.cache.append(batch, k, v, rope=binding.Rope(torch.from_numpy(table).cuda(), interleaved))
+        s.expect(starts, ref.rotate(_plain(k), table, np.arange(70), interleaved), _plain(v))

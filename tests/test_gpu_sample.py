@@ -199,3 +199,42 @@ def test_another_stream_and_a_graph(ctx):
         graph.replay()
         torch.cuda.synchronize()
         assert torch.equal(tokens, want)
+
+
+@pytest.mark.parametrize("rows,vocab,kind", [(2, 3000001, "f32"), (600, 300, "bf16"), (1, 1100000, "f16"), (40, 4097, "residue")])
+def test_many_rows_and_many_tokens(ctx, rows, vocab, kind):
+    """Chunks of more tokens than usual, and more rows than the card has workgroups."""
+    logits = _logits(rows, vocab, kind, seed=vocab)
+    plain = _plain(logits)
+    for how in [(0.8, 0, 1.0, 0.0), (0.8, 100, 0.9, 0.0), (0.6, 0, 0.5, 0.0)]:
+        hows = [_away(z, how) for z in plain]
+        chosen = [_choose(z, *h, pick=(0.07 + 0.37 * r) % 1) for r, (z, h) in enumerate(zip(plain, hows))]
+        t, k, p, m = zip(*hows)
+        got = _run(ctx, logits.cuda(), [c[0] for c in chosen], temperature=t, top_k=k, top_p=p, min_p=m)
+        assert got.tolist() == [c[1] for c in chosen]
+
+
+def test_cuts_among_many_close_logits(ctx):
+    """A bin that holds more tokens than a list: the cut is searched over the whole row."""
+    z = (torch.randn(3, 60000, generator=torch.Generator().manual_seed(8)) * 1e-3).float()
+    plain = _plain(z)
+    hows = [_away(p, h) for p, h in zip(plain, [(1.0, 20000, 1.0, 0.0), (1.0, 0, 0.3, 0.0), (1.0, 30000, 0.6, 0.999)])]
+    for row, (p, h) in enumerate(zip(plain, hows)):
+        kept, w, _ = ref.kept_tokens(p, *h)
+        run = np.cumsum(np.where(kept, w, 0.0))
+        for u in (0.1, 0.5, 0.9):
+            t, k, q, m = h
+            token = int(_run(ctx, z[row:row + 1].cuda(), [u], temperature=[t], top_k=[k], top_p=[q], min_p=[m])[0])
+            assert kept[token]
+            # a share of 1 / 20000 is as small as the weights' rounding can be told apart from
+            assert run[token] / run[-1] - w[token] / run[-1] - MARGIN <= u <= run[token] / run[-1] + MARGIN
+
+
+def test_logits_that_begin_anywhere(ctx):
+    z = _logits(3, 5000, "f16", seed=77).cuda()
+    u = [0.2, 0.5, 0.8]
+    want = _run(ctx, z, u, top_p=[0.9] * 3)
+    for shift in (1, 3, 7):
+        moved = torch.empty(3, 5009, dtype=torch.float16, device="cuda").flatten()[shift:shift + 3 * 5001].view(3, 5001)[:, :5000]
+        moved.copy_(z)
+        assert _run(ctx, moved, u, top_p=[0.9] * 3).tolist() == want.tolist()
