@@ -234,7 +234,10 @@ __device__ __forceinline__ int value_place(int t, int d) { return (d >> 4) * 102
 template <int TYPE, int THREADS, int MOST16>
 __device__ void append_pieces(const KvArgs &kv, const RopeArgs &rope, const Values &x, const Pieces &pieces, int which, int h, int b, int j,
                               signed char *tile, float *shared) {
+    // Items a thread may have of each kind, and rows of registers for both: pairs take rows from the front, singles from the
+    // back.  With p pairs of m x 16 channels that is 2 ceil(p / 4) + ceil((m - p) / 2), at most m / 2 + 2.
     constexpr int kTokens = THREADS / 4, kPairs = (MOST16 * kTokens + THREADS - 1) / THREADS, kSingles = (2 * MOST16 * kTokens + THREADS - 1) / THREADS;
+    constexpr int kRows = MOST16 / 2 + 2;
     const int start = kv.starts[b], n = kv.starts[b + 1] - start, first = kv.lens[b] - n;
     const int block = max(first, 0) / kKvBlock + j, at = block * kKvBlock;
     const int lo = max(first, at);
@@ -248,17 +251,17 @@ __device__ void append_pieces(const KvArgs &kv, const RopeArgs &rope, const Valu
     const float old = lo > at ? *scale_at : 0.0f;
     const int pairs = which ? 0 : pieces.pairs, singles = which ? kv.dim16 * 2 : pieces.singles;
     const Divisor of_singles = which ? Divisor(kv.dim16 * 2) : pieces.of_singles;
-    float p[kPairs][2][8], s[kSingles][8], most = 0;
+    float v[kRows][8], most = 0;
     // item q of a token's pieces: lane r of four has token 4 * quad + r
     auto token_of = [&](int q, const Divisor &of, int &piece) {
         const int rest = q >> 2, quad = of(rest);
         piece = rest - quad * of.d;
         return quad * 4 + (q & 3);
     };
-    auto meet = [&](const float (&v)[8]) {
+    auto meet = [&](const float (&row)[8]) {
 #pragma unroll
         for (int k = 0; k < 8; ++k) {
-            const float a = fabsf(v[k]);
+            const float a = fabsf(row[k]);
             if (a < INFINITY) most = fmaxf(most, a);
         }
     };
@@ -268,22 +271,26 @@ __device__ void append_pieces(const KvArgs &kv, const RopeArgs &rope, const Valu
         const int q = tid + k * THREADS, t = token_of(q, pieces.of_pairs, piece);
         if (pairs && t < count) {
             const long row = start + (lo + t - first);
-            load_piece<TYPE>(x, row, h * dim + piece * 8, p[k][0]);
-            load_piece<TYPE>(x, row, h * dim + rope.half + piece * 8, p[k][1]);
-            turn(rope.table + ((long)(lo + t) * rope.half + piece * 8) * 2, p[k][0], p[k][1]);
-            meet(p[k][0]), meet(p[k][1]);
+            load_piece<TYPE>(x, row, h * dim + piece * 8, v[2 * k]);
+            load_piece<TYPE>(x, row, h * dim + rope.half + piece * 8, v[2 * k + 1]);
+            turn(rope.table + ((long)(lo + t) * rope.half + piece * 8) * 2, v[2 * k], v[2 * k + 1]);
+            meet(v[2 * k]), meet(v[2 * k + 1]);
         }
     }
 #pragma unroll
     for (int k = 0; k < kSingles; ++k) {
         int piece;
         const int q = tid + k * THREADS, t = token_of(q, of_singles, piece), d = (2 * pairs + piece) * 8;
+        float (&own)[8] = v[kRows - 1 - k];
+        if (singles && t < count) {
+            if (d < dim) {
+                load_piece<TYPE>(x, start + (lo + t - first), h * dim + d, own);
+                if (!which && rope.table && rope.interleaved && d < 2 * rope.half) turn(rope.table + ((long)(lo + t) * rope.half + d / 2) * 2, own);
+                meet(own);
+            } else {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) s[k][i] = 0;
-        if (singles && t < count && d < dim) {
-            load_piece<TYPE>(x, start + (lo + t - first), h * dim + d, s[k]);
-            if (!which && rope.table && rope.interleaved && d < 2 * rope.half) turn(rope.table + ((long)(lo + t) * rope.half + d / 2) * 2, s[k]);
-            meet(s[k]);
+                for (int i = 0; i < 8; ++i) own[i] = 0;
+            }
         }
     }
     for (int k = 32; k; k >>= 1) most = fmaxf(most, __shfl_xor(most, k));
@@ -311,8 +318,8 @@ __device__ void append_pieces(const KvArgs &kv, const RopeArgs &rope, const Valu
         __syncthreads();
     }
     // a whole block is put in order in LDS, part of one goes to its places
-    auto put = [&](int t, int d, const float (&v)[8]) {
-        const u32 low = codes_of(v, inverse), high = codes_of(v + 4, inverse);
+    auto put = [&](int t, int d, const float (&row)[8]) {
+        const u32 low = codes_of(row, inverse), high = codes_of(row + 4, inverse);
         if (which == 0) {
             *(uint2 *)((whole ? tile : codes) + key_place(t, d, kv.dim16)) = uint2{low, high};
         } else if (whole) {
@@ -328,13 +335,13 @@ __device__ void append_pieces(const KvArgs &kv, const RopeArgs &rope, const Valu
     for (int k = 0; k < kPairs; ++k) {
         int piece;
         const int q = tid + k * THREADS, t = token_of(q, pieces.of_pairs, piece);
-        if (pairs && t < count) put(t_lo + t, piece * 8, p[k][0]), put(t_lo + t, rope.half + piece * 8, p[k][1]);
+        if (pairs && t < count) put(t_lo + t, piece * 8, v[2 * k]), put(t_lo + t, rope.half + piece * 8, v[2 * k + 1]);
     }
 #pragma unroll
     for (int k = 0; k < kSingles; ++k) {
         int piece;
         const int q = tid + k * THREADS, t = token_of(q, of_singles, piece), d = (2 * pairs + piece) * 8;
-        if (singles && t < count) put(t_lo + t, d, s[k]);
+        if (singles && t < count) put(t_lo + t, d, v[kRows - 1 - k]);
     }
     if (whole) {
         __syncthreads();
