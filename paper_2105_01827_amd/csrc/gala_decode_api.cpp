@@ -102,7 +102,7 @@ extern "C" int gala_kv_append(const gala_ctx *c, void *stream, const gala_kv_cac
         return GALA_EARG;
     const int64_t blocks = (batch->max_new + 62) / 64 + 1;
     if (heads_q > (1 << 20) || !fits_grid((int64_t)batch->count * batch->max_new) ||
-        !fits_grid((int64_t)batch->count * blocks * cache->heads * 2 + (int64_t)batch->count * batch->max_new))
+        !fits_grid(((int64_t)batch->count * blocks + 7) * cache->heads * 2 + (int64_t)batch->count * batch->max_new))
         return GALA_EARG;
     if (!c->has_device) return GALA_EHIP;
     if (!batch->count || !batch->max_new || (!q && !k)) return GALA_OK;
@@ -117,7 +117,7 @@ extern "C" int gala_kv_export(const gala_ctx *c, void *stream, const gala_kv_cac
     if (!c || !cache_ok(cache) || !batch_ok(batch)) return GALA_EARG;
     const int64_t row = (int64_t)cache->heads * cache->head_dim;
     if (!values_ok(k_out, row, true) || !values_ok(v_out, row, true) || k_out->type != v_out->type) return GALA_EARG;
-    if (!fits_grid((int64_t)batch->count * ((batch->max_new + 62) / 64 + 1) * cache->heads * 2)) return GALA_EARG;
+    if (!fits_grid(((int64_t)batch->count * ((batch->max_new + 62) / 64 + 1) + 7) * cache->heads * 2)) return GALA_EARG;
     if (!c->has_device) return GALA_EHIP;
     if (!batch->count || !batch->max_new) return GALA_OK;
     return launch_kv_export(stream, kv_args(cache, batch), values(c, k_out), values(c, v_out)) ? GALA_EHIP : GALA_OK;
