@@ -429,9 +429,8 @@ int gala_kv_export(const gala_ctx *ctx, void *stream, const gala_kv_cache *cache
  * heads_q a multiple of the cache's heads; query head h reads head h / (heads_q / heads); out may be q where the
  * types agree.  Operands of the products, sums in 32 bits: queries enter as whole numbers of 16 bits of their row's
  * largest and weights as 15 bits of the largest so far; as 24 and 23 where q or out is GALA_F32 or GALA_RESIDUE; else,
- * where a sequence brings 128 queries or more for a head of the cache, both may enter in half precision, queries scaled
- * by a power of two to their row's largest, weights times their block's scale of values to within 2^8 of the largest.
- * All of these are below the rounding of the outputs' types, half precision's own 11 bits at the most apart.
+ * where a sequence brings 128 queries or more for a head of the cache, weights may enter in half precision (11 bits, in
+ * units of 2^-24 of the largest at the least), multiplied by their block's scale of values.
  * workspace: device scratch, caller-owned, of gala_kv_attention_workspace bytes (0 for bad arguments).  Asynchronous,
  * allocates nothing; results do not depend on timing.  Errors: GALA_EARG, GALA_ENOMEM (workspace too small), GALA_EHIP. */
 size_t gala_kv_attention_workspace(const gala_kv_cache *cache, const gala_kv_batch *batch, int heads_q, int window,

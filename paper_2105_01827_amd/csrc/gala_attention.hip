@@ -127,6 +127,45 @@ __device__ __forceinline__ float joined(const v4i (&acc)[ND], int r) {
         return fmaf((float)acc[ND - 1][r], 65536.0f, (float)low);
 }
 
+// A lane's part of a query, 16 channels of each 64, as digits; returns what a unit of them is worth in exponents of 2,
+// with the scale.  `bad`: the query holds a NaN or an infinity; its digits are 0 then.
+template <int NC, int ND>
+__device__ __forceinline__ float digits_of(const float (&x)[NC][16], float scale, v4i (&qd)[NC][ND], bool &bad) {
+    float most = 0;
+    bool fine = true;
+#pragma unroll
+    for (int k = 0; k < NC; ++k)
+#pragma unroll
+        for (int j = 0; j < 16; ++j) {
+            most = fmaxf(most, fabsf(x[k][j]));
+            fine &= fabsf(x[k][j]) < INFINITY;
+        }
+    most = fmaxf(most, __shfl_xor(most, 16));
+    most = fmaxf(most, __shfl_xor(most, 32));
+    int all = fine;
+    all &= __shfl_xor(all, 16);
+    all &= __shfl_xor(all, 32);
+    bad = !all;
+    const bool some = most > 0 && !bad;
+    // a power of two first: the reciprocal of a tiny number would be infinite
+    const int e = some ? min(max(ilogbf(most), -126), 126) : 0;
+    const float down = ldexpf(1.0f, -e), scaled = some ? most * down : 1.0f, mul = Digits<ND>::most / scaled * (scale < 0 ? -1.0f : 1.0f);
+    const float unit_q = ldexpf(scaled / Digits<ND>::most, e) * fabsf(scale) * kLog2E;
+#pragma unroll
+    for (int k = 0; k < NC; ++k)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            u32 w[4];
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const int v = some ? (int)rintf(x[k][4 * j + r] * down * mul) : 0;
+                w[r] = (u32)(v + (ND == 2 ? 128 : 128 * 257));
+            }
+            planes<ND>(w, j, qd[k]);
+        }
+    return unit_q;
+}
+
 // Both products run on the matrix cores as exact sums of 8-bit products: the cache's codes as they lie in memory by
 // the base-256 digits of the queries and of the weights (NC x 64 channels; ND digits).  Of a block's scores a lane has
 // 16 of one column's, and they are the very weights that it hands to the second product, because the values' codes
@@ -182,8 +221,7 @@ __global__ __launch_bounds__(64 * kWaves, N32 * ND <= 12 ? 2 : 1) void kv_attent
     float unit_q;
     bool bad;
     {
-        float x[NC][16], most = 0;
-        bool fine = true;
+        float x[NC][16];
         auto load = [&](auto type) __attribute__((always_inline)) {
 #pragma unroll
             for (int k = 0; k < NC; ++k) {
@@ -192,36 +230,7 @@ __global__ __launch_bounds__(64 * kWaves, N32 * ND <= 12 ? 2 : 1) void kv_attent
             }
         };
         by_type(a.q.type, load);
-#pragma unroll
-        for (int k = 0; k < NC; ++k)
-#pragma unroll
-            for (int j = 0; j < 16; ++j) {
-                most = fmaxf(most, fabsf(x[k][j]));
-                fine &= fabsf(x[k][j]) < INFINITY;
-            }
-        most = fmaxf(most, __shfl_xor(most, 16));
-        most = fmaxf(most, __shfl_xor(most, 32));
-        int all = fine;
-        all &= __shfl_xor(all, 16);
-        all &= __shfl_xor(all, 32);
-        bad = !all;
-        const bool some = most > 0 && !bad;
-        // a power of two first: the reciprocal of a tiny number would be infinite
-        const int e = some ? min(max(ilogbf(most), -126), 126) : 0;
-        const float down = ldexpf(1.0f, -e), scaled = some ? most * down : 1.0f, mul = Digits<ND>::most / scaled * (a.scale < 0 ? -1.0f : 1.0f);
-        unit_q = ldexpf(scaled / Digits<ND>::most, e) * fabsf(a.scale) * kLog2E;
-#pragma unroll
-        for (int k = 0; k < NC; ++k)
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                u32 w[4];
-#pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    const int v = some ? (int)rintf(x[k][4 * j + r] * down * mul) : 0;
-                    w[r] = (u32)(v + (ND == 2 ? 128 : 128 * 257));
-                }
-                planes<ND>(w, j, qd[k]);
-            }
+        unit_q = digits_of<NC, ND>(x, a.scale, qd, bad);
     }
     v4f o[NV];
 #pragma unroll
@@ -374,11 +383,12 @@ __global__ __launch_bounds__(64 * kJoinWaves) void kv_attention_join_kernel(Atte
 }
 
 // ---- many queries of a sequence ---------------------------------------------------------------------------------------
-// Here the products and the weights count, not the cache's bytes.  The codes are whole numbers that half precision holds
-// exactly, so a workgroup turns a block into half-precision fragments in LDS once, for kGroup wavefronts of a
-// column tile each; both products run on the matrix cores in half precision with 32-bit sums, queries scaled to their
-// row's largest (11 bits of each channel), weights in 11 bits.  A weight carries its block's scale of values, so that the
-// sums need no work between blocks: w = 2^(t + log2(scale) - base), base within 2^8 of the largest so far.
+// Here the products and the weights count, not the cache's bytes.  Scores are the same exact sums as above; of the values a
+// workgroup makes half-precision fragments in LDS once for its eight wavefronts of a column tile each (the codes are whole
+// numbers that half precision holds exactly), so that the second product adds up in 32-bit floats and needs no work
+// between blocks.  Its other operand, a weight, is rounded to 11 bits and carries its block's scale of values:
+// w = 2^(t + log2(scale) - base), base within 2^8 of the largest so far.  Keys stay 8-bit in LDS: half the reads of
+// half-precision fragments.  Wavefronts in their products go before those that make weights.
 constexpr int kGroup = 8;
 typedef _Float16 v8h __attribute__((ext_vector_type(8)));
 typedef _Float16 v2h __attribute__((ext_vector_type(2)));
@@ -403,8 +413,8 @@ __device__ __forceinline__ void halves_of(const v4i &codes, v8h (&to)[2]) {
 
 template <int NK>
 __global__ __launch_bounds__(64 * kGroup, NK <= 4 ? 4 : 2) void kv_attention_many_kernel(Attention a) {
-    constexpr int NV = 2 * NK;                       // tiles of 16 channels, beside NK products of 32
-    constexpr int kHalf = NK * 4096, kBuffer = 2 * kHalf;           // keys, then values
+    constexpr int NC = (NK + 1) / 2, NV = 2 * NK;    // products of 64 channels of keys, tiles of 16 channels of values
+    constexpr int kKeys = NC * 4096, kBuffer = kKeys + NK * 4096;   // keys as they are, values in half precision
     constexpr int kLoads = (2 * NK + kGroup - 1) / kGroup;          // pieces of 16 codes a thread loads, of keys and of values
     extern __shared__ __attribute__((aligned(16))) char lds[];
     const KvArgs &kv = a.kv;
@@ -422,39 +432,23 @@ __global__ __launch_bounds__(64 * kGroup, NK <= 4 ? 4 : 2) void kv_attention_man
     const int base_at = s.at_lo - s.col0 / a.group, at_lo = base_at + min(c0, c1) / a.group, at_hi = base_at + c1 / a.group;
     const bool idle = c0 > c1;
     int at;
-    v8h qf[NK];
+    v4i qd[NC][2];
     float unit_q;
     bool bad;
     {
         const int c = min(c0 + col, s.col0 + s.cols - 1), qi = c / a.group, hq = h * a.group + c % a.group;
         const long row = s.start + qi;
         at = base_at + qi;
-        float most = 0;
-        bool fine = true;
-        float x[NK][8];
+        float x[NC][16];
+        auto load = [&](auto type) __attribute__((always_inline)) {
 #pragma unroll
-        for (int k = 0; k < NK; ++k) {
-            auto load = [&](auto type) __attribute__((always_inline)) {
-                load_channels<decltype(type)::value, 1>(a.q, a.pieces, row, hq * kv.dim + k * 32 + part * 8, hq * kv.dim + kv.dim, x[k]);
-            };
-            by_type(a.q.type, load);
-#pragma unroll
-            for (int j = 0; j < 8; ++j) most = fmaxf(most, fabsf(x[k][j])), fine &= fabsf(x[k][j]) < INFINITY;
-        }
-        most = fmaxf(most, __shfl_xor(most, 16));
-        most = fmaxf(most, __shfl_xor(most, 32));
-        int all = fine;
-        all &= __shfl_xor(all, 16);
-        all &= __shfl_xor(all, 32);
-        bad = !all;
-        const bool some = most > 0 && all;
-        const int e = some ? min(max(ilogbf(most), -126), 126) : 0;
-        const float down = some ? ldexpf(a.scale < 0 ? -1.0f : 1.0f, -e) : 0.0f;
-        unit_q = ldexpf(fabsf(a.scale) * kLog2E, e);
-#pragma unroll
-        for (int k = 0; k < NK; ++k)
-#pragma unroll
-            for (int j = 0; j < 8; ++j) qf[k][j] = some ? (_Float16)(x[k][j] * down) : (_Float16)0;
+            for (int k = 0; k < NC; ++k) {
+                const int d = k * 64 + part * 16;
+                load_channels<decltype(type)::value, 2>(a.q, a.pieces, row, hq * kv.dim + d, hq * kv.dim + kv.dim, x[k]);
+            }
+        };
+        by_type(a.q.type, load);
+        unit_q = digits_of<NC, 2>(x, a.scale, qd, bad);
     }
     v4f o[NV];
     float base = 0, limit = -INFINITY, sum = 0;      // limit: what an exponent may be before the base is raised
@@ -463,9 +457,7 @@ __global__ __launch_bounds__(64 * kGroup, NK <= 4 ? 4 : 2) void kv_attention_man
     // channels that fill up a product of 32 are zero in both buffers from here on
     if (kv.dim16 & 1)
         for (int i = tid; i < 2 * 128; i += 64 * kGroup) {
-            char *to = lds + (i >> 7) * kBuffer;
-            *(v4i *)(to + ((i >> 5 & 3) * NK + NK - 1) * 1024 + 512 + (i & 31) * 16) = v4i{0, 0, 0, 0};
-            *(v4i *)(to + kHalf + ((i >> 6 & 1) * NV + NV - 1) * 1024 + (i & 63) * 16) = v4i{0, 0, 0, 0};
+            *(v4i *)(lds + (i >> 7) * kBuffer + kKeys + ((i >> 6 & 1) * NV + NV - 1) * 1024 + (i & 63) * 16) = v4i{0, 0, 0, 0};
         }
     // a block's pieces on their way from the cache to LDS
     const size_t head_bytes = kv_head_bytes(kv.dim16);
@@ -475,7 +467,7 @@ __global__ __launch_bounds__(64 * kGroup, NK <= 4 ? 4 : 2) void kv_attention_man
 #pragma unroll
     for (int k = 0; k < kLoads; ++k) {
         const int i = tid + k * 64 * kGroup, t16 = (i >> 4) / kv.dim16, d16 = (i >> 4) - t16 * kv.dim16;
-        key_at[k] = (t16 * NK + (d16 >> 1)) * 1024 + (d16 & 1) * 512 + (i & 15) * 16;
+        key_at[k] = (t16 * 4 * NC + d16) * 256 + (i & 15) * 16;
     }
     float scale_k = 0, scale_v = 0;
     int page = -1, page_next = 0;
@@ -498,15 +490,13 @@ __global__ __launch_bounds__(64 * kGroup, NK <= 4 ? 4 : 2) void kv_attention_man
     page_next = page_at(0);
     if (s.total) fetch(0);
     for (int u = 0; u < s.total; ++u) {
-        char *keys = lds + (u & 1) * kBuffer, *values = keys + kHalf;
+        char *keys = lds + (u & 1) * kBuffer, *values = keys + kKeys;
 #pragma unroll
         for (int k = 0; k < kLoads; ++k) {
             if (tid + k * 64 * kGroup < pieces) {
-                v8h x[2];
-                // keys: of a product of 32 channels a lane has eight of a token
-                halves_of(staged[0][k], x);
-                *(v8h *)(keys + key_at[k]) = x[0], *(v8h *)(keys + key_at[k] + 256) = x[1];
+                *(v4i *)(keys + key_at[k]) = staged[0][k];
                 // values: the first and the last 32 tokens of a channel
+                v8h x[2];
                 halves_of(staged[1][k], x);
                 char *to = values + (tid + k * 64 * kGroup) * 16;
                 *(v8h *)to = x[0], *(v8h *)(to + NV * 1024) = x[1];
@@ -519,16 +509,23 @@ __global__ __launch_bounds__(64 * kGroup, NK <= 4 ? 4 : 2) void kv_attention_man
         if (idle || t0 > at_hi || t0 >= end || (a.window && t0 + 63 <= at_lo - a.window && t0 >= a.sinks)) continue;
         const bool edge = t0 + 63 > at_lo || t0 + 64 > end || (a.window && t0 <= at_hi - a.window);
         const float log_v = __builtin_amdgcn_logf(now_v), unit_l = 1.0f / now_v;
+        __builtin_amdgcn_s_setprio(1);
         v4f acc[4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) acc[i] = v4f{0, 0, 0, 0};
+        for (int i = 0; i < 4; ++i) {
+            v4i sums[2];
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
+            for (int n = 0; n < 2; ++n) sums[n] = v4i{0, 0, 0, 0};
 #pragma unroll
-            for (int k = 0; k < NK; ++k) {
-                const v8h x = *(const v8h *)(keys + (i * NK + k) * 1024 + lane * 16);
-                acc[i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(x, qf[k], acc[i], 0, 0, 0);
+            for (int k = 0; k < NC; ++k) {       // channels beyond the head's meet digits of 0
+                const v4i x = *(const v4i *)(keys + (i * NC + k) * 1024 + lane * 16);
+#pragma unroll
+                for (int n = 0; n < 2; ++n) sums[n] = __builtin_amdgcn_mfma_i32_16x16x64_i8(x, qd[k][n], sums[n], 0, 0, 0);
             }
+#pragma unroll
+            for (int r = 0; r < 4; ++r) acc[i][r] = joined<2>(sums, r);
+        }
+        __builtin_amdgcn_s_setprio(0);
         v8h w[2];
         const float unit_s = fmaxf(unit_q * now_k, 0x1p-126f);      // not 0: what is not seen stays at -infinity
         if (edge) {
@@ -581,11 +578,13 @@ __global__ __launch_bounds__(64 * kGroup, NK <= 4 ? 4 : 2) void kv_attention_man
                 w[i >> 1][(i & 1) * 4 + r] = (_Float16)x;
             }
         sum = fmaf(part_sum, unit_l, sum);
+        __builtin_amdgcn_s_setprio(1);
 #pragma unroll
         for (int f = 0; f < 2 * NV; ++f) {
             o[f >> 1] = __builtin_amdgcn_mfma_f32_16x16x32_f16(ahead[f & 3], w[f & 1], o[f >> 1], 0, 0, 0);
             if (f + 4 < 2 * NV) ahead[f & 3] = fragment(f + 4);
         }
+        __builtin_amdgcn_s_setprio(0);
     }
     float all = sum;
     all += __shfl_xor(all, 16);
@@ -677,7 +676,7 @@ int launch_kv_attention(void *stream, const KvArgs &kv, int heads_q, float scale
     auto launch = [&](auto n32) {
         constexpr int N32 = decltype(n32)::value, NC = (N32 + 1) / 2;
         if (c.many) {
-            hipLaunchKernelGGL((kv_attention_many_kernel<N32>), dim3(groups), dim3(64 * kGroup), N32 * 16384, (hipStream_t)stream, a);
+            hipLaunchKernelGGL((kv_attention_many_kernel<N32>), dim3(groups), dim3(64 * kGroup), 2 * (NC + N32) * 4096, (hipStream_t)stream, a);
             return;
         }
         // A launch that leaves CUs with one workgroup gets eight wavefronts in each: 32 windows of 1024 tokens take 12.0 us with

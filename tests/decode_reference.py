@@ -102,8 +102,8 @@ def kept_tokens(z, temperature, top_k, top_p, min_p):
 
 
 def attention_in_halves(q, k, v, scales, seen, scale):
-    """The same with half-precision operands: each channel of the query and each weight times its block's scale of values
-    (`scales`, a token each) rounded to 11 bits, such a weight to 2^-25 of the largest of them at least; sums in 32 bits."""
+    """The same with queries of 16 bits and weights in half precision: each weight times its block's scale of values (`scales`, a
+    token each) rounded to 11 bits, or to 2^-25 of the largest of them where that is more; sums in 32 bits."""
     dim = len(q)
     if not seen.any():
         return np.zeros(dim), np.zeros(dim)
@@ -111,8 +111,7 @@ def attention_in_halves(q, k, v, scales, seen, scale):
     s = scale * (k @ q)
     w = np.exp(s - s.max())
     out = (w[:, None] * v).sum(0) / w.sum()
-    size = abs(scale) * (np.abs(k) @ np.abs(q))
-    slack = (2.0 ** -11 + 2.0 ** -20) * size + 2.0 ** -20 * (np.abs(s) + np.abs(s).max() + 1)
+    slack = abs(scale) * np.abs(k).sum(1) * np.abs(q).max() * 2.0 ** -15 + 2.0 ** -20 * (np.abs(s) + abs(scale) * (np.abs(k) @ np.abs(q)) + np.abs(s).max() + 1)
     rel = np.expm1(2 * slack.max()) + 2.0 ** -11
     spread = (w[:, None] * np.abs(v)).sum(0) / w.sum()
     return out, 2 * rel * spread + len(w) * 127 * 2.0 ** -25 * (w * scales).max() / w.sum() + 2.0 ** -18 * spread
