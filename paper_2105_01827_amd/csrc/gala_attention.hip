@@ -419,10 +419,11 @@ __global__ __launch_bounds__(64 * kGroup, NK <= 4 ? 4 : 2) void kv_attention_man
     extern __shared__ __attribute__((aligned(16))) char lds[];
     const KvArgs &kv = a.kv;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 15, part = lane >> 4, tid = threadIdx.x;
+    // The last queries see most keys: they go first, of all heads (4096 tokens alone 173 us; head after head 223).  A head's groups
+    // go to one XCD where there are eight heads.
     int unit = blockIdx.x;
-    // the last queries see most keys: they go first
-    const int group = a.tiles - 1 - unit % a.tiles;
-    unit /= a.tiles;
+    const int per_group = kv.count * kv.heads, group = a.tiles - 1 - unit / per_group;
+    unit %= per_group;
     const int h = unit % kv.heads, b = unit / kv.heads;
     constexpr int kColumnsOf = kGroup * kColumns;
     const Seen s = seen_by(a, b, group, kColumnsOf);
