@@ -11,11 +11,14 @@ using namespace gala;
 // A row's tokens are put into bins by how far their logit is below the largest, a cut is found from the bins' counts
 // and weights, and only the bin that the cut falls into is looked at token by token.  A row is shared by several
 // workgroups, and each step that needs all of them is a launch of its own:
-//   best    the largest logit of every chunk of the row;
+//   best    the largest logit of every workgroup's part of the row;
 //   bins    counts and weights of the bins, where the row has a top-k or top-p;
 //   gather  of every chunk, the weight of the tokens that are kept for sure, and a list of those in the cut's bin;
 //   draw    the cut within its bin, the chunk that the uniform number falls into, and the token in it.
 // Weights are whole numbers, so the sums do not depend on who adds what first.
+// Many long rows are bound by HBM (256 of 131072 residues: 268 MB read twice in 105 us of 113), fewer by the vector ALU (64 of
+// 100003 with top-p: 44 instructions a logit in `bins`, 12.7 of 36.7 us), one row by its four launches (2.9, 4.6, 6.0
+// and 10.0 us for 32000 logits).
 namespace {
 
 constexpr int kThreads = 512, kDrawThreads = 512;
@@ -24,7 +27,9 @@ constexpr float kWeightOne = 1099511627776.0f;      // 2^40
 constexpr int kBins = 896;
 constexpr float kBinsPerUnit = 32.0f;
 constexpr int kListed = 2048;                       // tokens of a list; a row that needs more is searched as a whole
-constexpr int kCounted = 128;                       // longest list that is put in order by counting
+// Longest list that is put in order by counting: a list of a few tokens takes 23.3 us of one row's time so and 27.0 us through the
+// network.
+constexpr int kCounted = 128;
 constexpr int kMostChunks = 256;
 
 // A logit's place in descending order: the larger, the smaller; both zeros alike.
@@ -117,7 +122,7 @@ __device__ __forceinline__ u64 wave_sum(u64 v) { return from_lane(upto_of(v), 63
 __device__ __forceinline__ u64 wave_min(u64 v) {
     return from_lane(scanned(v, ~0ull, [](u64 a, u64 b) { return min(a, b); }), 63);
 }
-// by every wavefront for itself, from the chunks' largest logits
+// by every wavefront for itself, from the largest logits of the row's parts
 __device__ __forceinline__ Row row_of(const Sample &a, int row) {
     Row r;
     u64 best = ~0ull;
@@ -589,14 +594,15 @@ __global__ __launch_bounds__(kDrawThreads) void sample_draw_kernel(Sample a) {
     }
 }
 
-// Chunks of a row: 4096 tokens, 2048 where rows alone do not fill the card, more where a row would have too many.  Workgroups of a row: enough for the card, with whole
-// chunks each.
+// Chunks of a row: 2048 tokens, which the last launch goes through for the token; more where a row would have too many
+// (64 rows of 100003 logits 36.1 us with 2048, 38.8 with 4096, 36.3 with 1024; 256 of 131072 residues 118, 117 and 126).
+// Workgroups of a row: enough for the card, with whole chunks each; 640 of all rows take 113 us for those residues, 512 118.
 void cut_up(Sample &a) {
-    a.shift = a.rows < 32 ? 11 : 12;
+    a.shift = 11;
     while (((long)a.vocab + (1l << a.shift) - 1) >> a.shift > kMostChunks) ++a.shift;
     a.chunk = 1 << a.shift;
     a.chunks = (int)(((long)a.vocab + a.chunk - 1) / a.chunk);
-    const int wanted = std::max(1, std::min(a.chunks, (512 + a.rows - 1) / std::max(a.rows, 1)));
+    const int wanted = std::max(1, std::min(a.chunks, (640 + a.rows - 1) / std::max(a.rows, 1)));
     a.each = (a.chunks + wanted - 1) / wanted;
     a.groups = (a.chunks + a.each - 1) / a.each;
 }
