@@ -431,8 +431,8 @@ int gala_kv_export(const gala_ctx *ctx, void *stream, const gala_kv_cache *cache
  * largest and weights as 15 bits of the largest so far; as 24 and 23 where q or out is GALA_F32 or GALA_RESIDUE; else,
  * where a sequence brings 128 queries or more for a head of the cache, weights may enter in half precision (11 bits, in
  * units of 2^-24 of the largest at the least), multiplied by their block's scale of values.
- * workspace: device scratch, caller-owned, of gala_kv_attention_workspace bytes (0 for bad arguments).  Asynchronous,
- * allocates nothing; results do not depend on timing.  Errors: GALA_EARG, GALA_ENOMEM (workspace too small), GALA_EHIP. */
+ * workspace: device scratch, caller-owned, 16-byte aligned, of gala_kv_attention_workspace bytes (0 for bad arguments and
+ * where none is needed; it may be NULL then); calls that overlap need one each.  Asynchronous, allocates nothing; results do not depend on timing.  Errors: GALA_EARG, GALA_ENOMEM (workspace too small), GALA_EHIP. */
 size_t gala_kv_attention_workspace(const gala_kv_cache *cache, const gala_kv_batch *batch, int heads_q, int window,
                                    int sinks);
 int gala_kv_attention(const gala_ctx *ctx, void *stream, const gala_kv_cache *cache, const gala_kv_batch *batch,
@@ -449,7 +449,8 @@ int gala_kv_attention(const gala_ctx *ctx, void *stream, const gala_kv_cache *ca
  * and always the first.  The token is the lowest index at which the running sum of kept weights, in the order of
  * indices, exceeds u times their sum.  temperature <= 0: the first token.  NaN logits are never drawn; a row with
  * nothing but NaN and -infinity gives -1; where the largest is +infinity it alone has weight.  temperature, top_k,
- * top_p, min_p, u: one number a row, device memory; each but u may be NULL (1, 0, 1, 0).  tokens: rows of int32_t. */
+ * top_p, min_p, u: one number a row, device memory; each but u may be NULL (1, 0, 1, 0).  tokens: rows of int32_t.
+ * workspace: as above, of gala_sample_workspace bytes.  Asynchronous, allocates nothing. */
 typedef struct {
     const float *temperature;
     const int32_t *top_k;
