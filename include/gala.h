@@ -428,9 +428,9 @@ int gala_kv_export(const gala_ctx *ctx, void *stream, const gala_kv_cache *cache
  * 0, one that holds a NaN or an infinity gives NaN (its own heads' rows alone).  q, out: rows of heads_q x head_dim,
  * heads_q a multiple of the cache's heads; query head h reads head h / (heads_q / heads); out may be q where the
  * types agree.  Operands of the products, sums in 32 bits: queries enter as whole numbers of 16 bits of their row's
- * largest and weights as 15 bits of the largest so far; as 24 and 23 where q or out is GALA_F32 or GALA_RESIDUE; else,
- * where a sequence brings 128 queries or more for a head of the cache, weights may enter in half precision (11 bits, in
- * units of 2^-24 of the largest at the least), multiplied by their block's scale of values.
+ * largest, of 24 where q or out is GALA_F32 or GALA_RESIDUE; weights as 31 bits of the largest in their block; except that
+ * where neither is, and a sequence brings 128 queries or more for a head of the cache, weights may enter in half precision
+ * (11 bits, in units of 2^-24 of the largest at the least), multiplied by their block's scale of values.
  * workspace: device scratch, caller-owned, 16-byte aligned, of gala_kv_attention_workspace bytes (0 for bad arguments and
  * where none is needed; it may be NULL then); calls that overlap need one each.  Asynchronous, allocates nothing; results do not depend on timing.  Errors: GALA_EARG, GALA_ENOMEM (workspace too small), GALA_EHIP. */
 size_t gala_kv_attention_workspace(const gala_kv_cache *cache, const gala_kv_batch *batch, int heads_q, int window,

@@ -104,18 +104,25 @@ __device__ __forceinline__ void planes(const u32 (&w)[4], int at, v4i (&to)[ND])
         to[1][at] = (int)mid;
     } else {
         to[1][at] = (int)(mid ^ 0x80808080u);
-        const u32 ab2 = __builtin_amdgcn_perm(w[1], w[0], 0x0c0c0602), cd2 = __builtin_amdgcn_perm(w[3], w[2], 0x0c0c0602);
-        to[2][at] = (int)__builtin_amdgcn_perm(cd2, ab2, 0x05040100);
+        const u32 ab2 = __builtin_amdgcn_perm(w[1], w[0], 0x07030602), cd2 = __builtin_amdgcn_perm(w[3], w[2], 0x07030602);
+        const u32 third = __builtin_amdgcn_perm(cd2, ab2, 0x05040100);
+        if constexpr (ND == 3) {
+            to[2][at] = (int)third;
+        } else {
+            to[2][at] = (int)(third ^ 0x80808080u);
+            to[3][at] = (int)__builtin_amdgcn_perm(cd2, ab2, 0x07060302);
+        }
     }
 }
 template <int ND>
 struct Digits;
-// the largest number, and 2^23 with 128 in every digit but the highest: added to a float below 2^23 it leaves the
-// float's nearest whole number, offset so, in the low bits
+// the largest number, and 128 in every digit but the highest
 template <>
-struct Digits<2> { static constexpr float most = 127 * 256.0f, offset = 8388608.0f + 128; };
+struct Digits<2> { static constexpr float most = 127 * 256.0f; static constexpr u32 offset = 128; };
 template <>
-struct Digits<3> { static constexpr float most = 127 * 65536.0f, offset = 8388608.0f + 128 * 257; };
+struct Digits<3> { static constexpr float most = 127 * 65536.0f; static constexpr u32 offset = 128 * 257; };
+template <>
+struct Digits<4> { static constexpr float most = 127 * 16777216.0f; static constexpr u32 offset = 128 * 65793; };
 
 // the number whose digits' products were added up apart
 template <int ND>
@@ -123,8 +130,10 @@ __device__ __forceinline__ float joined(const v4i (&acc)[ND], int r) {
     const int low = acc[0][r] + (acc[1][r] << 8);
     if constexpr (ND == 2)
         return (float)low;
+    else if constexpr (ND == 3)
+        return fmaf((float)acc[2][r], 65536.0f, (float)low);
     else
-        return fmaf((float)acc[ND - 1][r], 65536.0f, (float)low);
+        return fmaf((float)(acc[2][r] + (acc[3][r] << 8)), 65536.0f, (float)low);
 }
 
 // A lane's part of a query, 16 channels of each 64, as digits; returns what a unit of them is worth in exponents of 2,
@@ -159,7 +168,7 @@ __device__ __forceinline__ float digits_of(const float (&x)[NC][16], float scale
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
                 const int v = some ? (int)rintf(x[k][4 * j + r] * down * mul) : 0;
-                w[r] = (u32)(v + (ND == 2 ? 128 : 128 * 257));
+                w[r] = (u32)v + Digits<ND>::offset;
             }
             planes<ND>(w, j, qd[k]);
         }
@@ -167,15 +176,18 @@ __device__ __forceinline__ float digits_of(const float (&x)[NC][16], float scale
 }
 
 // Both products run on the matrix cores as exact sums of 8-bit products: the cache's codes as they lie in memory by
-// the base-256 digits of the queries and of the weights (NC x 64 channels; ND digits).  Of a block's scores a lane has
+// the base-256 digits of the queries and of the weights (NC x 64 channels; ND and NW digits).  Of a block's scores a lane has
 // 16 of one column's, and they are the very weights that it hands to the second product, because the values' codes
 // lie in that order of tokens.  So a block goes from memory to the sums without LDS or an exchange between lanes, but
 // for the largest score.  A wavefront has blocks of its own; a workgroup's wavefronts are joined at the end.
-// One query a sequence is bound by HBM: 64 sequences of 8192 tokens (8 heads of 128 channels, 807 MB) take 150 us, 5.4 TB/s; the
-// matrix cores are busy for 0.07 of it.
+// A weight has four digits, 31 bits of the largest in its block: with the two that a query of 16 bits has, thousands of keys that share
+// what one heavy key leaves were rounded away (a quarter of the output where the first token has 0.9 of 8192 keys' weight).
+// One query a sequence is bound by HBM: 64 sequences of 8192 tokens (8 heads of 128 channels, 807 MB) take 157 us, 5.1 TB/s; 151 us
+// with two digits, and 128 queries of 32 heads over 30000 tokens 162 and 124 us.
 template <int N32, int ND, int kWaves>
 __global__ __launch_bounds__(64 * kWaves, N32 * ND <= 12 ? 2 : 1) void kv_attention_kernel(Attention a) {
     constexpr int NC = (N32 + 1) / 2, NV = 2 * N32;          // products of 64 channels, tiles of 16
+    constexpr int NW = 4;                                    // digits of a weight
     __shared__ float sums[kWaves][kColumns][NV * 16 + 1];
     __shared__ float stats[kWaves][kColumns][2];
     const KvArgs &kv = a.kv;
@@ -241,7 +253,7 @@ __global__ __launch_bounds__(64 * kWaves, N32 * ND <= 12 ? 2 : 1) void kv_attent
     for (; u < to; u += kWaves) {
         const int block = s.block(u), end = page < 0 ? 0 : kv.max_len;
         const signed char *codes = kv.codes + ((size_t)max(page, 0) * kv.heads + h) * head_bytes;
-        const float unit_s = unit_q * scale_k, unit_v = scale_v * (1.0f / Digits<ND>::most);
+        const float unit_s = unit_q * scale_k, scale_of_v = scale_v;
         v4i values[NV];
 #pragma unroll
         for (int j = 0; j < NV; ++j)
@@ -285,26 +297,31 @@ __global__ __launch_bounds__(64 * kWaves, N32 * ND <= 12 ? 2 : 1) void kv_attent
 #pragma unroll
             for (int j = 0; j < NV; ++j) o[j] *= was;
         }
-        const float base = top == -INFINITY ? 0.0f : top;
-        v4i w[ND];
+        // Weights as shares of the block's own largest, as whole numbers: a token that outweighs all others by far takes bits from
+        // its block's other tokens at most, not from all that come later.
+        const float base = most == -INFINITY ? 0.0f : most, part_of = most == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(most - top);
+        const float unit_v = scale_of_v * part_of * (1.0f / Digits<NW>::most);
+        float part_sum = 0;
+        v4i w[NW];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             u32 word[4];
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
                 const float p = __builtin_amdgcn_exp2f(t[4 * i + r] - base);
-                sum += p;
-                word[r] = __float_as_uint(fmaf(p, Digits<ND>::most, Digits<ND>::offset));
+                part_sum += p;
+                word[r] = (u32)fmaf(p, Digits<NW>::most, 0.5f) + Digits<NW>::offset;
             }
-            planes<ND>(word, i, w);
+            planes<NW>(word, i, w);
         }
+        sum = fmaf(part_sum, part_of, sum);
 #pragma unroll
         for (int j = 0; j < NV; ++j) {
-            v4i acc[ND];
+            v4i acc[NW];
 #pragma unroll
-            for (int n = 0; n < ND; ++n) acc[n] = __builtin_amdgcn_mfma_i32_16x16x64_i8(values[j], w[n], v4i{0, 0, 0, 0}, 0, 0, 0);
+            for (int n = 0; n < NW; ++n) acc[n] = __builtin_amdgcn_mfma_i32_16x16x64_i8(values[j], w[n], v4i{0, 0, 0, 0}, 0, 0, 0);
 #pragma unroll
-            for (int r = 0; r < 4; ++r) o[j][r] = fmaf(joined<ND>(acc, r), unit_v, o[j][r]);
+            for (int r = 0; r < 4; ++r) o[j][r] = fmaf(joined<NW>(acc, r), unit_v, o[j][r]);
         }
     }
     // the wavefronts' sums in one
@@ -636,8 +653,8 @@ Cut cut_of(const KvArgs &kv, int heads_q, int window, int sinks, bool fine) {
     const long keys = window ? std::min(reach, (long)window + kv.max_new + sinks + 2 * kKvBlock) : reach;
     const long blocks = std::max(1l, (keys + kKvBlock - 1) / kKvBlock);
     // Whole prompts in half precision, where they fill the card or have few keys: 8 x 128 queries of 32 heads over 4000
-    // tokens (256 workgroups) take 110 us so and 142 us as exact sums, 4 x 300 over 300 14 and 30 us; but 4 x 128 over
-    // 4000 (128 workgroups) 108 and 69 us, because exact sums can share a tile's keys.
+    // tokens (256 workgroups) take 105 us so and 179 us as exact sums, 4 x 300 over 300 14 and 33 us; but 4 x 128 over
+    // 4000 (128 workgroups) 104 and 91 us, because exact sums can share a tile's keys.
     const long groups = (columns + of_group - 1) / of_group * kv.count * kv.heads;
     c.many = !fine && columns >= of_group && (groups >= 192 || blocks <= 16);
     if (c.many) {

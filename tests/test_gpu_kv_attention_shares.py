@@ -1,0 +1,84 @@
+"""Attention over the paged 8-bit cache where few keys have most of the weight and thousands share the rest: what those give
+must come out within a few roundings of the output, however many they are.  Values have a mean far from zero, so that what is
+lost does not average out.
+
+Queries are whole multiples of 1/64 with a largest of 127/64, so that whole numbers of 16 bits hold them exactly and the bounds
+need no allowance for the queries' rounding."""
+import numpy as np
+import pytest
+import torch
+
+from tests import decode_reference as ref
+from tests.test_gpu_kv_attention import TYPES, UNIT, Case, _plain, ctx  # noqa: F401
+
+pytestmark = pytest.mark.gpu
+FIRST = 127.0 / 64                # the first channel of every query, and of the first key
+
+
+def _case(ctx, new, lens, heads, group, dim, kind, out, share, spread, seed):
+    """Every sequence's first token has no value and about `share` of the last query's weight; `spread` scales the other keys'
+    scores apart, 0 leaves them equal.  Returns (case, scale of the scores)."""
+    c = Case(ctx, new, lens, heads, group, dim, kind, out, seed=seed)
+    rng = np.random.default_rng(seed)
+    k = rng.integers(-127, 128, c.k.shape).astype(np.int8)
+    v = rng.integers(20, 128, c.v.shape).astype(np.int8)
+    k[..., 0] = 0
+    for pages in c.table.numpy():
+        k[pages[0], :, 0] = 0
+        k[pages[0], :, 0, 0] = 127
+        v[pages[0], :, 0] = 0
+    codes = np.zeros((*k.shape[:2], ref.head_bytes(dim)), np.int8)
+    for part, place in zip((k, v), ref.code_places(dim)):
+        codes[:, :, place] = part
+    c.k, c.v = k, v
+    c.cache.codes.copy_(torch.from_numpy(codes).view(codes.shape[0], -1))
+    c.cache.scales[..., 0] = 1.0 / 64
+    scale = float(np.float32(np.log(share / (1 - share) * (max(lens) - 1)) / FIRST ** 2))
+    q = rng.integers(-3, 4, tuple(c.q.shape)) * (spread / 64)
+    q[..., 0] = FIRST
+    q = torch.from_numpy(q)
+    c.q = (torch.round(q / UNIT).to(torch.int64).remainder(1032193) if kind == "residue" else q.to(TYPES[kind])).cuda()
+    return c, scale
+
+
+def _check(c, out, rows, of_block):
+    """of_block: the largest error of a weight as a share of the largest weight in its block of 64 keys"""
+    got, q, scales = _plain(out), _plain(c.q), c.cache.scales.cpu().double().numpy()
+    eps = ref.UNIT_ROUNDOFF.get(str(out.dtype).replace("torch.", ""), 0)
+    tiny = UNIT / 2 if c.out_kind == "residue" else 2.0 ** -24
+    for b, i in rows:
+        pages, n = c.table[b].numpy(), c.lens[b] - c.new[b] + i + 1
+        for h in range(c.heads * c.group):
+            head = h // c.group
+            k, v = ((x[pages, head].astype(np.float64) * scales[pages, head, w][:, None, None]).reshape(-1, c.dim)[:n]
+                    for w, x in enumerate((c.k, c.v)))
+            x = q[c.starts[b] + i, h]
+            s = c.scale * (k @ x)
+            w = np.exp(s - s.max())
+            want, mean = (w[:, None] * v).sum(0) / w.sum(), (w[:, None] * np.abs(v)).sum(0) / w.sum()
+            # exponents and sums in 32 bits, of the numerator and of the weights' sum
+            slack = 2.0 ** -20 * (np.abs(s) + c.scale * (np.abs(k) @ np.abs(x)) + np.abs(s).max() + 1)
+            bound = (2 * np.expm1(slack.max()) + 2.0 ** -18) * mean
+            edges = np.arange(0, n, 64)
+            bound += of_block * (np.maximum.reduceat(w, edges)[:, None] * np.add.reduceat(np.abs(v), edges)).sum(0) / w.sum()
+            bound += eps * (np.abs(want) + bound) + tiny
+            if n > 64:
+                assert (bound < 0.03 * np.abs(want)).all() or c.out_kind == "residue"          # nothing, or half, would not do
+                assert (bound < 0.2 * np.abs(want)).all()
+            over = (np.abs(got[c.starts[b] + i, h] - want) / bound).max()
+            assert over <= 1, (b, i, h, over, float(np.median(got[c.starts[b] + i, h] / want)))
+
+
+# (new tokens, lengths, heads, query heads of each): one workgroup a head; more than 256 workgroups; keys split over workgroups;
+# short prompts beside a long history
+SHAPES = [([1], [900], 2, 3), ([1] * 20, [1500] * 20, 16, 1), ([1], [8192], 2, 2), ([1, 1], [30001, 20000], 2, 2), ([20, 3], [3000, 2500], 2, 4)]
+
+
+@pytest.mark.parametrize("kind,out", [("f16", "f16"), ("bf16", "bf16"), ("f32", "f32"), ("residue", "f32"), ("f32", "residue")])
+@pytest.mark.parametrize("share,spread", [(0.9, 0), (0.95, 1), (0.98, 0), (0.98, 1)])
+@pytest.mark.parametrize("shape", range(len(SHAPES)))
+def test_a_first_token_without_a_value(ctx, shape, share, spread, kind, out):
+    new, lens, heads, group = SHAPES[shape]
+    c, scale = _case(ctx, new, lens, heads, group, 64, kind, out, share, spread, seed=shape)
+    rows = {(0, 0), (0, new[0] - 1), (len(new) - 1, new[-1] - 1)}
+    _check(c, c.run(scale=scale), rows, 2.0 ** -32)
