@@ -430,7 +430,7 @@ int gala_kv_export(const gala_ctx *ctx, void *stream, const gala_kv_cache *cache
  * types agree.  Operands of the products, sums in 32 bits: queries enter as whole numbers of 16 bits of their row's
  * largest, of 24 where q or out is GALA_F32 or GALA_RESIDUE; weights as 31 bits of the largest in their block; except that
  * where neither is, and a sequence brings 128 queries or more for a head of the cache, weights may enter in half precision
- * (11 bits, in units of 2^-24 of the largest at the least), multiplied by their block's scale of values.
+ * (11 bits, in steps of 2^-31 of the largest so far at the most where they are small), multiplied by their block's scale of values.
  * workspace: device scratch, caller-owned, 16-byte aligned, of gala_kv_attention_workspace bytes (0 for bad arguments and
  * where none is needed; it may be NULL then); calls that overlap need one each.  Asynchronous, allocates nothing; results do not depend on timing.  Errors: GALA_EARG, GALA_ENOMEM (workspace too small), GALA_EHIP. */
 size_t gala_kv_attention_workspace(const gala_kv_cache *cache, const gala_kv_batch *batch, int heads_q, int window,

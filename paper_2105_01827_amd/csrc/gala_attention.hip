@@ -410,7 +410,10 @@ __global__ __launch_bounds__(64 * kJoinWaves) void kv_attention_join_kernel(Atte
 // half-precision fragments.  Wavefronts in their products go before those that make weights.  4096 queries over themselves, 32
 // heads of 128 channels: 173 us, 0.79 P a second; bound by the vector ALU, 170 instructions and 16 exponentials for 16 x 64
 // scores, which eight wavefronts between two barriers overlap only in part with the products.
+// The largest weight is raised to 2^7 and may grow to 2^15, near the end of half precision: so it has 11 bits for weights
+// down to 2^-21 of the largest, and steps of 2^-31 of it below.
 constexpr int kGroup = 8;
+constexpr float kRaised = 7, kHighest = 15;      // exponents
 typedef _Float16 v8h __attribute__((ext_vector_type(8)));
 typedef _Float16 v2h __attribute__((ext_vector_type(2)));
 
@@ -530,7 +533,7 @@ __global__ __launch_bounds__(64 * kGroup, NK <= 4 ? 4 : 2) void kv_attention_man
         __syncthreads();
         if (idle || t0 > at_hi || t0 >= end || (a.window && t0 + 63 <= at_lo - a.window && t0 >= a.sinks)) continue;
         const bool edge = t0 + 63 > at_lo || t0 + 64 > end || (a.window && t0 <= at_hi - a.window);
-        const float log_v = __builtin_amdgcn_logf(now_v), unit_l = 1.0f / now_v;
+        const float log_v = __builtin_amdgcn_logf(now_v), unit_l = __builtin_amdgcn_exp2f(-kRaised) / now_v;
         __builtin_amdgcn_s_setprio(1);
         v4f acc[4];
 #pragma unroll
@@ -574,10 +577,11 @@ __global__ __launch_bounds__(64 * kGroup, NK <= 4 ? 4 : 2) void kv_attention_man
         if (__any(most > limit)) {
             most = fmaxf(most, __shfl_xor(most, 16));
             most = fmaxf(most, __shfl_xor(most, 32));
-            if (most > limit || most > 0) {
+            if (most > limit || most > kRaised) {
+                most -= kRaised;
                 const float was = limit == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(-most);          // nothing yet with the first base
                 base += most;
-                limit = 8;
+                limit = kHighest;
                 sum *= was;
 #pragma unroll
                 for (int j = 0; j < NV; ++j) o[j] *= was;
@@ -612,6 +616,8 @@ __global__ __launch_bounds__(64 * kGroup, NK <= 4 ? 4 : 2) void kv_attention_man
     all += __shfl_xor(all, 16);
     all += __shfl_xor(all, 32);
     const float f = bad ? __builtin_nanf("") : all > 0 ? 1.0f / all : 0.0f;
+    // the sum is that of weights with a largest of 1: its reciprocal stays a normal number
+    auto lowered = [](float x) __attribute__((always_inline)) { return x * __builtin_amdgcn_exp2f(-kRaised); };
     const int c = c0 + col;
     if (c > c1) return;
     const long row = s.start + c / a.group;
@@ -626,14 +632,14 @@ __global__ __launch_bounds__(64 * kGroup, NK <= 4 ? 4 : 2) void kv_attention_man
                     E e[4];
                 } quad;
 #pragma unroll
-                for (int r = 0; r < 4; ++r) quad.e[r] = from_float<decltype(type)::value>(o[j][r] * f, a.out.unit, a.out.p);
+                for (int r = 0; r < 4; ++r) quad.e[r] = from_float<decltype(type)::value>(lowered(o[j][r]) * f, a.out.unit, a.out.p);
                 *(Quad *)((E *)a.out.data + row * a.out.stride + column + j * 16) = quad;
             };
             by_type(a.out.type, store);
         } else {
 #pragma unroll
             for (int r = 0; r < 4; ++r)
-                if (d + r < kv.dim) store_any(a.out, row, column + j * 16 + r, o[j][r] * f);
+                if (d + r < kv.dim) store_any(a.out, row, column + j * 16 + r, lowered(o[j][r]) * f);
         }
     }
 }

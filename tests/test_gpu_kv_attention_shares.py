@@ -41,8 +41,9 @@ def _case(ctx, new, lens, heads, group, dim, kind, out, share, spread, seed):
     return c, scale
 
 
-def _check(c, out, rows, of_block):
-    """of_block: the largest error of a weight as a share of the largest weight in its block of 64 keys"""
+def _check(c, out, rows, of_block, halves=False):
+    """of_block: the largest error of a weight as a share of the largest weight in its block of 64 keys; halves: weights times
+    their block's scale of values in half precision instead, with steps of 2^-31 of the largest at the most where they are small."""
     got, q, scales = _plain(out), _plain(c.q), c.cache.scales.cpu().double().numpy()
     eps = ref.UNIT_ROUNDOFF.get(str(out.dtype).replace("torch.", ""), 0)
     tiny = UNIT / 2 if c.out_kind == "residue" else 2.0 ** -24
@@ -59,8 +60,12 @@ def _check(c, out, rows, of_block):
             # exponents and sums in 32 bits, of the numerator and of the weights' sum
             slack = 2.0 ** -20 * (np.abs(s) + c.scale * (np.abs(k) @ np.abs(x)) + np.abs(s).max() + 1)
             bound = (2 * np.expm1(slack.max()) + 2.0 ** -18) * mean
-            edges = np.arange(0, n, 64)
-            bound += of_block * (np.maximum.reduceat(w, edges)[:, None] * np.add.reduceat(np.abs(v), edges)).sum(0) / w.sum()
+            if halves:
+                of_scale = np.repeat(scales[pages, head, 1], 64)[:n]
+                bound += 2.0 ** -11 * mean + n * 127 * 2.0 ** -32 * (w * of_scale).max() / w.sum()
+            else:
+                edges = np.arange(0, n, 64)
+                bound += of_block * (np.maximum.reduceat(w, edges)[:, None] * np.add.reduceat(np.abs(v), edges)).sum(0) / w.sum()
             bound += eps * (np.abs(want) + bound) + tiny
             if n > 64:
                 assert (bound < 0.03 * np.abs(want)).all() or c.out_kind == "residue"          # nothing, or half, would not do
@@ -82,3 +87,16 @@ def test_a_first_token_without_a_value(ctx, shape, share, spread, kind, out):
     c, scale = _case(ctx, new, lens, heads, group, 64, kind, out, share, spread, seed=shape)
     rows = {(0, 0), (0, new[0] - 1), (len(new) - 1, new[-1] - 1)}
     _check(c, c.run(scale=scale), rows, 2.0 ** -32)
+
+
+# prompts long enough for weights in half precision: few keys, or many groups of queries
+PROMPTS = [([150, 40], [1000, 700], 16, 4), ([260, 200], [8192, 6000], 16, 8)]
+
+
+@pytest.mark.parametrize("kind,out", [("f16", "f16"), ("bf16", "bf16"), ("f16", "bf16")])
+@pytest.mark.parametrize("share,spread", [(0.9, 0), (0.98, 0), (0.98, 1), (0.995, 0), (0.998, 0)])
+@pytest.mark.parametrize("shape", range(len(PROMPTS)))
+def test_a_first_token_without_a_value_in_prompts(ctx, shape, share, spread, kind, out):
+    new, lens, heads, group = PROMPTS[shape]
+    c, scale = _case(ctx, new, lens, heads, group, 64, kind, out, share, spread, seed=10 + shape)
+    _check(c, c.run(scale=scale), {(0, 0), (0, new[0] - 1), (1, new[1] - 1)}, None, halves=True)
