@@ -528,7 +528,8 @@ __global__ __launch_bounds__(64 * kGroup, NK <= 4 ? 4 : 2) void kv_attention_man
             }
         }
         const int block = s.block(u), t0 = block * kKvBlock, end = page < 0 ? 0 : kv.max_len;
-        const float now_k = scale_k, now_v = page < 0 ? 1.0f : fmaxf(scale_v, 0x1p-100f);
+        // Values of nothing get a scale that is small, but does not take their weights, which count in the sum, out of 32 bits.
+        const float now_k = scale_k, now_v = page < 0 ? 1.0f : scale_v >= 0x1p-100f ? scale_v : 0x1p-64f;
         if (u + 1 < s.total) fetch(u + 1);
         __syncthreads();
         if (idle || t0 > at_hi || t0 >= end || (a.window && t0 + 63 <= at_lo - a.window && t0 >= a.sinks)) continue;

@@ -100,3 +100,17 @@ def test_a_first_token_without_a_value_in_prompts(ctx, shape, share, spread, kin
     new, lens, heads, group = PROMPTS[shape]
     c, scale = _case(ctx, new, lens, heads, group, 64, kind, out, share, spread, seed=10 + shape)
     _check(c, c.run(scale=scale), {(0, 0), (0, new[0] - 1), (1, new[1] - 1)}, None, halves=True)
+
+
+@pytest.mark.parametrize("new", [1, 150])
+@pytest.mark.parametrize("large", [1.0, 2.0 ** 20, 2.0 ** 50])
+def test_blocks_of_zeros_beside_large_values(ctx, new, large):
+    """Every second block holds nothing but zeros: its keys count in the weights' sum whatever the others' values are."""
+    c, scale = _case(ctx, [new], [640], 32, 4, 64, "bf16", "bf16", 0.5, 0, seed=40)
+    c.cache.scales[..., 1] *= large
+    zero = c.table[0, ::2].long()
+    c.cache.scales[zero.cuda(), :, 1] = 0
+    _check(c, c.run(scale=0.0), {(0, 0), (0, new - 1)}, 2.0 ** -32, halves=new > 1)
+    c.cache.codes.view(c.cache.codes.shape[0], c.heads, -1)[zero.cuda(), :, ref.head_bytes(64) // 2:] = 0
+    c.v[zero.numpy()] = 0
+    _check(c, c.run(scale=scale), {(0, 0), (0, new - 1)}, 2.0 ** -32, halves=new > 1)
