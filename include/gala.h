@@ -439,7 +439,7 @@ int gala_kv_attention(const gala_ctx *ctx, void *stream, const gala_kv_cache *ca
                       int heads_q, float scale, int window, int sinks, const gala_values *q, const gala_values *out,
                       void *workspace, size_t workspace_bytes);
 
-/* One token a row from `rows` rows of `vocab` <= 2^30 logits and uniform numbers u in [0, 1).  Order: larger logits first, of
+/* One token a row from `rows` rows of `vocab` < 2^24 logits and uniform numbers u in [0, 1).  Order: larger logits first, of
  * equal ones the lower index first.  A token's weight is exp((z - largest) * (1 / temperature)) in 32 bits, taken
  * down to a whole multiple of 2^-40, so that sums are exact and in any order the same.  Kept are
  *   top-k: the first top_k tokens (0 or less: all);

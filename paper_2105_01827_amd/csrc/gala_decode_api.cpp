@@ -12,6 +12,7 @@ using namespace gala;
 namespace {
 
 constexpr int kFarthest = 1 << 30;      // no sequence is longer: distances beyond it are cut to it
+constexpr int kMostTokens = (1 << 24) - 1;      // of a vocabulary: that many weights of 2^40 add up in 64 bits
 constexpr double kTwoPi = 6.283185307179586476925286766559;
 
 size_t type_size(int type) { return type == GALA_F32 ? 4 : type == GALA_RESIDUE ? 8 : 2; }
@@ -148,12 +149,12 @@ extern "C" int gala_kv_attention(const gala_ctx *c, void *stream, const gala_kv_
 }
 
 extern "C" size_t gala_sample_workspace(int rows, int vocab) {
-    return rows < 0 || vocab < 1 || vocab > (1 << 30) ? 0 : sample_workspace(rows, vocab);
+    return rows < 0 || vocab < 1 || vocab > kMostTokens ? 0 : sample_workspace(rows, vocab);
 }
 
 extern "C" int gala_sample(const gala_ctx *c, void *stream, const gala_values *logits, int rows, int vocab,
                            const gala_sampling *how, int32_t *tokens, void *workspace, size_t workspace_bytes) {
-    if (!c || rows < 0 || vocab < 1 || vocab > (1 << 30) || !values_ok(logits, vocab, false) || !how || !how->u || !tokens) return GALA_EARG;
+    if (!c || rows < 0 || vocab < 1 || vocab > kMostTokens || !values_ok(logits, vocab, false) || !how || !how->u || !tokens) return GALA_EARG;
     const size_t need = sample_workspace(rows, vocab);
     if (need && (!workspace || (uintptr_t)workspace % 16)) return GALA_EARG;
     if (workspace_bytes < need) return GALA_ENOMEM;

@@ -15,7 +15,7 @@ using namespace gala;
 //   bins    counts and weights of the bins, where the row has a top-k or top-p;
 //   gather  of every chunk, the weight of the tokens that are kept for sure, and a list of those in the cut's bin;
 //   draw    the cut within its bin, the chunk that the uniform number falls into, and the token in it.
-// Weights are whole numbers, so the sums do not depend on who adds what first.
+// Weights are whole numbers, at most 2^40 each of less than 2^24, so the sums do not depend on who adds what first.
 // Many long rows are bound by HBM (256 of 131072 residues: 268 MB read twice in 105 us of 113), fewer by the vector ALU (64 of
 // 100003 with top-p: 44 instructions a logit in `bins`, 12.7 of 36.7 us), one row by its four launches (2.9, 4.6, 6.0
 // and 10.0 us for 32000 logits).
@@ -550,6 +550,7 @@ __global__ __launch_bounds__(kDrawThreads) void sample_draw_kernel(Sample a) {
     // the chunk, then the token
     u64 sum = 0;
     for (int i = tid; i < a.chunks; i += kDrawThreads) sum += chunk_mass[i];
+    if (tid == 0) found = 0, found_mass = 0;
     const u64 all = sum_of(sum);
     const double drawn = (double)u * (double)all;
     u64 target = drawn > 0 ? min((u64)drawn, all - 1) : 0;
