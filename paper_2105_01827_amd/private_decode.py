@@ -4,11 +4,14 @@ The server holds the weights and evaluates every linear layer on ciphertexts (``
 activations and the cache, and runs what lies between two linear layers on the values that its share and the server's add
 up to: positions, the paged 8-bit cache, attention and the choice of the next token.  Both ends run in this process, on
 one device.  Weights are random, as small whole numbers; activations travel as fixed-point numbers modulo p.
+What hides one end's numbers from the other -- keys, encryption, the server's shares and masks -- is drawn afresh from the
+system's random source at every use, whatever the model's seed.
 
 One decoder block, several sequences at once: prompts of different lengths first, then token by token.
 """
 import argparse
 import dataclasses
+import secrets
 
 import numpy as np
 import torch
@@ -29,37 +32,41 @@ class Shape:
     unit_w: float = 2.0 ** -6        # ... and of a weight
 
 
+def _fresh(*shape):
+    """64-bit words that nobody else knows"""
+    return np.frombuffer(secrets.token_bytes(8 * int(np.prod(shape))), np.uint64).reshape(shape).copy()
+
+
 class Linear:
     """y = W x on ciphertexts, or (private=False) in the clear by the same whole numbers: both give the same residues."""
 
-    def __init__(self, ctx, keys, weights, seed, private):
-        self.ctx, self.sk, self.seed, self.private = ctx, keys, seed, private
+    def __init__(self, ctx, keys, weights, private):
+        self.ctx, self.sk, self.private = ctx, keys, private
         self.n_o, self.n_i = weights.shape
         residues = (weights % wl.P).astype(np.uint64)
         if private:
             self.plan = ctx.fc_plan(residues)
-            self.plan.bind(ctx.galois_keygen(keys, self.plan.rotations(), seed=seed))
+            self.plan.bind(ctx.galois_keygen(keys, self.plan.rotations(), seed=secrets.randbits(64)))
             # where a packed input keeps what: slot -> 1 + index of the input, 0 for none
             self.places = devmem.to_dev(self.plan.pack_input(np.arange(1, self.n_i + 1, dtype=np.uint64)))
         self.weights = torch.from_numpy(weights.astype(np.float64)).cuda()
-        self.calls = 0
 
     def __call__(self, x):
         """x (rows, n_i) residues -> (rows, n_o) residues"""
         rows, n = x.shape[0], self.ctx.n
-        self.calls += 1
         if not self.private:
             centred = torch.where(x > wl.P // 2, x - wl.P, x).double()
             return (centred @ self.weights.t()).to(torch.int64).remainder(wl.P)
-        # client: copies into slots, encryption
+        # client: copies into slots, encryption with randomness of its own for each row
         slots = torch.nn.functional.pad(x, (1, 0))[:, self.places].contiguous()
-        seeds = torch.arange(rows, dtype=torch.int64, device="cuda") + (self.seed << 32) + (self.calls << 16)
+        seeds = devmem.to_dev(_fresh(rows))
         ct, out = devmem.dev_empty(rows * 2 * n), devmem.dev_empty(rows * 2 * n)
         self.ctx.encrypt_batch(self.sk, slots, seeds, rows, ct)
-        # server: the layer, masked by its share
-        r = torch.randint(0, wl.P, (rows, self.n_o), dtype=torch.int64, device="cuda")
+        # server: the layer, masked by its share, and the other slots by masks from a seed that the client does not know: without
+        # them they hold partial inner products of the weights
+        r = devmem.to_dev(_fresh(rows, self.n_o) % np.uint64(wl.P))
         need = self.plan.workspace_bytes(rows)
-        self.plan.he_fc(ct, rows, r, self.calls, out, torch.empty(need, dtype=torch.uint8, device="cuda"), need)
+        self.plan.he_fc(ct, rows, r, secrets.randbits(64), out, torch.empty(need, dtype=torch.uint8, device="cuda"), need)
         # client: its share, and the server's
         share = torch.empty(rows, self.n_o, dtype=torch.int64, device="cuda")
         self.ctx.decrypt_batch(self.sk, out, rows, slots)
@@ -73,14 +80,14 @@ class Model:
         par = wl.DEFAULT
         self.ctx = binding.Context(par.n, par.q, par.p, par.gadget_bits)
         rng = np.random.default_rng(seed)
-        keys = self.ctx.keygen(seed) if private else None
+        keys = self.ctx.keygen(secrets.randbits(64)) if private else None
         qkv = (s.heads + 2 * s.heads_kv) * s.head_dim
 
-        def linear(n_o, n_i, k):
-            return Linear(self.ctx, keys, rng.integers(-15, 16, (n_o, n_i)), seed + k, private)
+        def linear(n_o, n_i):
+            return Linear(self.ctx, keys, rng.integers(-15, 16, (n_o, n_i)), private)
 
         self.embedding = torch.from_numpy(rng.standard_normal((s.vocab, s.width))).float().cuda()
-        self.qkv, self.merge, self.head = linear(qkv, s.width, 1), linear(s.width, s.heads * s.head_dim, 2), linear(s.vocab, s.width, 3)
+        self.qkv, self.merge, self.head = linear(qkv, s.width), linear(s.width, s.heads * s.head_dim), linear(s.vocab, s.width)
         self.blocks = 4
         self.cache = binding.KvCache(self.ctx, s.heads_kv, s.head_dim, pages=s.batch * self.blocks)
         # pages in any order
