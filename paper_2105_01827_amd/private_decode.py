@@ -28,6 +28,7 @@ class Shape:
     head_dim: int = 32
     batch: int = 3
     steps: int = 6
+    context: int = 256               # tokens that a sequence may have, its answer's included
     unit_x: float = 2.0 ** -5        # what one unit of an activation stands for
     unit_w: float = 2.0 ** -6        # ... and of a weight
 
@@ -88,7 +89,7 @@ class Model:
 
         self.embedding = torch.from_numpy(rng.standard_normal((s.vocab, s.width))).float().cuda()
         self.qkv, self.merge, self.head = linear(qkv, s.width), linear(s.width, s.heads * s.head_dim), linear(s.vocab, s.width)
-        self.blocks = 4
+        self.blocks = -(-s.context // 64)
         self.cache = binding.KvCache(self.ctx, s.heads_kv, s.head_dim, pages=s.batch * self.blocks)
         # pages in any order
         self.table = torch.from_numpy(rng.permutation(s.batch * self.blocks).astype(np.int32).reshape(s.batch, self.blocks)).cuda()
@@ -105,6 +106,8 @@ class Model:
     def step(self, tokens, counts):
         """`tokens`: new ones of all sequences, counts[b] of sequence b; returns the logits after each sequence's last, as residues"""
         s, unit = self.shape, self.shape.unit_x * self.shape.unit_w
+        if max(a + b for a, b in zip(self.lens, counts)) > s.context:
+            raise ValueError(f"a sequence has room for {s.context} tokens")
         self.lens = [a + b for a, b in zip(self.lens, counts)]
         starts = torch.tensor([0] + list(np.cumsum(counts)), dtype=torch.int32, device="cuda")
         batch = binding.KvBatch(starts, torch.tensor(self.lens, dtype=torch.int32, device="cuda"), self.table, max(counts), max(self.lens))
@@ -123,8 +126,12 @@ class Model:
         return self.head(self.residues(self.norm(x[(starts[1:] - 1).long()])))
 
     def answer(self, prompts, temperature=0.8, top_k=40, top_p=0.95, seed=0):
-        """Prompts (lists of tokens) -> the tokens that follow, (steps, batch)"""
+        """Prompts (lists of tokens) -> the tokens that follow, (steps, batch); sequences begin anew"""
         s, rows = self.shape, len(prompts)
+        # the last token drawn needs no place
+        if max(map(len, prompts)) + s.steps - 1 > s.context:
+            raise ValueError(f"a sequence has room for {s.context} tokens, its answer's included")
+        self.lens = [0] * s.batch
         gen = torch.Generator().manual_seed(seed)
         need = self.ctx.sample_workspace_bytes(rows, s.vocab)
         workspace = torch.empty(max(need, 16), dtype=torch.uint8, device="cuda")
@@ -152,6 +159,7 @@ def main():
     a = ap.parse_args()
     shape = Shape(steps=a.steps, batch=a.batch)
     prompts = prompts_for(shape)
+    shape = dataclasses.replace(shape, context=max(map(len, prompts)) + shape.steps)
     for private in (True, False):
         answer = Model(shape, private=private).answer(prompts)
         for b, p in enumerate(prompts):
