@@ -106,6 +106,8 @@ class Model:
     def step(self, tokens, counts):
         """`tokens`: new ones of all sequences, counts[b] of sequence b; returns the logits after each sequence's last, as residues"""
         s, unit = self.shape, self.shape.unit_x * self.shape.unit_w
+        if min(counts) < 1:
+            raise ValueError("logits come after a sequence's last new token: each has to bring one")
         if max(a + b for a, b in zip(self.lens, counts)) > s.context:
             raise ValueError(f"a sequence has room for {s.context} tokens")
         self.lens = [a + b for a, b in zip(self.lens, counts)]

@@ -32,3 +32,11 @@ def test_as_long_as_the_context():
     model = pd.Model(pd.Shape(batch=1, steps=3, context=300), private=False)
     logits = model.step(torch.arange(300, device="cuda"), [300])
     assert model.blocks == 5 and int(logits.unique().numel()) > 100
+
+
+def test_a_sequence_without_new_tokens():
+    """There is no last token of its own whose logits it could get."""
+    model = pd.Model(pd.Shape(batch=2, steps=1), private=False)
+    with pytest.raises(ValueError):
+        model.answer([[1, 2], []])
+    assert model.lens == [0, 0]
