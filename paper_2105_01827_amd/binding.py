@@ -202,10 +202,6 @@ def _dev(t):
     return C.c_void_p(t if isinstance(t, int) else t.data_ptr())
 
 
-def _at(t):
-    return t if isinstance(t, int) else t.data_ptr()
-
-
 def _stream(s):
     if s is None:
         return None
@@ -234,6 +230,35 @@ def _values(t, unit):
                 raise ValueError("the values of a row have to be contiguous")
             step *= t.size(i)
     return _pack_values(t.data_ptr(), strides[0], kind, unit)
+
+
+def _on_gpu(t, what):
+    if not t.is_cuda:
+        raise TypeError(f"{what} has to be on the GPU")
+
+
+def _heads_values(t, heads, head_dim, unit, what):
+    """(gala_values, rows, heads) of a tensor on the GPU whose rows hold `heads` (0: any number of) x head_dim numbers"""
+    shape, strides, kind = t.shape, t.stride(), _types.get(t.dtype)
+    if len(shape) == 3 and shape[2] == head_dim and (shape[1] == heads or not heads) and strides[2] == 1 and strides[1] == head_dim \
+            and kind is not None and t.is_cuda:                               # as they mostly are
+        return _pack_values(t.data_ptr(), strides[0], kind, unit), shape[0], shape[1]
+    numbers = math.prod(shape[1:])
+    if numbers % head_dim or (heads and numbers != heads * head_dim):
+        raise ValueError(f"a row of {what} has to hold {heads or 'heads'} x {head_dim} values, not {tuple(shape[1:])}")
+    values = _values(t, unit)
+    _on_gpu(t, what)
+    return values, shape[0], numbers // head_dim
+
+
+def _scratch(t, size):
+    """Address of a workspace of `size` bytes: a tensor, or an address"""
+    if isinstance(t, int):
+        return t
+    if t.nbytes < size:
+        raise ValueError(f"the workspace has {t.nbytes} bytes, not {size}")
+    _on_gpu(t, "the workspace")
+    return t.data_ptr()
 
 
 def _words(t, dtype, what):
@@ -432,10 +457,12 @@ class Context:
         at = [self._per_row(t, rows, "torch.float32", name) for t, name in
               ((temperature, "temperature"), (top_p, "top_p"), (min_p, "min_p"), (u, "u"))]
         top_k = self._per_row(top_k, rows, "torch.int32", "top_k")
-        _check(self.lib.gala_sample(self.h, _stream(stream), _values(logits, unit), rows, vocab,
+        values = _values(logits, unit)
+        _on_gpu(logits, "logits")
+        _check(self.lib.gala_sample(self.h, _stream(stream), values, rows, vocab,
                                     _pack_sampling(at[0], top_k, at[1], at[2], at[3]),
-                                    self._per_row(tokens, rows, "torch.int32", "tokens"), _at(workspace), workspace_bytes),
-               "gala_sample")
+                                    self._per_row(tokens, rows, "torch.int32", "tokens"), _scratch(workspace, workspace_bytes),
+                                    workspace_bytes), "gala_sample")
 
     @staticmethod
     def _per_row(t, rows, dtype, name):
@@ -443,7 +470,9 @@ class Context:
             return 0
         if t.numel() != rows:
             raise ValueError(f"{name} has to have one number a row")
-        return _words(t, dtype, name)
+        at = _words(t, dtype, name)
+        _on_gpu(t, name)
+        return at
 
 
 class SecretKey:
@@ -670,6 +699,9 @@ class Rope:
 
     def __init__(self, table, interleaved=False):
         self.table = table
+        if table.dim() != 3 or table.shape[2] != 2:
+            raise ValueError("the table holds a cosine and a sine for each position and pair")
+        _on_gpu(table, "the table")
         self.arg = RopeArg(_words(table, "torch.float32", "the table"), table.shape[0], 2 * table.shape[1], int(interleaved), 0)
         self.ref = C.byref(self.arg)
 
@@ -683,6 +715,8 @@ class KvBatch:
             raise ValueError("starts has one entry more than lens, and the table a row for each of them")
         self.arg = KvBatchArg(lens.numel(), max_new, max_len, table.shape[1], _words(starts, "torch.int32", "starts"),
                               _words(lens, "torch.int32", "lens"), _words(table, "torch.int32", "the table"))
+        for t, what in ((starts, "starts"), (lens, "lens"), (table, "the table")):
+            _on_gpu(t, what)
         self.ref = C.byref(self.arg)
 
 
@@ -702,31 +736,52 @@ class KvCache:
         self._lib, self._ctx = ctx.lib, ctx.h
         self.arg = KvCacheArg(heads, head_dim, codes.shape[0], 0, _words(codes, "torch.int8", "codes"),
                               _words(scales, "torch.float32", "scales"))
+        _on_gpu(codes, "codes")
+        _on_gpu(scales, "scales")
         self.ref = C.byref(self.arg)
 
     @staticmethod
     def page_bytes(heads, head_dim):
         return int(load().gala_kv_cache_bytes(1, heads, head_dim))
 
-    def _heads(self, q):
-        return q.size(1) if q.dim() == 3 else math.prod(q.shape[1:]) // self.head_dim
+    def _kv_values(self, k, v, unit, names):
+        """gala_values of keys and of values, which come together or not at all"""
+        k, rows, _ = _heads_values(k, self.heads, self.head_dim, unit, names[0])
+        v, others, _ = _heads_values(v, self.heads, self.head_dim, unit, names[1])
+        if rows != others:
+            raise ValueError(f"{names[0]} has {rows} rows, {names[1]} {others}")
+        return k, v
+
+    def _q_values(self, q, out, unit, name):
+        """gala_values of queries and of what becomes of them, and their heads"""
+        q, rows, heads = _heads_values(q, 0, self.head_dim, unit, "q")
+        out, others, _ = _heads_values(out, heads, self.head_dim, unit, name)
+        if others < rows:
+            raise ValueError(f"{name} has {others} rows for {rows}")
+        return q, out, heads
 
     def append(self, batch, k, v, q=None, q_out=None, rope=None, unit=1.0, stream=None):
         """k, v (rows, heads, head_dim) into the cache; q (rows, heads_q, head_dim) rotated into q_out."""
+        if (k is None) != (v is None) or (q is None) != (q_out is None):
+            raise ValueError("k comes with v, and q with q_out")
+        heads_q = 0
+        if k is not None:
+            k, v = self._kv_values(k, v, unit, ("k", "v"))
+        if q is not None:
+            q, q_out, heads_q = self._q_values(q, q_out, unit, "q_out")
         _check(self._lib.gala_kv_append(self._ctx, _stream(stream), self.ref, batch.ref, None if rope is None else rope.ref,
-                                           0 if q is None else self._heads(q), None if q is None else _values(q, unit),
-                                           None if q_out is None else _values(q_out, unit), None if k is None else _values(k, unit),
-                                           None if v is None else _values(v, unit)), "gala_kv_append")
+                                        heads_q, q, q_out, k, v), "gala_kv_append")
 
     def export(self, batch, k_out, v_out, unit=1.0, stream=None):
-        _check(self._lib.gala_kv_export(self._ctx, _stream(stream), self.ref, batch.ref, _values(k_out, unit),
-                                           _values(v_out, unit)), "gala_kv_export")
+        k_out, v_out = self._kv_values(k_out, v_out, unit, ("k_out", "v_out"))
+        _check(self._lib.gala_kv_export(self._ctx, _stream(stream), self.ref, batch.ref, k_out, v_out), "gala_kv_export")
 
     def attention_workspace_bytes(self, batch, heads_q, window=0, sinks=0):
         return int(self._lib.gala_kv_attention_workspace(self.ref, batch.ref, heads_q, window, sinks))
 
     def attention(self, batch, q, out, scale, workspace, workspace_bytes, window=0, sinks=0, unit=1.0, stream=None):
         """q (rows, heads_q, head_dim) -> out of the same shape."""
-        _check(self._lib.gala_kv_attention(self._ctx, _stream(stream), self.ref, batch.ref, self._heads(q), scale, window, sinks,
-                                              _values(q, unit), _values(out, unit), _at(workspace), workspace_bytes),
-               "gala_kv_attention")
+        q, out, heads_q = self._q_values(q, out, unit, "out")
+        workspace = _scratch(workspace, workspace_bytes)
+        _check(self._lib.gala_kv_attention(self._ctx, _stream(stream), self.ref, batch.ref, heads_q, scale, window, sinks, q, out,
+                                           workspace, workspace_bytes), "gala_kv_attention")
