@@ -428,9 +428,10 @@ int gala_kv_export(const gala_ctx *ctx, void *stream, const gala_kv_cache *cache
  * 0, one that holds a NaN or an infinity gives NaN (its own heads' rows alone).  q, out: rows of heads_q x head_dim,
  * heads_q a multiple of the cache's heads; query head h reads head h / (heads_q / heads); out may be q where the
  * types agree.  Operands of the products, sums in 32 bits: queries enter as whole numbers of 16 bits of their row's
- * largest, of 24 where q or out is GALA_F32 or GALA_RESIDUE; weights as 31 bits of the largest in their block; except that
- * where neither is, and a sequence brings 128 queries or more for a head of the cache, weights may enter in half precision
- * (11 bits, in steps of 2^-31 of the largest so far at the most where they are small), multiplied by their block's scale of values.
+ * largest, of 24 where q or out is GALA_F32 or GALA_RESIDUE; weights as 31 bits of the largest in their block.  Where
+ * neither is, and max_new * heads_q / heads is 128 or more, the weights of all the call's sequences, those with one new token
+ * too, may enter in half precision instead: 11 bits, in steps of 2^-31 of the largest so far at the most where they are
+ * small, multiplied by their block's scale of values.  So max_new is best no more than the sequences bring.
  * workspace: device scratch, caller-owned, 16-byte aligned, of gala_kv_attention_workspace bytes (0 for bad arguments and
  * where none is needed; it may be NULL then); calls that overlap need one each.  Asynchronous, allocates nothing; results do not depend on timing.  Errors: GALA_EARG, GALA_ENOMEM (workspace too small), GALA_EHIP. */
 size_t gala_kv_attention_workspace(const gala_kv_cache *cache, const gala_kv_batch *batch, int heads_q, int window,

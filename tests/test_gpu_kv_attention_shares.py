@@ -114,3 +114,16 @@ def test_blocks_of_zeros_beside_large_values(ctx, new, large):
     c.cache.codes.view(c.cache.codes.shape[0], c.heads, -1)[zero.cuda(), :, ref.head_bytes(64) // 2:] = 0
     c.v[zero.numpy()] = 0
     _check(c, c.run(scale=scale), {(0, 0), (0, new - 1)}, 2.0 ** -32, halves=new > 1)
+
+
+def test_long_prompts_as_exact_sums(ctx):
+    """Few groups of queries over many keys: weights are not in half precision there, whatever the types."""
+    for kind in ("f16", "bf16"):
+        c, scale = _case(ctx, [600, 450], [600, 1300], 1, 4, 128, kind, kind, 0.98, 1, seed=50)
+        _check(c, c.run(scale=scale), {(0, i) for i in (0, 15, 16, 63, 64, 255, 256, 599)} | {(1, i) for i in (0, 31, 32, 449)}, 2.0 ** -32)
+
+
+def test_a_token_beside_a_prompt(ctx):
+    """The call's bound on new tokens decides for all of its sequences: one token is worked out as the prompt's are."""
+    c, scale = _case(ctx, [150, 1, 1], [1000, 900, 70], 16, 4, 64, "f16", "f16", 0.98, 0, seed=51)
+    _check(c, c.run(scale=scale), {(0, 149), (1, 0), (2, 0)}, None, halves=True)
