@@ -761,7 +761,8 @@ class KvCache:
         return q, out, heads
 
     def append(self, batch, k, v, q=None, q_out=None, rope=None, unit=1.0, stream=None):
-        """k, v (rows, heads, head_dim) into the cache; q (rows, heads_q, head_dim) rotated into q_out."""
+        """k, v (rows, heads, head_dim) into the cache; q (rows, heads_q, head_dim) rotated into q_out.  ``unit``: what one unit
+        of a residue stands for, in all of them."""
         if (k is None) != (v is None) or (q is None) != (q_out is None):
             raise ValueError("k comes with v, and q with q_out")
         heads_q = 0
@@ -780,7 +781,7 @@ class KvCache:
         return int(self._lib.gala_kv_attention_workspace(self.ref, batch.ref, heads_q, window, sinks))
 
     def attention(self, batch, q, out, scale, workspace, workspace_bytes, window=0, sinks=0, unit=1.0, stream=None):
-        """q (rows, heads_q, head_dim) -> out of the same shape."""
+        """q (rows, heads_q, head_dim) -> out of the same shape; ``unit`` is that of residues in either, the same for both."""
         q, out, heads_q = self._q_values(q, out, unit, "out")
         workspace = _scratch(workspace, workspace_bytes)
         _check(self._lib.gala_kv_attention(self._ctx, _stream(stream), self.ref, batch.ref, heads_q, scale, window, sinks, q, out,

@@ -137,7 +137,8 @@ __device__ __forceinline__ float joined(const v4i (&acc)[ND], int r) {
 }
 
 // A lane's part of a query, 16 channels of each 64, as digits; returns what a unit of them is worth in exponents of 2,
-// with the scale.  `bad`: the query holds a NaN or an infinity; its digits are 0 then.
+// with the scale.  `bad`: the query holds a NaN or an infinity; its digits are 0 then.  Two digits round each channel by 2^-16
+// of the row's largest, at most a sixteenth of what f16 itself may round that largest by, and less of bf16; three by 2^-24.
 template <int NC, int ND>
 __device__ __forceinline__ float digits_of(const float (&x)[NC][16], float scale, v4i (&qd)[NC][ND], bool &bad) {
     float most = 0;
@@ -182,8 +183,8 @@ __device__ __forceinline__ float digits_of(const float (&x)[NC][16], float scale
 // for the largest score.  A wavefront has blocks of its own; a workgroup's wavefronts are joined at the end.
 // A weight has four digits, 31 bits of the largest in its block: with the two that a query of 16 bits has, thousands of keys that share
 // what one heavy key leaves were rounded away (a quarter of the output where the first token has 0.9 of 8192 keys' weight).
-// One query a sequence is bound by HBM: 64 sequences of 8192 tokens (8 heads of 128 channels, 807 MB) take 157 us, 5.1 TB/s; 151 us
-// with two digits, and 128 queries of 32 heads over 30000 tokens 162 and 124 us.
+// One query a sequence is bound by HBM: 64 sequences of 8192 tokens (8 heads of 128 channels, 807 MB) take 157 us, 5.1 TB/s, the
+// matrix cores busy for 0.1 of it; 151 us with two digits.  128 queries of 32 heads over 30000 tokens take 162 us, 124 with two digits.
 template <int N32, int ND, int kWaves>
 __global__ __launch_bounds__(64 * kWaves, N32 * ND <= 12 ? 2 : 1) void kv_attention_kernel(Attention a) {
     constexpr int NC = (N32 + 1) / 2, NV = 2 * N32;          // products of 64 channels, tiles of 16
@@ -659,7 +660,8 @@ Cut cut_of(const KvArgs &kv, int heads_q, int window, int sinks, bool fine) {
     const long reach = std::min<long>(kv.max_len, (long)kv.table_stride * kKvBlock);
     const long keys = window ? std::min(reach, (long)window + kv.max_new + sinks + 2 * kKvBlock) : reach;
     const long blocks = std::max(1l, (keys + kKvBlock - 1) / kKvBlock);
-    // Whole prompts in half precision, where they fill the card or have few keys: 8 x 128 queries of 32 heads over 4000
+    // The call's bound on new tokens decides for all of its sequences: a token beside a prompt has no others to share its keys with
+    // (a prompt of 2000 and 15 single tokens over 8192 tokens take 1029 us, in two calls 325).  Whole prompts in half precision, where they fill the card or have few keys: 8 x 128 queries of 32 heads over 4000
     // tokens (256 workgroups) take 105 us so and 179 us as exact sums, 4 x 300 over 300 14 and 33 us; but 4 x 128 over
     // 4000 (128 workgroups) 104 and 91 us, because exact sums can share a tile's keys.
     const long groups = (columns + of_group - 1) / of_group * kv.count * kv.heads;
@@ -670,8 +672,8 @@ Cut cut_of(const KvArgs &kv, int heads_q, int window, int sinks, bool fine) {
     }
     c.tiles = (int)((columns + kColumns - 1) / kColumns);
     c.columns = (int)std::min<long>(columns, kColumns);
-    // Workgroups for one round of the card, with 32 blocks at least: 64 sequences of 8192 tokens take 161 us in 512 workgroups,
-    // 191 us in 1024 and 208 us in 4096.
+    // Workgroups for one round of the card, with 32 blocks at least: 64 sequences of 8192 tokens take 157 us in 512 workgroups,
+    // 173 us in 1024 and 177 us in 4096.
     const long units = std::max(1l, (long)kv.count * kv.heads * c.tiles);
     c.splits = (int)std::max(1l, std::min((512 + units - 1) / units, (blocks + 31) / 32));
     return c;
@@ -708,8 +710,8 @@ int launch_kv_attention(void *stream, const KvArgs &kv, int heads_q, float scale
             hipLaunchKernelGGL((kv_attention_many_kernel<N32>), dim3(groups), dim3(64 * kGroup), 2 * (NC + N32) * 4096, (hipStream_t)stream, a);
             return;
         }
-        // A launch that leaves CUs with one workgroup gets eight wavefronts in each: 32 windows of 1024 tokens take 12.0 us with
-        // eight and 14.0 with four; 64 sequences of 500 tokens in 512 workgroups 16.9 and 13.4.
+        // A launch that leaves CUs with one workgroup gets eight wavefronts in each: 32 windows of 1024 tokens take 12.4 us with
+        // eight and 15.0 with four; 64 sequences of 500 tokens in 512 workgroups 18.1 and 14.5.
         auto waves = [&](auto w) {
             constexpr int W = decltype(w)::value;
             a.waves = W;

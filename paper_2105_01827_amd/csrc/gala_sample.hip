@@ -18,7 +18,8 @@ using namespace gala;
 // Weights are whole numbers, at most 2^40 each of less than 2^24, so the sums do not depend on who adds what first.
 // Many long rows are bound by HBM (256 of 131072 residues: 268 MB read twice in 105 us of 113), fewer by the vector ALU (64 of
 // 100003 with top-p: 44 instructions a logit in `bins`, 12.7 of 36.7 us), one row by its four launches (2.9, 4.6, 6.0
-// and 10.0 us for 32000 logits).
+// and 10.0 us for 32000 logits).  A cut among more tokens of a bin than a list holds is searched digit by digit by one workgroup:
+// top-p of 0.95 among 131072 logits of a long tail takes 51 us at temperature 1 and 566 us at 1.3.
 namespace {
 
 constexpr int kThreads = 512, kDrawThreads = 512;
