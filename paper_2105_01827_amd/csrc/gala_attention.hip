@@ -660,10 +660,11 @@ Cut cut_of(const KvArgs &kv, int heads_q, int window, int sinks, bool fine) {
     const long reach = std::min<long>(kv.max_len, (long)kv.table_stride * kKvBlock);
     const long keys = window ? std::min(reach, (long)window + kv.max_new + sinks + 2 * kKvBlock) : reach;
     const long blocks = std::max(1l, (keys + kKvBlock - 1) / kKvBlock);
-    // The call's bound on new tokens decides for all of its sequences: a token beside a prompt has no others to share its keys with
-    // (a prompt of 2000 and 15 single tokens over 8192 tokens take 1029 us, in two calls 325).  Whole prompts in half precision, where they fill the card or have few keys: 8 x 128 queries of 32 heads over 4000
-    // tokens (256 workgroups) take 105 us so and 179 us as exact sums, 4 x 300 over 300 14 and 33 us; but 4 x 128 over
-    // 4000 (128 workgroups) 104 and 91 us, because exact sums can share a tile's keys.
+    // The call's bound on new tokens decides for all of its sequences, and a token beside a prompt then shares its keys with nobody:
+    // a prompt of 2000 and 15 single tokens over 8192 tokens take 1029 us, in two calls 325.  Whole prompts in half precision,
+    // where they fill the card or have few keys: 8 x 128 queries of 32 heads over 4000 tokens (256 workgroups) take 105 us so and
+    // 179 us as exact sums, 4 x 300 over 300 14 and 33 us; but 4 x 128 over 4000 (128 workgroups) 104 and 91 us, because exact
+    // sums can share a tile's keys.
     const long groups = (columns + of_group - 1) / of_group * kv.count * kv.heads;
     c.many = !fine && columns >= of_group && (groups >= 192 || blocks <= 16);
     if (c.many) {
