@@ -440,6 +440,88 @@ int gala_kv_attention(const gala_ctx *ctx, void *stream, const gala_kv_cache *ca
                       int heads_q, float scale, int window, int sinks, const gala_values *q, const gala_values *out,
                       void *workspace, size_t workspace_bytes);
 
+/* The same cache in 4 bits, at 1 / 1.8 of the bytes.  A code is a sign (its bit 3) and one of the magnitudes 0, 1/2, 1, 3/2, 2, 3,
+ * 4, 6 (its bits 0 to 2).  Every 32 channels of a token's key share a power of two: the smallest 2^e, -120 <= e <= 125, of which
+ * the largest magnitude among them is at most 7 times.  A token's value in a head has one bfloat16 scale: max|x| * (1/6)
+ * rounded to it, 0 where that is below 2^-100 (and the value is stored as zeros then).  x is stored as the code nearest
+ * to x / scale, the quotient rounded to 32 bits; ties go to the even code, and what is beyond 6 becomes 6.  Infinities are
+ * stored as +-6 and NaN as 0, and neither counts for the scale.  A token's codes depend on no other token, and no
+ * code changes once it is written.
+ * All memory is the caller's: of each page and head gala_kv4_cache_bytes(1, 1, head_dim) bytes.  With m = ceil(head_dim / 32),
+ * two codes a byte, the first in its low bits, of token t of the page lies
+ *   the key's code of channel d:     in byte ((t/16)*m + d/32)*256 + (t%16)*16 + (d%32)/2, half d%2
+ *   the value's code of channel d:   in byte 1024*m + (d/32)*1024 + ((t%16)/4)*256 + (d%16)*16 + (d%32)/16*8 + (t/32)*4 + (t%32)/16*2 + t%4/2,
+ *                                    half t%2
+ *   e + 127 of channels 32g .. 32g+31 of the key:   in byte 2048*m + g*64 + (t%16)*4 + t/16
+ *   the value's scale (bfloat16):    at byte 2112*m + ((t%16)/4)*32 + (t/16)*8 + (t%4)*2
+ * and channels from head_dim to 32*m hold 0.  Pages, batches, skipped tokens and rows behind a sequence's end are as above. */
+typedef struct {
+    int32_t heads, head_dim;     /* heads of keys and values; 1 <= head_dim <= 256 */
+    int32_t pages;
+    int32_t reserved;            /* 0 */
+    uint8_t *data;               /* pages x heads; 16-byte aligned */
+} gala_kv4_cache;
+size_t gala_kv4_cache_bytes(int pages, int heads, int head_dim);
+/* As gala_kv_append, gala_kv_export, gala_kv_attention_workspace and gala_kv_attention on such a cache, but that a key whose position
+ * the rope table does not have is stored as 0.  Attention: the products are those of the codes with their powers of two,
+ * exact in bfloat16, with queries as they are (in up to three bfloat16 parts, 24 bits), sums in 32 bits; a weight times its
+ * token's scale enters the second product in two bfloat16 parts, 16 bits of itself, in three, 24 bits, where q or out is
+ * GALA_F32 or GALA_RESIDUE. */
+int gala_kv4_append(const gala_ctx *ctx, void *stream, const gala_kv4_cache *cache, const gala_kv_batch *batch,
+                    const gala_rope *rope, int heads_q, const gala_values *q, const gala_values *q_out,
+                    const gala_values *k, const gala_values *v);
+int gala_kv4_export(const gala_ctx *ctx, void *stream, const gala_kv4_cache *cache, const gala_kv_batch *batch,
+                    const gala_values *k_out, const gala_values *v_out);
+size_t gala_kv4_attention_workspace(const gala_kv4_cache *cache, const gala_kv_batch *batch, int heads_q, int window,
+                                    int sinks);
+int gala_kv4_attention(const gala_ctx *ctx, void *stream, const gala_kv4_cache *cache, const gala_kv_batch *batch,
+                       int heads_q, float scale, int window, int sinks, const gala_values *q, const gala_values *out,
+                       void *workspace, size_t workspace_bytes);
+
+/* Rotary positions with several axes, as the tokens of an image or a video have them (time, height, width; a token of text
+ * stands at the same position on all).  Of a head's first rot_dim channels the pair i turns by the angle of its axis: that of
+ * column column[i] of the table's row for the position on axis axis[i].  Pairs and rounding are those of gala_rope.  table
+ * (device memory): (cos, sin), positions x columns of them. */
+typedef struct {
+    const float *table;
+    int32_t positions, columns, rot_dim, interleaved, axes, reserved;        /* 1 <= axes <= 4; reserved 0 */
+    uint8_t axis[128], column[128];
+} gala_rope_axes;
+/* Fills axis, column, columns, rot_dim and axes for `sections`, the pairs of each axis (none may be negative, 1 to 128 together):
+ * GALA_AXES_BLOCKS: the first axis has the first pairs, the next axis the pairs behind them, and column[i] = i; GALA_AXES_TURNS:
+ * the axes take turns as long as they have pairs left, and column[i] = i; GALA_AXES_OWN: as GALA_AXES_BLOCKS, but each axis begins
+ * at column 0, so that all have the fastest angles.  A table of gala_rope_table with rot_dim = 2 * columns fits the first two;
+ * for the last one of rot_dim = 2 * columns too, where all sections are alike. */
+typedef enum { GALA_AXES_BLOCKS = 0, GALA_AXES_TURNS = 1, GALA_AXES_OWN = 2 } gala_axes_order;
+int gala_rope_axes_layout(int axes, const int32_t *sections, int order, gala_rope_axes *out);
+/* x, out: rows of heads x head_dim (queries and keys that lie together in a row are heads of one call); out is not GALA_RESIDUE
+ * and may be x where the types agree.  at (device memory): row i stands at at[i * at_stride + a] on axis a.  A row that has a
+ * position that the table does not have comes out as NaN.  Asynchronous, allocates nothing. */
+int gala_rope_apply(const gala_ctx *ctx, void *stream, const gala_rope_axes *rope, const int32_t *at, int64_t at_stride,
+                    int rows, int heads, int head_dim, const gala_values *x, const gala_values *out);
+
+/* The step in front of a linear layer: s = x + add, y = s * (1 / sqrt(mean(s^2) + epsilon)) * weight over the `width` numbers of
+ * each row, and y in whole numbers of few bits, as a layer on ciphertexts takes its inputs.  Sums of a row are
+ * carried in 64 bits and the factor rounded to 32; x + add, both products and all that follows are 32-bit operations
+ * rounded one by one, so that codes do not depend on the order of a sum.
+ * x, add, out: rows of `width` numbers; add NULL for none.  sum_out: s, rounded to its type (not GALA_RESIDUE), NULL where
+ * it is not wanted; weight: one row (not GALA_RESIDUE), NULL for 1.  sum_out may be x or add, and out may be any of them, where type and stride
+ * agree; out and sum_out may not be the same.
+ * out GALA_F32, GALA_F16, GALA_BF16: y; `scales` is NULL then.  Else whole numbers held to +-limit, as int8_t (GALA_INT8, a type
+ * that only this call takes, limit <= 127) or as residues mod p (limit <= p / 2, below 2^24; 0: p / 2): without scales the
+ * nearest to y / unit, ties to even; with scales (rows x ceil(width / group) floats; group 0: the row) the nearest to y * (1 / scale),
+ * scale = max|y| * (1 / limit) over `group` numbers at a time, infinities and NaN aside.  NaN becomes 0, infinities +-limit (0
+ * where the scale is 0).  What the next layer returns is then worth scale times the unit of its weights: a scale a row stands
+ * outside of the products, one for each group does not.  Asynchronous, allocates nothing. */
+#define GALA_INT8 4
+typedef struct {
+    double epsilon;              /* >= 0 */
+    int32_t limit, group;
+    float *scales;
+} gala_norm;
+int gala_rms_norm(const gala_ctx *ctx, void *stream, const gala_norm *how, int rows, int width, const gala_values *x,
+                  const gala_values *add, const gala_values *sum_out, const gala_values *weight, const gala_values *out);
+
 /* One token a row from `rows` rows of `vocab` < 2^24 logits and uniform numbers u in [0, 1).  Order: larger logits first, of
  * equal ones the lower index first.  A token's weight is exp((z - largest) * (1 / temperature)) in 32 bits, taken
  * down to a whole multiple of 2^-40, so that sums are exact and in any order the same.  Kept are

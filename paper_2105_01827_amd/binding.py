@@ -67,6 +67,15 @@ class RopeArg(C.Structure):
     _fields_ = [("table", C.c_void_p)] + [(k, C.c_int32) for k in ("positions", "rot_dim", "interleaved", "reserved")]
 
 
+class Kv4CacheArg(C.Structure):
+    _fields_ = [(k, C.c_int32) for k in ("heads", "head_dim", "pages", "reserved")] + [("data", C.c_void_p)]
+
+
+class RopeAxesArg(C.Structure):
+    _fields_ = ([("table", C.c_void_p)] + [(k, C.c_int32) for k in ("positions", "columns", "rot_dim", "interleaved", "axes", "reserved")] +
+                [("axis", C.c_uint8 * 128), ("column", C.c_uint8 * 128)])
+
+
 class OpCount(C.Structure):
     _fields_ = [("perm", C.c_int64), ("decperm_in", C.c_int64), ("hstperm_in", C.c_int64),
                 ("scmult", C.c_int64), ("add", C.c_int64)]
@@ -152,6 +161,14 @@ SIGNATURES = {
     "gala_kv_export": (_I, [_VP, _VP, _VP, _VP, _VP, _VP]),
     "gala_kv_attention_workspace": (C.c_size_t, [_VP, _VP, _I, _I, _I]),
     "gala_kv_attention": (_I, [_VP, _VP, _VP, _VP, _I, C.c_float, _I, _I, _VP, _VP, _VP, C.c_size_t]),
+    "gala_kv4_cache_bytes": (C.c_size_t, [_I, _I, _I]),
+    "gala_kv4_append": (_I, [_VP, _VP, _VP, _VP, _VP, _I, _VP, _VP, _VP, _VP]),
+    "gala_kv4_export": (_I, [_VP, _VP, _VP, _VP, _VP, _VP]),
+    "gala_kv4_attention_workspace": (C.c_size_t, [_VP, _VP, _I, _I, _I]),
+    "gala_kv4_attention": (_I, [_VP, _VP, _VP, _VP, _I, C.c_float, _I, _I, _VP, _VP, _VP, C.c_size_t]),
+    "gala_rope_axes_layout": (_I, [_I, _VP, _I, C.POINTER(RopeAxesArg)]),
+    "gala_rope_apply": (_I, [_VP, _VP, _VP, _VP, C.c_int64, _I, _I, _I, _VP, _VP]),
+    "gala_rms_norm": (_I, [_VP, _VP, _VP, _I, _I, _VP, _VP, _VP, _VP, _VP]),
     "gala_sample_workspace": (C.c_size_t, [_I, _I]),
     "gala_sample": (_I, [_VP, _VP, _VP, _I, _I, _VP, _VP, _VP, C.c_size_t]),
     "gala_conv_tiling_plan": (_I, [_VP, _I, _I, _I, _I, _I, C.POINTER(ConvTiling)]),
@@ -212,6 +229,7 @@ _TYPES = {"torch.float32": 0, "torch.float16": 1, "torch.bfloat16": 2, "torch.in
 _types = {}                                    # the same by the dtype itself, filled as dtypes are met
 _named = {}                                    # dtypes by their names, likewise
 _pack_values = struct.Struct("Pqif").pack      # gala_values
+_pack_norm = struct.Struct("diiP").pack        # gala_norm
 _pack_sampling = struct.Struct("PPPPP").pack   # gala_sampling
 
 
@@ -251,6 +269,18 @@ def _heads_values(t, heads, head_dim, unit, what):
     return values, shape[0], numbers // head_dim
 
 
+def _row_values(t, rows, width, unit, what, codes=False):
+    """gala_values of `rows` rows of `width` numbers on the GPU; int8 where a call writes codes"""
+    if t.shape[0] != rows or math.prod(t.shape[1:]) != width:
+        raise ValueError(f"{what} has to hold {rows} rows of {width} numbers, not {tuple(t.shape)}")
+    _on_gpu(t, what)
+    if codes and str(t.dtype) == "torch.int8":
+        if not t[:1].is_contiguous():
+            raise ValueError("the values of a row have to be contiguous")
+        return _pack_values(t.data_ptr(), t.stride(0), 4, unit)
+    return _values(t, unit)
+
+
 def _scratch(t, size):
     """Address of a workspace of `size` bytes: a tensor, or an address"""
     if isinstance(t, int):
@@ -277,6 +307,15 @@ def rope_table(positions, rot_dim, base=10000.0, scaling=0, factor=1.0, original
     _check(load().gala_rope_table(positions, rot_dim, base, scaling, factor, original, low, high,
                                   out.ctypes.data_as(C.c_void_p)), "gala_rope_table")
     return out
+
+
+def axes_layout(sections, order=0):
+    """(axis, column) of each pair of a head for ``sections``, the pairs of each axis; order 0: blocks, 1: the axes take turns,
+    2: blocks whose columns begin at 0 for each axis."""
+    arg, sizes = RopeAxesArg(), np.asarray(sections, np.int32)
+    _check(load().gala_rope_axes_layout(len(sizes), sizes.ctypes.data_as(C.c_void_p), order, C.byref(arg)), "gala_rope_axes_layout")
+    pairs = arg.rot_dim // 2
+    return list(arg.axis[:pairs]), list(arg.column[:pairs])
 
 
 def _rots(rots):
@@ -447,6 +486,40 @@ class Context:
         return FcHybridPlan(self, W)
 
     # ---- a language model's last step
+    def rms_norm(self, x, out, add=None, sum_out=None, weight=None, epsilon=1e-6, limit=0, scales=None, group=0, unit=1.0,
+                 x_unit=1.0, add_unit=1.0, stream=None):
+        """s = x + add into ``sum_out``, its root-mean-square norm times ``weight`` (one number a column) into ``out``: rows of numbers,
+        all of the same width.  ``out`` int8 or residues: whole numbers held to +-limit, of ``unit``, or with ``scales`` (rows, scales of
+        a row) float32, one for every ``group`` columns (0: for the row)."""
+        rows = x.shape[0]
+        width = math.prod(x.shape[1:])
+        given = [None if t is None else _row_values(t, rows, width, u, what) for t, u, what in
+                 ((x, x_unit, "x"), (add, add_unit, "add"), (sum_out, 1.0, "sum_out"))]
+        given.append(None if weight is None else _row_values(weight.reshape(1, -1), 1, width, 1.0, "weight"))
+        given.append(_row_values(out, rows, width, unit, "out", codes=True))
+        at = 0
+        if scales is not None:
+            at = _words(scales, "torch.float32", "scales")
+            _on_gpu(scales, "scales")
+            if scales.numel() < rows * (-(-width // group) if group > 0 else 1):
+                raise ValueError("scales has to have a number for each row and group")
+        _check(self.lib.gala_rms_norm(self.h, _stream(stream), _pack_norm(epsilon, limit, group, at), rows, width, *given), "gala_rms_norm")
+
+    def rope_apply(self, rope, at, x, out, unit=1.0, stream=None):
+        """x (rows, heads, head_dim) turned by an AxesRope into ``out`` of the same shape; at (rows, axes) int32 positions."""
+        if x.dim() != 3 or x.shape != out.shape:
+            raise ValueError("x and out are rows x heads x head_dim, both alike")
+        rows, heads, head_dim = x.shape
+        if at.dim() != 2 or at.shape[0] != rows or at.shape[1] < rope.axes or (at.shape[1] > 1 and at.stride(1) != 1):
+            raise ValueError("at has a position on each axis for each row")
+        if str(at.dtype) != "torch.int32":
+            raise TypeError("at has to be an int32 tensor")
+        x, _, _ = _heads_values(x, heads, head_dim, unit, "x")
+        out, _, _ = _heads_values(out, heads, head_dim, unit, "out")
+        _on_gpu(at, "at")
+        _check(self.lib.gala_rope_apply(self.h, _stream(stream), rope.ref, at.data_ptr(), at.stride(0), rows, heads, head_dim, x, out),
+               "gala_rope_apply")
+
     def sample_workspace_bytes(self, rows, vocab):
         return int(self.lib.gala_sample_workspace(rows, vocab))
 
@@ -706,6 +779,25 @@ class Rope:
         self.ref = C.byref(self.arg)
 
 
+class AxesRope:
+    """gala_rope_axes: a (positions, columns, 2) float32 table on the device, and the axis and the column of each pair."""
+
+    def __init__(self, table, axis, column, interleaved=False):
+        self.table = table
+        if table.dim() != 3 or table.shape[2] != 2:
+            raise ValueError("the table holds a cosine and a sine for each position and column")
+        if not 1 <= len(axis) <= 128 or len(axis) != len(column):
+            raise ValueError("axis and column have a number for each pair, 1 to 128 of them")
+        if min(axis) < 0 or max(axis) > 3 or min(column) < 0 or max(column) >= table.shape[1]:
+            raise ValueError("there are four axes at most, and a column has to be in the table")
+        _on_gpu(table, "the table")
+        self.axes = max(axis) + 1
+        fill = [0] * (128 - len(axis))
+        self.arg = RopeAxesArg(_words(table, "torch.float32", "the table"), table.shape[0], table.shape[1], 2 * len(axis), int(interleaved),
+                               self.axes, 0, (C.c_uint8 * 128)(*axis, *fill), (C.c_uint8 * 128)(*column, *fill))
+        self.ref = C.byref(self.arg)
+
+
 class KvBatch:
     """gala_kv_batch: the sequences of a call, int32 tensors on the device; max_new and max_len bound what they hold."""
 
@@ -723,6 +815,7 @@ class KvBatch:
 class KvCache:
     """gala_kv_cache: 8-bit keys and values in pages of 64 tokens.  ``codes`` (pages, ...) int8 and ``scales``
     (pages, heads, 2) float32 are the caller's, or are made here for ``pages`` pages."""
+    _calls = "gala_kv_append", "gala_kv_export", "gala_kv_attention_workspace", "gala_kv_attention"
 
     def __init__(self, ctx, heads, head_dim, codes=None, scales=None, pages=0):
         import torch
@@ -770,19 +863,45 @@ class KvCache:
             k, v = self._kv_values(k, v, unit, ("k", "v"))
         if q is not None:
             q, q_out, heads_q = self._q_values(q, q_out, unit, "q_out")
-        _check(self._lib.gala_kv_append(self._ctx, _stream(stream), self.ref, batch.ref, None if rope is None else rope.ref,
-                                        heads_q, q, q_out, k, v), "gala_kv_append")
+        name = self._calls[0]
+        _check(getattr(self._lib, name)(self._ctx, _stream(stream), self.ref, batch.ref, None if rope is None else rope.ref, heads_q, q, q_out,
+                                        k, v), name)
 
     def export(self, batch, k_out, v_out, unit=1.0, stream=None):
         k_out, v_out = self._kv_values(k_out, v_out, unit, ("k_out", "v_out"))
-        _check(self._lib.gala_kv_export(self._ctx, _stream(stream), self.ref, batch.ref, k_out, v_out), "gala_kv_export")
+        name = self._calls[1]
+        _check(getattr(self._lib, name)(self._ctx, _stream(stream), self.ref, batch.ref, k_out, v_out), name)
 
     def attention_workspace_bytes(self, batch, heads_q, window=0, sinks=0):
-        return int(self._lib.gala_kv_attention_workspace(self.ref, batch.ref, heads_q, window, sinks))
+        return int(getattr(self._lib, self._calls[2])(self.ref, batch.ref, heads_q, window, sinks))
 
     def attention(self, batch, q, out, scale, workspace, workspace_bytes, window=0, sinks=0, unit=1.0, stream=None):
         """q (rows, heads_q, head_dim) -> out of the same shape; ``unit`` is that of residues in either, the same for both."""
         q, out, heads_q = self._q_values(q, out, unit, "out")
         workspace = _scratch(workspace, workspace_bytes)
-        _check(self._lib.gala_kv_attention(self._ctx, _stream(stream), self.ref, batch.ref, heads_q, scale, window, sinks, q, out,
-                                           workspace, workspace_bytes), "gala_kv_attention")
+        name = self._calls[3]
+        _check(getattr(self._lib, name)(self._ctx, _stream(stream), self.ref, batch.ref, heads_q, scale, window, sinks, q, out, workspace,
+                                        workspace_bytes), name)
+
+
+class Kv4Cache(KvCache):
+    """gala_kv4_cache: the same in 4 bits, with the same calls.  ``data`` (pages, ...) uint8 is the caller's, or is made here for
+    ``pages`` pages."""
+    _calls = "gala_kv4_append", "gala_kv4_export", "gala_kv4_attention_workspace", "gala_kv4_attention"
+
+    def __init__(self, ctx, heads, head_dim, data=None, pages=0):
+        import torch
+        self.ctx, self.heads, self.head_dim = ctx, heads, head_dim
+        if data is None:
+            data = torch.empty((pages, self.page_bytes(heads, head_dim)), dtype=torch.uint8, device="cuda")
+        if data.numel() != data.shape[0] * self.page_bytes(heads, head_dim):
+            raise ValueError("data does not fit the heads and their dimension")
+        self.data = data
+        self._lib, self._ctx = ctx.lib, ctx.h
+        self.arg = Kv4CacheArg(heads, head_dim, data.shape[0], 0, _words(data, "torch.uint8", "data"))
+        _on_gpu(data, "data")
+        self.ref = C.byref(self.arg)
+
+    @staticmethod
+    def page_bytes(heads, head_dim):
+        return int(load().gala_kv4_cache_bytes(1, heads, head_dim))

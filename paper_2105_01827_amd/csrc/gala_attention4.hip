@@ -1,0 +1,345 @@
+// Attention of a batch's queries over the paged 4-bit cache.
+#include "gala_attention.h"
+
+using namespace gala;
+
+namespace {
+
+typedef __bf16 v8b __attribute__((ext_vector_type(8)));
+typedef __bf16 v2b __attribute__((ext_vector_type(2)));
+
+// A head of G x 32 channels is multiplied in G products of 32.  Four lanes (parts) have a token's key: of four groups of 32
+// channels one each, of two left over half a group each, of one left over eight channels each, so that a lane loads 16,
+// 8 or 4 bytes.  Product n takes the lanes' n-th words: the order of channels within it is the queries' too.
+template <int G>
+struct Words {
+    static constexpr int kFours = G / 4;
+    // group and word within it
+    static __device__ __forceinline__ int group(int n, int part) {
+        if (n < 4 * kFours) return n / 4 * 4 + part;
+        if ((G & 2) && n < 4 * kFours + 2) return 4 * kFours + (part >> 1);
+        return G - 1;
+    }
+    static __device__ __forceinline__ int word(int n, int part) {
+        if (n < 4 * kFours) return n & 3;
+        if ((G & 2) && n < 4 * kFours + 2) return (part & 1) * 2 + (n & 1);
+        return part;
+    }
+};
+template <int G>
+struct Keys {
+    u32 code[4][G];          // of four tiles of 16 tokens
+    u32 exponent[G];         // a byte for each tile; word n's
+};
+template <int G>
+__device__ __forceinline__ void load_keys(const char *data, int token, int part, Keys<G> &k) {
+    typedef Words<G> W;
+    constexpr int kTwo = 4 * W::kFours;
+    auto at = [&](int i, int n) { return data + (i * G + W::group(n, part)) * 256 + token * 16 + W::word(n, part) * 4; };
+    auto exponent = [&](int n) { return *(const u32 *)(data + kv4_exponents(G) + token * 4 + W::group(n, part) * 64); };
+#pragma unroll
+    for (int n = 0; n < kTwo; n += 4) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int4 x = *(const int4 *)at(i, n);
+            k.code[i][n] = x.x, k.code[i][n + 1] = x.y, k.code[i][n + 2] = x.z, k.code[i][n + 3] = x.w;
+        }
+        k.exponent[n] = k.exponent[n + 1] = k.exponent[n + 2] = k.exponent[n + 3] = exponent(n);
+    }
+    if constexpr (G & 2) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int2 x = *(const int2 *)at(i, kTwo);
+            k.code[i][kTwo] = x.x, k.code[i][kTwo + 1] = x.y;
+        }
+        k.exponent[kTwo] = k.exponent[kTwo + 1] = exponent(kTwo);
+    }
+    if constexpr (G & 1) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) k.code[i][G - 1] = *(const u32 *)at(i, G - 1);
+        k.exponent[G - 1] = exponent(G - 1);
+    }
+}
+__device__ __forceinline__ v8b numbers_of(u32 codes, float scale) {
+    union {
+        v2b pair[4];
+        v8b all;
+    } u;
+    u.pair[0] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 0);
+    u.pair[1] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 1);
+    u.pair[2] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 2);
+    u.pair[3] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 3);
+    return u.all;
+}
+// x as the sum of N bfloat16 numbers of eight bits each: the first ones cut off, the last one rounded, so that 8 N bits of x are
+// kept, to half a step
+template <int N>
+__device__ __forceinline__ void parts_of(float (&x)[8], v8b (&to)[N]) {
+    union {
+        u32 word[4];
+        v8b all;
+    } u;
+#pragma unroll
+    for (int n = 0; n + 1 < N; ++n) {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) u.word[k] = __builtin_amdgcn_perm(__float_as_uint(x[2 * k + 1]), __float_as_uint(x[2 * k]), 0x07060302);
+        to[n] = u.all;
+#pragma unroll
+        for (int k = 0; k < 8; ++k) x[k] -= __uint_as_float(__float_as_uint(x[k]) & 0xffff0000u);
+    }
+#pragma unroll
+    for (int k = 0; k < 8; ++k) to[N - 1][k] = (__bf16)x[k];
+}
+
+// Scores are products of the codes with their powers of two, exact in bfloat16, and of the queries in NQ bfloat16 parts (8 bits
+// each; a query of 8, 11 or 24 bits is all of its parts).  Of a block's scores a lane has 16 of one column's, and they are
+// the very weights that it hands to the second product, because the values' codes lie in that order of tokens: a block goes from memory
+// to the sums without LDS or an exchange between lanes, but for the largest score.  A weight takes its token's scale of
+// values along and is cut into NW parts.  A wavefront has blocks of its own; a workgroup's wavefronts are joined at the end.
+template <int G, int NQ, int NW, int kWaves>
+__global__ __launch_bounds__(64 * kWaves, G <= 4 ? 2 : 1) void kv4_attention_kernel(Attention a) {
+    constexpr int NV = 2 * G;                                // tiles of 16 channels of values
+    typedef Words<G> W;
+    __shared__ float sums[kWaves][kColumns][NV * 16 + 1];
+    __shared__ float stats[kWaves][kColumns][2];
+    const KvArgs &kv = a.kv;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 15, part = lane >> 4;
+    int unit = blockIdx.x;
+    const int split = unit % a.splits;
+    unit /= a.splits;
+    const int tile = unit % a.tiles;
+    unit /= a.tiles;
+    const int h = unit % kv.heads, b = unit / kv.heads;
+    const Seen s = seen_by(a, b, tile);
+    if (!s.cols) return;
+    const int share = share_of(a, s.total), from = split * share, to = min(s.total, from + share);
+    if (split && from >= s.total) return;
+    // The next block's keys are under way while this one's weights are made, the one after's page too.
+    constexpr size_t kHead = 64 * (33 * G + 2);
+    Keys<G> keys;
+    int u = from + wave, page, page_next;
+    auto page_at = [&](int v) { return v < to ? page_of(kv, b, s.block(v)) : -1; };
+    // without a page the first one is read and not seen: no branch around what is under way
+    auto data_of = [&](int page) { return (const char *)kv.codes + ((size_t)max(page, 0) * kv.heads + h) * kHead; };
+    page = page_at(u), page_next = page_at(u + kWaves);
+    if (u < to) load_keys<G>(data_of(page), col, part, keys);
+    // the column's query
+    const int c = s.col0 + min(col, s.cols - 1), qi = c / a.group, g = c % a.group;
+    const long row = s.start + qi;
+    const int at = s.at_lo - s.col0 / a.group + qi, hq = h * a.group + g;
+    v8b q[G][NQ];
+    bool bad;
+    {
+        int fine = 1;
+        auto load = [&](auto type) __attribute__((always_inline)) {
+#pragma unroll
+            for (int n = 0; n < G; ++n) {
+                float x[8];
+                const int d = W::group(n, part) * 32 + W::word(n, part) * 8;
+                load_channels<decltype(type)::value, 1>(a.q, a.pieces, row, hq * kv.dim + d, hq * kv.dim + kv.dim, x);
+#pragma unroll
+                for (int k = 0; k < 8; ++k) {
+                    fine &= fabsf(x[k]) < INFINITY;
+                    x[k] = fabsf(x[k]) < INFINITY ? x[k] : 0.0f;
+                }
+                parts_of<NQ>(x, q[n]);
+            }
+        };
+        by_type(a.q.type, load);
+        fine &= __shfl_xor(fine, 16);
+        fine &= __shfl_xor(fine, 32);
+        bad = !fine;
+    }
+    const float unit_q = a.scale * kLog2E;
+    v4f o[NV];
+#pragma unroll
+    for (int j = 0; j < NV; ++j) o[j] = v4f{0, 0, 0, 0};
+    float top = -INFINITY, sum = 0;
+    for (; u < to; u += kWaves) {
+        const int block = s.block(u), end = page < 0 ? 0 : kv.max_len;
+        const char *data = data_of(page);
+        u32 values[G][4];
+#pragma unroll
+        for (int j = 0; j < G; ++j) {
+            const int4 x = *(const int4 *)(data + 1024 * G + j * 1024 + lane * 16);
+            values[j][0] = x.x, values[j][1] = x.y, values[j][2] = x.z, values[j][3] = x.w;
+        }
+        u32 scales[8];
+        {
+            const int4 *from = (const int4 *)(data + kv4_scales(G) + part * 32);
+            const int4 x = from[0], y = from[1];
+            scales[0] = x.x, scales[1] = x.y, scales[2] = x.z, scales[3] = x.w, scales[4] = y.x, scales[5] = y.y, scales[6] = y.z, scales[7] = y.w;
+        }
+        float t[16], scale_v[16];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) scale_v[2 * k] = __uint_as_float(scales[k] << 16), scale_v[2 * k + 1] = __uint_as_float(scales[k] & 0xffff0000u);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            v4f acc = v4f{0, 0, 0, 0};
+            v8b k[G];
+#pragma unroll
+            for (int n = 0; n < G; ++n) k[n] = numbers_of(keys.code[i][n], __uint_as_float((i < 3 ? keys.exponent[n] << (24 - 8 * i) >> 1 : keys.exponent[n] >> 1) & 0x7f800000u));
+#pragma unroll
+            for (int p = NQ - 1; p >= 0; --p)        // the small parts first
+#pragma unroll
+                for (int n = 0; n < G; ++n) acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k[n], q[n][p], acc, 0, 0, 0);
+#pragma unroll
+            for (int r = 0; r < 4; ++r) t[4 * i + r] = acc[r] * unit_q;
+        }
+        page = page_next;
+        load_keys<G>(data_of(page), col, part, keys);
+        page_next = page_at(u + 2 * kWaves);
+        const int t0 = block * kKvBlock;
+        if (t0 + 63 > s.at_lo || t0 + 64 > end || (a.window && t0 <= s.at_hi - a.window)) {
+            // keys of the block by their distance from the lane's first one; no branches between them
+            const int own = t0 + part * 4, hi = min(at, end - 1) - own;
+            const int lo = a.window ? at - a.window + 1 - own : -kKvBlock, sinks = a.window ? a.sinks - own : 0;
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    const int e = i * 16 + r;
+                    const bool seen = (e <= hi) & ((e >= lo) | (e < sinks));
+                    t[4 * i + r] = seen ? t[4 * i + r] : -INFINITY;
+                    scale_v[4 * i + r] = seen ? scale_v[4 * i + r] : 0.0f;           // what is not seen may be no number
+                }
+        }
+        float most = t[0];
+#pragma unroll
+        for (int i = 1; i < 16; ++i) most = fmaxf(most, t[i]);
+        most = fmaxf(most, __shfl_xor(most, 16));
+        most = fmaxf(most, __shfl_xor(most, 32));
+        if (__any(most > top)) {
+            const float now = fmaxf(top, most), was = now > top ? __builtin_amdgcn_exp2f(top - now) : 1.0f;
+            top = now;
+            sum *= was;
+#pragma unroll
+            for (int j = 0; j < NV; ++j) o[j] *= was;
+        }
+        const float base = top == -INFINITY ? 0.0f : top;
+        v8b w[2][NW];
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+            float x[8];
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                const float p = __builtin_amdgcn_exp2f(t[8 * half + k] - base);
+                sum += p;
+                x[k] = p * scale_v[8 * half + k];
+            }
+            parts_of<NW>(x, w[half]);
+        }
+#pragma unroll
+        for (int j = 0; j < NV; ++j) {
+#pragma unroll
+            for (int half = 0; half < 2; ++half) {
+                const v8b v = numbers_of(values[j >> 1][(j & 1) * 2 + half], 1.0f);
+#pragma unroll
+                for (int p = NW - 1; p >= 0; --p) o[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, w[half][p], o[j], 0, 0, 0);
+            }
+        }
+    }
+    // the wavefronts' sums in one
+    sum += __shfl_xor(sum, 16);
+    sum += __shfl_xor(sum, 32);
+#pragma unroll
+    for (int j = 0; j < NV; ++j)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) sums[wave][col][j * 16 + part * 4 + r] = o[j][r];
+    if (part == 0) stats[wave][col][0] = bad ? __builtin_nanf("") : top, stats[wave][col][1] = sum;
+    __syncthreads();
+    const long place = (((long)b * kv.heads + h) * a.tiles + tile) * a.splits + split;
+    for (int e = threadIdx.x; e < s.cols * kv.dim; e += 64 * kWaves) {
+        const int cc = e / kv.dim, d = e % kv.dim;
+        float most = -INFINITY, all = 0, x = 0;
+#pragma unroll
+        for (int k = 0; k < kWaves; ++k) most = fmaxf(most, stats[k][cc][0]);
+        const float base = most == -INFINITY ? 0.0f : most;
+#pragma unroll
+        for (int k = 0; k < kWaves; ++k) {
+            const float f = __builtin_amdgcn_exp2f(stats[k][cc][0] - base);       // NaN where the query is
+            all += f * stats[k][cc][1];
+            x += f * sums[k][cc][d];
+        }
+        if (a.splits == 1) {
+            const int column = s.col0 + cc;
+            store_any(a.out, s.start + column / a.group, (h * a.group + column % a.group) * kv.dim + d, all == 0 ? 0.0f : x / all);
+        } else {
+            a.sums[(place * a.columns + cc) * kv.dim + d] = x;
+            if (d == 0) a.stats[(place * a.columns + cc) * 2] = all != all ? __builtin_nanf("") : most, a.stats[(place * a.columns + cc) * 2 + 1] = all;
+        }
+    }
+}
+
+// How a call is cut up.
+struct Cut {
+    int tiles, splits, columns;
+    long places() const { return (long)tiles * splits * columns; }
+};
+Cut cut_of(const KvArgs &kv, int heads_q, int window, int sinks) {
+    Cut c;
+    const long columns = (long)kv.max_new * (heads_q / kv.heads);
+    const long reach = std::min<long>(kv.max_len, (long)kv.table_stride * kKvBlock);
+    const long keys = window ? std::min(reach, (long)window + kv.max_new + sinks + 2 * kKvBlock) : reach;
+    const long blocks = std::max(1l, (keys + kKvBlock - 1) / kKvBlock);
+    c.tiles = (int)((columns + kColumns - 1) / kColumns);
+    c.columns = (int)std::min<long>(columns, kColumns);
+    const long units = std::max(1l, (long)kv.count * kv.heads * c.tiles);
+    c.splits = (int)std::max(1l, std::min((512 + units - 1) / units, (blocks + 31) / 32));
+    return c;
+}
+
+}  // namespace
+
+namespace gala {
+
+size_t kv4_attention_workspace(const KvArgs &kv, int heads_q, int window, int sinks) {
+    const Cut c = cut_of(kv, heads_q, window, sinks);
+    return c.splits == 1 ? 0 : (size_t)kv.count * kv.heads * c.places() * (kv.dim + 2) * sizeof(float);
+}
+
+int launch_kv4_attention(void *stream, const KvArgs &kv, int heads_q, float scale, int window, int sinks, const Values &q,
+                         const Values &out, void *workspace) {
+    const bool fine = q.type == GALA_F32 || q.type == GALA_RESIDUE || out.type == GALA_F32 || out.type == GALA_RESIDUE;
+    const Cut c = cut_of(kv, heads_q, window, sinks);
+    Attention a{};
+    a.kv = kv, a.q = q, a.out = out;
+    const size_t size = q.type == GALA_F32 ? 4 : q.type == GALA_RESIDUE ? 8 : 2;
+    a.pieces = (uintptr_t)q.data % 16 == 0 && q.stride * size % 16 == 0 && kv.dim % 8 == 0;
+    a.heads_q = heads_q, a.group = heads_q / kv.heads;
+    a.scale = scale, a.window = window, a.sinks = sinks;
+    a.tiles = c.tiles, a.splits = c.splits, a.columns = c.columns;
+    a.sums = (float *)workspace;
+    a.stats = a.sums + (size_t)kv.count * kv.heads * c.places() * kv.dim;
+    const unsigned groups = (unsigned)((long)kv.count * kv.heads * c.tiles * c.splits);
+    auto launch = [&](auto n32) {
+        constexpr int G = decltype(n32)::value;
+        auto waves = [&](auto w) {
+            constexpr int W = decltype(w)::value;
+            a.waves = W;
+            if (fine)
+                hipLaunchKernelGGL((kv4_attention_kernel<G, 3, 3, W>), dim3(groups), dim3(64 * W), 0, (hipStream_t)stream, a);
+            else if (q.type == GALA_F16)
+                hipLaunchKernelGGL((kv4_attention_kernel<G, 2, 2, W>), dim3(groups), dim3(64 * W), 0, (hipStream_t)stream, a);
+            else
+                hipLaunchKernelGGL((kv4_attention_kernel<G, 1, 2, W>), dim3(groups), dim3(64 * W), 0, (hipStream_t)stream, a);
+        };
+        waves(std::integral_constant<int, 4>());
+        if (c.splits == 1) return;
+        const unsigned rows = (unsigned)((long)kv.count * kv.heads * c.tiles * c.columns);
+        hipLaunchKernelGGL((kv_attention_join_kernel<(G + 1) / 2>), dim3(rows), dim3(64 * kJoinWaves), 0, (hipStream_t)stream, a);
+    };
+    switch (kv4_groups(kv.dim)) {
+        case 1: launch(std::integral_constant<int, 1>()); break;
+        case 2: launch(std::integral_constant<int, 2>()); break;
+        case 3: launch(std::integral_constant<int, 3>()); break;
+        case 4: launch(std::integral_constant<int, 4>()); break;
+        case 5: launch(std::integral_constant<int, 5>()); break;
+        case 6: launch(std::integral_constant<int, 6>()); break;
+        case 7: launch(std::integral_constant<int, 7>()); break;
+        default: launch(std::integral_constant<int, 8>()); break;
+    }
+    return hipGetLastError() != hipSuccess;
+}
+
+}  // namespace gala

@@ -38,6 +38,32 @@ int launch_kv_export(void *stream, const KvArgs &kv, const Values &k_out, const 
 size_t kv_attention_workspace(const KvArgs &kv, int heads_q, int window, int sinks);
 int launch_kv_attention(void *stream, const KvArgs &kv, int heads_q, float scale, int window, int sinks, const Values &q,
                         const Values &out, void *workspace);
+// The same on a cache in 4 bits: its data are the codes, scales and dim16 are not used.
+constexpr int kGroupOf = 32;     // channels of a key that share a power of two
+constexpr int kLeastExponent = -120, kMostExponent = 125;
+GALA_HD int kv4_groups(int dim) { return (dim + kGroupOf - 1) / kGroupOf; }
+GALA_HD size_t kv4_head_bytes(int groups) { return (size_t)kKvBlock * (33 * groups + 2); }
+// where a head's part of a page has the keys' exponents and the values' scales; the values' codes are at 1024 * groups
+GALA_HD int kv4_exponents(int groups) { return 2048 * groups; }
+GALA_HD int kv4_scales(int groups) { return 2112 * groups; }
+int launch_kv4_append(void *stream, const KvArgs &kv, const RopeArgs &rope, int heads_q, const Values &q, const Values &q_out,
+                      const Values &k, const Values &v);
+int launch_kv4_export(void *stream, const KvArgs &kv, const Values &k_out, const Values &v_out);
+size_t kv4_attention_workspace(const KvArgs &kv, int heads_q, int window, int sinks);
+int launch_kv4_attention(void *stream, const KvArgs &kv, int heads_q, float scale, int window, int sinks, const Values &q,
+                         const Values &out, void *workspace);
+int launch_rope_apply(void *stream, const gala_rope_axes &rope, const int *at, long at_stride, int rows, int heads, int dim, const Values &x,
+                      const Values &out);
+// How a norm's row becomes whole numbers.
+struct NormArgs {
+    double epsilon;
+    float limit, step;               // step: 1 / limit
+    int group;                       // channels of a scale
+    float *scales;                   // nullptr: none
+    int rows, width;
+};
+int launch_rms_norm(void *stream, const NormArgs &how, const Values &x, const Values &add, const Values &sum, const Values &weight,
+                    const Values &out);
 size_t sample_workspace(int rows, int vocab);
 int launch_sample(void *stream, const Values &logits, int rows, int vocab, const gala_sampling &how, int *tokens,
                   void *workspace);

@@ -15,7 +15,7 @@ constexpr int kFarthest = 1 << 30;      // no sequence is longer: distances beyo
 constexpr int kMostTokens = (1 << 24) - 1;      // of a vocabulary: that many weights of 2^40 add up in 64 bits
 constexpr double kTwoPi = 6.283185307179586476925286766559;
 
-size_t type_size(int type) { return type == GALA_F32 ? 4 : type == GALA_RESIDUE ? 8 : 2; }
+size_t type_size(int type) { return type == GALA_F32 ? 4 : type == GALA_RESIDUE ? 8 : type == GALA_INT8 ? 1 : 2; }
 
 // `row`: numbers of a row; an output's rows must not overlap
 bool values_ok(const gala_values *v, int64_t row, bool output) {
@@ -52,6 +52,30 @@ bool attention_ok(const gala_kv_cache *cache, const gala_kv_batch *batch, int he
     if (!cache_ok(cache) || !batch_ok(batch) || heads_q < 1 || heads_q % cache->heads || window < 0 || sinks < 0) return false;
     return heads_q <= (1 << 20) && fits_grid((int64_t)batch->count * batch->max_new) &&
            fits_grid((int64_t)batch->count * batch->max_new * heads_q);
+}
+
+// ... and in threads
+bool fits_launch(int64_t groups, int threads) { return groups <= 0xffffffffll / threads; }
+bool cache4_ok(const gala_kv4_cache *k) {
+    if (!k || k->heads < 1 || k->head_dim < 1 || k->head_dim > kMaxHeadDim || k->pages < 0 || k->reserved) return false;
+    return (!k->pages || k->data) && (uintptr_t)k->data % 16 == 0;
+}
+KvArgs kv4_args(const gala_kv4_cache *k, const gala_kv_batch *b) {
+    const gala_kv_cache same{k->heads, k->head_dim, k->pages, 0, (int8_t *)k->data, nullptr};
+    return kv_args(&same, b);
+}
+bool attention4_ok(const gala_kv4_cache *cache, const gala_kv_batch *batch, int heads_q, int window, int sinks) {
+    if (!cache4_ok(cache) || !batch_ok(batch) || heads_q < 1 || heads_q > (1 << 20) || heads_q % cache->heads || window < 0 || sinks < 0) return false;
+    const int64_t tiles = ((int64_t)batch->max_new * (heads_q / cache->heads) + 15) / 16;
+    return tiles <= (1 << 24) && fits_launch(tiles * batch->count, 1) && fits_launch(tiles * batch->count * cache->heads, 256);
+}
+// what a call writes may be what it reads where every number lies at the same place
+bool apart_or_same(const gala_values *a, const gala_values *b) {
+    return !a || !b || a->data != b->data || (a->type == b->type && a->stride == b->stride);
+}
+bool rope_ok(const gala_rope *rope, int dim) {
+    return !rope || (rope->table && rope->positions >= 1 && rope->rot_dim >= 2 && rope->rot_dim % 2 == 0 && rope->rot_dim <= dim &&
+                     (uintptr_t)rope->table % 8 == 0);
 }
 
 }  // namespace
@@ -146,6 +170,144 @@ extern "C" int gala_kv_attention(const gala_ctx *c, void *stream, const gala_kv_
     if (!batch->count || !batch->max_new) return GALA_OK;
     return launch_kv_attention(stream, kv, heads_q, scale, window, sinks, values(c, q), values(c, out), workspace) ? GALA_EHIP
                                                                                                                    : GALA_OK;
+}
+
+extern "C" size_t gala_kv4_cache_bytes(int pages, int heads, int head_dim) {
+    if (pages < 0 || heads < 1 || head_dim < 1 || head_dim > kMaxHeadDim) return 0;
+    return (size_t)pages * heads * kv4_head_bytes(kv4_groups(head_dim));
+}
+
+extern "C" int gala_kv4_append(const gala_ctx *c, void *stream, const gala_kv4_cache *cache, const gala_kv_batch *batch,
+                               const gala_rope *rope, int heads_q, const gala_values *q, const gala_values *q_out,
+                               const gala_values *k, const gala_values *v) {
+    if (!c || !cache4_ok(cache) || !batch_ok(batch) || heads_q < 0 || heads_q > (1 << 20)) return GALA_EARG;
+    if (!q != !q_out || !q != !heads_q || !k != !v) return GALA_EARG;
+    const int dim = cache->head_dim;
+    if (q && (!values_ok(q, (int64_t)heads_q * dim, false) || !values_ok(q_out, (int64_t)heads_q * dim, true) ||
+              q_out->type == GALA_RESIDUE || !apart_or_same(q, q_out)))
+        return GALA_EARG;
+    if (k && (!values_ok(k, (int64_t)cache->heads * dim, false) || !values_ok(v, (int64_t)cache->heads * dim, false) ||
+              k->type != v->type))
+        return GALA_EARG;
+    if ((q && k && q->type != k->type) || !rope_ok(rope, dim)) return GALA_EARG;
+    const int64_t blocks = (batch->max_new + 62) / 64 + 1, of_blocks = batch->count * blocks + 7, rows = (int64_t)batch->count * batch->max_new;
+    if (!fits_launch(of_blocks, 256) || !fits_launch(rows, 256) || !fits_launch(of_blocks * cache->heads * 2 + rows, 256)) return GALA_EARG;
+    if (!c->has_device) return GALA_EHIP;
+    if (!batch->count || !batch->max_new || (!q && !k)) return GALA_OK;
+    const RopeArgs r{rope ? rope->table : nullptr, rope ? rope->positions : 0, rope ? rope->rot_dim / 2 : 0,
+                     rope ? rope->interleaved != 0 : 0};
+    return launch_kv4_append(stream, kv4_args(cache, batch), r, heads_q, values(c, q), values(c, q_out), values(c, k),
+                             values(c, v)) ? GALA_EHIP : GALA_OK;
+}
+
+extern "C" int gala_kv4_export(const gala_ctx *c, void *stream, const gala_kv4_cache *cache, const gala_kv_batch *batch,
+                               const gala_values *k_out, const gala_values *v_out) {
+    if (!c || !cache4_ok(cache) || !batch_ok(batch)) return GALA_EARG;
+    const int64_t row = (int64_t)cache->heads * cache->head_dim;
+    if (!values_ok(k_out, row, true) || !values_ok(v_out, row, true) || k_out->type != v_out->type) return GALA_EARG;
+    const int64_t of_blocks = (int64_t)batch->count * ((batch->max_new + 62) / 64 + 1) + 7;
+    if (!fits_launch(of_blocks, 256) || !fits_launch(of_blocks * cache->heads * 2, 256)) return GALA_EARG;
+    if (!c->has_device) return GALA_EHIP;
+    if (!batch->count || !batch->max_new) return GALA_OK;
+    return launch_kv4_export(stream, kv4_args(cache, batch), values(c, k_out), values(c, v_out)) ? GALA_EHIP : GALA_OK;
+}
+
+extern "C" size_t gala_kv4_attention_workspace(const gala_kv4_cache *cache, const gala_kv_batch *batch, int heads_q, int window,
+                                               int sinks) {
+    if (!attention4_ok(cache, batch, heads_q, window, sinks)) return 0;
+    return kv4_attention_workspace(kv4_args(cache, batch), heads_q, std::min(window, kFarthest), std::min(sinks, kFarthest));
+}
+
+extern "C" int gala_kv4_attention(const gala_ctx *c, void *stream, const gala_kv4_cache *cache, const gala_kv_batch *batch,
+                                  int heads_q, float scale, int window, int sinks, const gala_values *q, const gala_values *out,
+                                  void *workspace, size_t workspace_bytes) {
+    if (!c || !attention4_ok(cache, batch, heads_q, window, sinks) || !std::isfinite(scale)) return GALA_EARG;
+    const int64_t row = (int64_t)heads_q * cache->head_dim;
+    if (!values_ok(q, row, false) || !values_ok(out, row, true) || !apart_or_same(q, out)) return GALA_EARG;
+    const KvArgs kv = kv4_args(cache, batch);
+    window = std::min(window, kFarthest), sinks = std::min(sinks, kFarthest);
+    const size_t need = kv4_attention_workspace(kv, heads_q, window, sinks);
+    if (need && (!workspace || (uintptr_t)workspace % 16)) return GALA_EARG;
+    if (workspace_bytes < need) return GALA_ENOMEM;
+    if (!c->has_device) return GALA_EHIP;
+    if (!batch->count || !batch->max_new) return GALA_OK;
+    return launch_kv4_attention(stream, kv, heads_q, scale, window, sinks, values(c, q), values(c, out), workspace) ? GALA_EHIP
+                                                                                                                    : GALA_OK;
+}
+
+extern "C" int gala_rope_axes_layout(int axes, const int32_t *sections, int order, gala_rope_axes *out) {
+    if (axes < 1 || axes > 4 || !sections || !out || order < GALA_AXES_BLOCKS || order > GALA_AXES_OWN) return GALA_EARG;
+    int pairs = 0, most = 0;
+    for (int a = 0; a < axes; ++a) {
+        if (sections[a] < 0 || sections[a] > kMaxHeadDim / 2 - pairs) return GALA_EARG;
+        pairs += sections[a], most = std::max(most, sections[a]);
+    }
+    if (!pairs) return GALA_EARG;
+    int left[4] = {}, i = 0;
+    std::copy(sections, sections + axes, left);
+    if (order == GALA_AXES_TURNS) {
+        for (int a = 0; i < pairs; a = (a + 1) % axes)
+            if (left[a]) --left[a], out->axis[i] = (uint8_t)a, out->column[i] = (uint8_t)i, ++i;
+    } else {
+        for (int a = 0; a < axes; ++a)
+            for (int k = 0; k < sections[a]; ++k, ++i) out->axis[i] = (uint8_t)a, out->column[i] = (uint8_t)(order == GALA_AXES_OWN ? k : i);
+    }
+    std::fill(out->axis + pairs, out->axis + 128, 0);
+    std::fill(out->column + pairs, out->column + 128, 0);
+    out->axes = axes, out->rot_dim = 2 * pairs, out->columns = order == GALA_AXES_OWN ? most : pairs;
+    return GALA_OK;
+}
+
+extern "C" int gala_rope_apply(const gala_ctx *c, void *stream, const gala_rope_axes *rope, const int32_t *at, int64_t at_stride,
+                               int rows, int heads, int head_dim, const gala_values *x, const gala_values *out) {
+    if (!c || !rope || !at || (uintptr_t)at % 4 || at_stride < 0 || rows < 0 || heads < 1 || heads > (1 << 20) || head_dim < 1 || head_dim > kMaxHeadDim)
+        return GALA_EARG;
+    if (!rope->table || (uintptr_t)rope->table % 8 || rope->positions < 1 || rope->columns < 1 || rope->columns > 256 || rope->rot_dim < 2 ||
+        rope->rot_dim % 2 || rope->rot_dim > head_dim || rope->axes < 1 || rope->axes > 4 || rope->reserved)
+        return GALA_EARG;
+    for (int i = 0; i < rope->rot_dim / 2; ++i)
+        if (rope->axis[i] >= rope->axes || rope->column[i] >= rope->columns) return GALA_EARG;
+    const int64_t row = (int64_t)heads * head_dim;
+    if (!values_ok(x, row, false) || !values_ok(out, row, true) || out->type == GALA_RESIDUE || !apart_or_same(x, out)) return GALA_EARG;
+    if (!fits_launch(rows, 256)) return GALA_EARG;
+    if (!c->has_device) return GALA_EHIP;
+    if (!rows) return GALA_OK;
+    return launch_rope_apply(stream, *rope, at, (long)at_stride, rows, heads, head_dim, values(c, x), values(c, out)) ? GALA_EHIP : GALA_OK;
+}
+
+extern "C" int gala_rms_norm(const gala_ctx *c, void *stream, const gala_norm *how, int rows, int width, const gala_values *x,
+                             const gala_values *add, const gala_values *sum_out, const gala_values *weight, const gala_values *out) {
+    if (!c || !how || rows < 0 || width < 1 || !(how->epsilon >= 0) || !std::isfinite(how->epsilon)) return GALA_EARG;
+    if (how->limit < 0 || how->limit >= 1 << 24 || how->group < 0 || (uintptr_t)how->scales % 4) return GALA_EARG;
+    if (!values_ok(x, width, false) || (add && !values_ok(add, width, false)) || (weight && !values_ok(weight, width, false)) ||
+        (weight && weight->type == GALA_RESIDUE) || (sum_out && (!values_ok(sum_out, width, true) || sum_out->type == GALA_RESIDUE)))
+        return GALA_EARG;
+    const bool codes = out && out->type == GALA_INT8;
+    if (codes ? (!out->data || out->stride < width || !how->limit || how->limit > 127) : !values_ok(out, width, true)) return GALA_EARG;
+    const bool whole = codes || out->type == GALA_RESIDUE;
+    if (!whole && (how->scales || how->limit || how->group)) return GALA_EARG;
+    if (how->group && !how->scales) return GALA_EARG;
+    if (codes && !how->scales && !(out->unit > 0 && std::isfinite(out->unit))) return GALA_EARG;
+    if (out->type == GALA_RESIDUE && (uint64_t)how->limit > c->p / 2) return GALA_EARG;
+    for (const gala_values *written : {out, sum_out})
+        for (const gala_values *read : {x, add, weight})
+            if (!apart_or_same(written, read)) return GALA_EARG;
+    if ((sum_out && sum_out->data == out->data) || (weight && (weight->data == out->data || (sum_out && sum_out->data == weight->data)))) return GALA_EARG;
+    if (!fits_launch(rows, 1024)) return GALA_EARG;
+    if (!c->has_device) return GALA_EHIP;
+    if (!rows) return GALA_OK;
+    NormArgs n{};
+    n.epsilon = how->epsilon;
+    n.limit = (float)how->limit;
+    if (whole && !how->limit) {          // the largest number of 24 bits
+        n.limit = (float)(c->p / 2);
+        if ((double)n.limit > (double)(c->p / 2)) n.limit = std::nextafter(n.limit, 0.0f);
+    }
+    n.step = (float)(1.0 / n.limit);
+    n.group = how->scales && how->group && how->group < width ? how->group : width;
+    n.scales = how->scales;
+    n.rows = rows, n.width = width;
+    return launch_rms_norm(stream, n, values(c, x), values(c, add), values(c, sum_out), values(c, weight), values(c, out)) ? GALA_EHIP : GALA_OK;
 }
 
 extern "C" size_t gala_sample_workspace(int rows, int vocab) {
