@@ -2,7 +2,8 @@
 
 The server holds the weights and evaluates every linear layer on ciphertexts (``he_fc``); the client holds the tokens, the
 activations and the cache, and runs what lies between two linear layers on the values that its share and the server's add
-up to: positions, the paged 8-bit cache, attention and the choice of the next token.  Both ends run in this process, on
+up to: the residual stream and its norm in 8 bits, positions, the paged cache of 8 or 4 bits, attention and the choice of the
+next token.  Both ends run in this process, on
 one device.  Weights are random, as small whole numbers; activations travel as fixed-point numbers modulo p.
 What hides one end's numbers from the other -- keys, encryption, the server's shares and masks -- is drawn afresh from the
 system's random source at every use, whatever the model's seed.
@@ -29,6 +30,7 @@ class Shape:
     batch: int = 3
     steps: int = 6
     context: int = 256               # tokens that a sequence may have, its answer's included
+    bits: int = 8                    # of a number in the cache: 8 or 4
     unit_x: float = 2.0 ** -5        # what one unit of an activation stands for
     unit_w: float = 2.0 ** -6        # ... and of a weight
 
@@ -90,18 +92,18 @@ class Model:
         self.embedding = torch.from_numpy(rng.standard_normal((s.vocab, s.width))).float().cuda()
         self.qkv, self.merge, self.head = linear(qkv, s.width), linear(s.width, s.heads * s.head_dim), linear(s.vocab, s.width)
         self.blocks = -(-s.context // 64)
-        self.cache = binding.KvCache(self.ctx, s.heads_kv, s.head_dim, pages=s.batch * self.blocks)
+        self.cache = {8: binding.KvCache, 4: binding.Kv4Cache}[s.bits](self.ctx, s.heads_kv, s.head_dim, pages=s.batch * self.blocks)
         # pages in any order
         self.table = torch.from_numpy(rng.permutation(s.batch * self.blocks).astype(np.int32).reshape(s.batch, self.blocks)).cuda()
         table = binding.rope_table(64 * self.blocks, s.head_dim)
         self.rope = binding.Rope(torch.from_numpy(table).cuda())
         self.lens = [0] * s.batch
 
-    def residues(self, x):
-        return torch.round(x / self.shape.unit_x).clamp(-127, 127).to(torch.int64).remainder(wl.P)
-
-    def norm(self, x):
-        return x * torch.rsqrt(x.square().mean(-1, keepdim=True) + 1e-6)
+    def normed(self, x, merged=None):
+        """The stream x, a layer's output added if there is one, as the next layer takes it: its norm as whole numbers of 8 bits"""
+        out = torch.empty(x.shape, dtype=torch.int64, device="cuda")
+        self.ctx.rms_norm(x, out, add=merged, limit=127, unit=self.shape.unit_x, add_unit=self.shape.unit_x * self.shape.unit_w)
+        return out
 
     def step(self, tokens, counts):
         """`tokens`: new ones of all sequences, counts[b] of sequence b; returns the logits after each sequence's last, as residues"""
@@ -114,7 +116,7 @@ class Model:
         starts = torch.tensor([0] + list(np.cumsum(counts)), dtype=torch.int32, device="cuda")
         batch = binding.KvBatch(starts, torch.tensor(self.lens, dtype=torch.int32, device="cuda"), self.table, max(counts), max(self.lens))
         x = self.embedding[tokens]
-        qkv = self.qkv(self.residues(self.norm(x))).view(-1, s.heads + 2 * s.heads_kv, s.head_dim)
+        qkv = self.qkv(self.normed(x)).view(-1, s.heads + 2 * s.heads_kv, s.head_dim)
         q, k, v = qkv.split([s.heads, s.heads_kv, s.heads_kv], 1)
         turned = torch.empty(q.shape, dtype=torch.float32, device="cuda")
         self.cache.append(batch, k, v, q=q, q_out=turned, rope=self.rope, unit=unit)
@@ -124,8 +126,8 @@ class Model:
         self.cache.attention(batch, turned, mixed, s.head_dim ** -0.5, torch.empty(max(need, 16), dtype=torch.uint8, device="cuda"),
                              need, unit=s.unit_x)
         merged = self.merge(mixed.view(-1, s.heads * s.head_dim))
-        x = x + torch.where(merged > wl.P // 2, merged - wl.P, merged).float() * unit
-        return self.head(self.residues(self.norm(x[(starts[1:] - 1).long()])))
+        last = (starts[1:] - 1).long()
+        return self.head(self.normed(x[last], merged[last]))
 
     def answer(self, prompts, temperature=0.8, top_k=40, top_p=0.95, seed=0):
         """Prompts (lists of tokens) -> the tokens that follow, (steps, batch); sequences begin anew"""
@@ -158,8 +160,9 @@ def main():
     ap = argparse.ArgumentParser(description=__doc__, formatter_class=argparse.RawDescriptionHelpFormatter)
     ap.add_argument("--steps", type=int, default=Shape.steps)
     ap.add_argument("--batch", type=int, default=Shape.batch)
+    ap.add_argument("--bits", type=int, default=Shape.bits, choices=(8, 4), help="of a number in the cache")
     a = ap.parse_args()
-    shape = Shape(steps=a.steps, batch=a.batch)
+    shape = Shape(steps=a.steps, batch=a.batch, bits=a.bits)
     prompts = prompts_for(shape)
     shape = dataclasses.replace(shape, context=max(map(len, prompts)) + shape.steps)
     for private in (True, False):
