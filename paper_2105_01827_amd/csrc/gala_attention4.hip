@@ -1,4 +1,6 @@
 // Attention of a batch's queries over the paged 4-bit cache.
+#include <cmath>
+
 #include "gala_attention.h"
 
 using namespace gala;
@@ -7,6 +9,8 @@ namespace {
 
 typedef __bf16 v8b __attribute__((ext_vector_type(8)));
 typedef __bf16 v2b __attribute__((ext_vector_type(2)));
+typedef _Float16 v8h __attribute__((ext_vector_type(8)));
+typedef _Float16 v2h __attribute__((ext_vector_type(2)));
 
 // A head of G x 32 channels is multiplied in G products of 32.  Four lanes (parts) have a token's key: of four groups of 32
 // channels one each, of two left over half a group each, of one left over eight channels each, so that a lane loads 16,
@@ -71,6 +75,21 @@ __device__ __forceinline__ v8b numbers_of(u32 codes, float scale) {
     u.pair[3] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 3);
     return u.all;
 }
+__device__ __forceinline__ v8h halves_of(u32 codes) {
+    union {
+        v2h pair[4];
+        v8h all;
+    } u;
+    u.pair[0] = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(codes, 1.0f, 0);
+    u.pair[1] = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(codes, 1.0f, 1);
+    u.pair[2] = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(codes, 1.0f, 2);
+    u.pair[3] = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(codes, 1.0f, 3);
+    return u.all;
+}
+// what the byte of tile i stands for
+__device__ __forceinline__ float power_of(u32 exponents, int i) {
+    return __uint_as_float((i < 3 ? exponents << (24 - 8 * i) >> 1 : exponents >> 1) & 0x7f800000u);
+}
 // x as the sum of N bfloat16 numbers of eight bits each: the first ones cut off, the last one rounded, so that 8 N bits of x are
 // kept, to half a step
 template <int N>
@@ -91,6 +110,31 @@ __device__ __forceinline__ void parts_of(float (&x)[8], v8b (&to)[N]) {
     for (int k = 0; k < 8; ++k) to[N - 1][k] = (__bf16)x[k];
 }
 
+// A lane's part of a query in NQ bfloat16 parts, 0 for a number that is none; whether all of it, over the four lanes, are numbers
+template <int G, int NQ>
+__device__ __forceinline__ bool load_query(const Attention &a, long row, int hq, int part, v8b (&q)[G][NQ]) {
+    typedef Words<G> W;
+    int fine = 1;
+    auto load = [&](auto type) __attribute__((always_inline)) {
+#pragma unroll
+        for (int n = 0; n < G; ++n) {
+            float x[8];
+            const int d = W::group(n, part) * 32 + W::word(n, part) * 8;
+            load_channels<decltype(type)::value, 1>(a.q, a.pieces, row, hq * a.kv.dim + d, hq * a.kv.dim + a.kv.dim, x);
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                fine &= fabsf(x[k]) < INFINITY;
+                x[k] = fabsf(x[k]) < INFINITY ? x[k] : 0.0f;
+            }
+            parts_of<NQ>(x, q[n]);
+        }
+    };
+    by_type(a.q.type, load);
+    fine &= __shfl_xor(fine, 16);
+    fine &= __shfl_xor(fine, 32);
+    return fine;
+}
+
 // Scores are products of the codes with their powers of two, exact in bfloat16, and of the queries in NQ bfloat16 parts (8 bits
 // each; a query of 8, 11 or 24 bits is all of its parts).  Of a block's scores a lane has 16 of one column's, and they are
 // the very weights that it hands to the second product, because the values' codes lie in that order of tokens: a block goes from memory
@@ -99,7 +143,6 @@ __device__ __forceinline__ void parts_of(float (&x)[8], v8b (&to)[N]) {
 template <int G, int NQ, int NW, int kWaves>
 __global__ __launch_bounds__(64 * kWaves, G <= 4 ? 2 : 1) void kv4_attention_kernel(Attention a) {
     constexpr int NV = 2 * G;                                // tiles of 16 channels of values
-    typedef Words<G> W;
     __shared__ float sums[kWaves][kColumns][NV * 16 + 1];
     __shared__ float stats[kWaves][kColumns][2];
     const KvArgs &kv = a.kv;
@@ -128,28 +171,7 @@ __global__ __launch_bounds__(64 * kWaves, G <= 4 ? 2 : 1) void kv4_attention_ker
     const long row = s.start + qi;
     const int at = s.at_lo - s.col0 / a.group + qi, hq = h * a.group + g;
     v8b q[G][NQ];
-    bool bad;
-    {
-        int fine = 1;
-        auto load = [&](auto type) __attribute__((always_inline)) {
-#pragma unroll
-            for (int n = 0; n < G; ++n) {
-                float x[8];
-                const int d = W::group(n, part) * 32 + W::word(n, part) * 8;
-                load_channels<decltype(type)::value, 1>(a.q, a.pieces, row, hq * kv.dim + d, hq * kv.dim + kv.dim, x);
-#pragma unroll
-                for (int k = 0; k < 8; ++k) {
-                    fine &= fabsf(x[k]) < INFINITY;
-                    x[k] = fabsf(x[k]) < INFINITY ? x[k] : 0.0f;
-                }
-                parts_of<NQ>(x, q[n]);
-            }
-        };
-        by_type(a.q.type, load);
-        fine &= __shfl_xor(fine, 16);
-        fine &= __shfl_xor(fine, 32);
-        bad = !fine;
-    }
+    const bool bad = !load_query<G, NQ>(a, row, hq, part, q);
     const float unit_q = a.scale * kLog2E;
     v4f o[NV];
 #pragma unroll
@@ -178,7 +200,7 @@ __global__ __launch_bounds__(64 * kWaves, G <= 4 ? 2 : 1) void kv4_attention_ker
             v4f acc = v4f{0, 0, 0, 0};
             v8b k[G];
 #pragma unroll
-            for (int n = 0; n < G; ++n) k[n] = numbers_of(keys.code[i][n], __uint_as_float((i < 3 ? keys.exponent[n] << (24 - 8 * i) >> 1 : keys.exponent[n] >> 1) & 0x7f800000u));
+            for (int n = 0; n < G; ++n) k[n] = numbers_of(keys.code[i][n], power_of(keys.exponent[n], i));
 #pragma unroll
             for (int p = NQ - 1; p >= 0; --p)        // the small parts first
 #pragma unroll
@@ -271,17 +293,209 @@ __global__ __launch_bounds__(64 * kWaves, G <= 4 ? 2 : 1) void kv4_attention_ker
     }
 }
 
+// ---- many queries of a sequence ---------------------------------------------------------------------------------------
+// A wavefront has T tiles of 16 queries for all the keys that they see, so that codes are unpacked once for T x 16 queries.  A
+// weight w = p * s, p = exp(score - ...) and s its token's scale of values, comes from one exponential: log2(s) is the score's initial
+// value in the accumulators.  It enters the second product in half precision, raised so that the largest is between 2^7 and 2^15: 11 bits down to
+// 2^-21 of the largest weight times scale, steps of 2^-31 of it below.  The divisor adds up w / s in 32 bits.
+constexpr float kRaised = 7, kHighest = 15;      // exponents
+constexpr float kNothing = 0x1p-64f;             // scale of values that are zeros: their weights count in the divisor
+template <int G, int NQ, int T, int kWaves>
+__global__ __launch_bounds__(64 * kWaves, G <= 4 ? 2 : 1) void kv4_attention_many_kernel(Attention a) {
+    constexpr int NV = 2 * G, kOf = T * kColumns;
+    constexpr size_t kHead = 64 * (33 * G + 2);
+    __shared__ __attribute__((aligned(16))) float of_scales[kWaves][2][kKvBlock];        // log2(s) / unit, 1 / s
+    const KvArgs &kv = a.kv;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 15, part = lane >> 4;
+    // the last queries see most keys: they go first, of all heads
+    int unit = blockIdx.x;
+    const int per_group = kv.count * kv.heads, group = a.tiles - 1 - unit / per_group;
+    unit %= per_group;
+    const int h = unit % kv.heads, b = unit / kv.heads;
+    const Seen s = seen_by(a, b, group * kWaves + wave, kOf);
+    if (!s.cols) return;
+    int at[T];
+    v8b q[T][G][NQ];
+    bool bad[T];
+#pragma unroll
+    for (int k = 0; k < T; ++k) {
+        const int c = s.col0 + min(k * kColumns + col, s.cols - 1), qi = c / a.group;
+        at[k] = s.at_lo - s.col0 / a.group + qi;
+        bad[k] = !load_query<G, NQ>(a, s.start + qi, h * a.group + c % a.group, part, q[k]);
+    }
+    const float unit_q = a.scale * kLog2E, per_unit = 1.0f / unit_q;
+    v4f o[T][NV];
+    float base[T], limit[T], sum[T];                  // limit: what an exponent may be before the base is raised
+#pragma unroll
+    for (int k = 0; k < T; ++k) {
+        base[k] = sum[k] = 0, limit[k] = -INFINITY;
+#pragma unroll
+        for (int j = 0; j < NV; ++j) o[k][j] = v4f{0, 0, 0, 0};
+    }
+    Keys<G> keys;
+    u32 scale;
+    auto page_at = [&](int u) { return u < s.total ? page_of(kv, b, s.block(u)) : -1; };
+    auto data_of = [&](int page) { return (const char *)kv.codes + ((size_t)max(page, 0) * kv.heads + h) * kHead; };
+    // tokens in the order of the scales' places, a lane each
+    const int of_lane = (lane & 15) / 4 * 16 + (lane >> 4) * 4 + (lane & 3);
+    auto load = [&](int page) __attribute__((always_inline)) {
+        const char *data = data_of(page);
+        load_keys<G>(data, col, part, keys);
+        scale = *(const unsigned short *)(data + kv4_scales(G) + of_lane * 2);
+    };
+    int page = page_at(0), page_next = page_at(1);
+    if (s.total) load(page);
+    for (int u = 0; u < s.total; ++u) {
+        const int block = s.block(u), end = page < 0 ? 0 : kv.max_len, t0 = block * kKvBlock;
+        const char *data = data_of(page);
+        u32 values[G][4];
+#pragma unroll
+        for (int j = 0; j < G; ++j) {
+            const int4 x = *(const int4 *)(data + 1024 * G + j * 1024 + lane * 16);
+            values[j][0] = x.x, values[j][1] = x.y, values[j][2] = x.z, values[j][3] = x.w;
+        }
+        {
+            // what is no scale of a number belongs to a token that is not seen, or to zeros
+            const float given = __uint_as_float(scale << 16), held = given >= 0x1p-100f && given < INFINITY ? given : kNothing;
+            of_scales[wave][0][lane] = __builtin_amdgcn_logf(held) * per_unit;
+            of_scales[wave][1][lane] = 1.0f / held;
+            __builtin_amdgcn_wave_barrier();                 // a wavefront's own: its instructions on LDS are done in order
+        }
+        v4f acc[T][4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const v4f start = *(const v4f *)&of_scales[wave][0][i * 16 + part * 4];
+            v8b k[G];
+#pragma unroll
+            for (int n = 0; n < G; ++n) k[n] = numbers_of(keys.code[i][n], power_of(keys.exponent[n], i));
+#pragma unroll
+            for (int t = 0; t < T; ++t) {
+                acc[t][i] = start;
+#pragma unroll
+                for (int p = NQ - 1; p >= 0; --p)
+#pragma unroll
+                    for (int n = 0; n < G; ++n) acc[t][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k[n], q[t][n][p], acc[t][i], 0, 0, 0);
+            }
+        }
+        v4f inverse[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) inverse[i] = *(const v4f *)&of_scales[wave][1][i * 16 + part * 4];
+        page = page_next;
+        load(page);
+        page_next = page_at(u + 2);
+        const bool edge = t0 + 63 > s.at_lo || t0 + 64 > end || (a.window && t0 <= s.at_hi - a.window);
+        v8h w[T][2];
+#pragma unroll
+        for (int t = 0; t < T; ++t) {
+            float most = -INFINITY;
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) acc[t][i][r] = fmaf(acc[t][i][r], unit_q, -base[t]);
+            if (edge) {
+                const int own = t0 + part * 4, hi = min(at[t], end - 1) - own;
+                const int lo = a.window ? at[t] - a.window + 1 - own : -kKvBlock, sinks = a.window ? a.sinks - own : 0;
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) {
+                        const int e = i * 16 + r;
+                        acc[t][i][r] = (e <= hi) & ((e >= lo) | (e < sinks)) ? acc[t][i][r] : -INFINITY;
+                    }
+            }
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) most = fmaxf(most, acc[t][i][r]);
+            if (__any(most > limit[t])) {
+                most = fmaxf(most, __shfl_xor(most, 16));
+                most = fmaxf(most, __shfl_xor(most, 32));
+                if (most > limit[t] || most > kRaised) {
+                    most -= kRaised;
+                    const float was = limit[t] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(-most);          // nothing yet with the first base
+                    base[t] += most;
+                    limit[t] = kHighest;
+                    sum[t] *= was;
+#pragma unroll
+                    for (int j = 0; j < NV; ++j) o[t][j] *= was;
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) acc[t][i] -= most;
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    const float x = __builtin_amdgcn_exp2f(acc[t][i][r]);
+                    sum[t] = fmaf(x, inverse[i][r], sum[t]);
+                    w[t][i >> 1][(i & 1) * 4 + r] = (_Float16)x;
+                }
+        }
+#pragma unroll
+        for (int j = 0; j < NV; ++j)
+#pragma unroll
+            for (int half = 0; half < 2; ++half) {
+                const v8h v = halves_of(values[j >> 1][(j & 1) * 2 + half]);
+#pragma unroll
+                for (int t = 0; t < T; ++t) o[t][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, w[t][half], o[t][j], 0, 0, 0);
+            }
+    }
+#pragma unroll
+    for (int t = 0; t < T; ++t) {
+        float all = sum[t];
+        all += __shfl_xor(all, 16);
+        all += __shfl_xor(all, 32);
+        const float f = bad[t] ? __builtin_nanf("") : all > 0 ? 1.0f / all : 0.0f;
+        if (t * kColumns + col >= s.cols) continue;
+        const int c = s.col0 + t * kColumns + col, column = (h * a.group + c % a.group) * kv.dim + part * 4;
+        const long row = s.start + c / a.group;
+#pragma unroll
+        for (int j = 0; j < NV; ++j) {
+            const int d = j * 16 + part * 4;
+            if (d + 4 <= kv.dim && a.out_quads) {
+                auto store = [&](auto type) __attribute__((always_inline)) {
+                    typedef typename Element<decltype(type)::value>::type E;
+                    struct alignas(4 * sizeof(E) < 16 ? 4 * sizeof(E) : 16) Quad {
+                        E e[4];
+                    } quad;
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) quad.e[r] = from_float<decltype(type)::value>(o[t][j][r] * f, a.out.unit, a.out.p);
+                    *(Quad *)((E *)a.out.data + row * a.out.stride + column + j * 16) = quad;
+                };
+                if (a.out.type == GALA_F16)
+                    store(std::integral_constant<int, GALA_F16>());
+                else
+                    store(std::integral_constant<int, GALA_BF16>());
+            } else {
+#pragma unroll
+                for (int r = 0; r < 4; ++r)
+                    if (d + r < kv.dim) store_any(a.out, row, column + j * 16 + r, o[t][j][r] * f);
+            }
+        }
+    }
+}
+
 // How a call is cut up.
+constexpr int kWavesOf = 4;
+constexpr int tiles_of(int groups) { return groups <= 4 ? 2 : 1; }       // of a wavefront
 struct Cut {
+    bool many;
     int tiles, splits, columns;
     long places() const { return (long)tiles * splits * columns; }
 };
-Cut cut_of(const KvArgs &kv, int heads_q, int window, int sinks) {
+Cut cut_of(const KvArgs &kv, int heads_q, int window, int sinks, bool fine) {
     Cut c;
     const long columns = (long)kv.max_new * (heads_q / kv.heads);
     const long reach = std::min<long>(kv.max_len, (long)kv.table_stride * kKvBlock);
     const long keys = window ? std::min(reach, (long)window + kv.max_new + sinks + 2 * kKvBlock) : reach;
     const long blocks = std::max(1l, (keys + kKvBlock - 1) / kKvBlock);
+    const int of_group = tiles_of(kv4_groups(kv.dim)) * kWavesOf * kColumns;
+    const long groups = (columns + of_group - 1) / of_group * kv.count * kv.heads;
+    c.many = !fine && columns >= of_group && (groups >= 192 || blocks <= 16);
+    if (c.many) {
+        c.tiles = (int)((columns + of_group - 1) / of_group), c.splits = 1, c.columns = 0;
+        return c;
+    }
     c.tiles = (int)((columns + kColumns - 1) / kColumns);
     c.columns = (int)std::min<long>(columns, kColumns);
     const long units = std::max(1l, (long)kv.count * kv.heads * c.tiles);
@@ -294,18 +508,22 @@ Cut cut_of(const KvArgs &kv, int heads_q, int window, int sinks) {
 namespace gala {
 
 size_t kv4_attention_workspace(const KvArgs &kv, int heads_q, int window, int sinks) {
-    const Cut c = cut_of(kv, heads_q, window, sinks);
+    const Cut c = cut_of(kv, heads_q, window, sinks, true);          // the other way needs none
     return c.splits == 1 ? 0 : (size_t)kv.count * kv.heads * c.places() * (kv.dim + 2) * sizeof(float);
 }
 
 int launch_kv4_attention(void *stream, const KvArgs &kv, int heads_q, float scale, int window, int sinks, const Values &q,
                          const Values &out, void *workspace) {
     const bool fine = q.type == GALA_F32 || q.type == GALA_RESIDUE || out.type == GALA_F32 || out.type == GALA_RESIDUE;
-    const Cut c = cut_of(kv, heads_q, window, sinks);
+    // a score times log2(e) and the logarithm of a scale share an accumulator: neither may drown the other
+    const float unit = std::fabs(scale) * kLog2E;
+    const Cut c = cut_of(kv, heads_q, window, sinks, fine || !(unit >= 0x1p-20f && unit <= 0x1p20f));
     Attention a{};
     a.kv = kv, a.q = q, a.out = out;
     const size_t size = q.type == GALA_F32 ? 4 : q.type == GALA_RESIDUE ? 8 : 2;
     a.pieces = (uintptr_t)q.data % 16 == 0 && q.stride * size % 16 == 0 && kv.dim % 8 == 0;
+    const size_t of_out = out.type == GALA_F32 ? 4 : out.type == GALA_RESIDUE ? 8 : 2, quad = std::min<size_t>(4 * of_out, 16);
+    a.out_quads = (uintptr_t)out.data % quad == 0 && out.stride * of_out % quad == 0 && kv.dim % 4 == 0;
     a.heads_q = heads_q, a.group = heads_q / kv.heads;
     a.scale = scale, a.window = window, a.sinks = sinks;
     a.tiles = c.tiles, a.splits = c.splits, a.columns = c.columns;
@@ -314,6 +532,17 @@ int launch_kv4_attention(void *stream, const KvArgs &kv, int heads_q, float scal
     const unsigned groups = (unsigned)((long)kv.count * kv.heads * c.tiles * c.splits);
     auto launch = [&](auto n32) {
         constexpr int G = decltype(n32)::value;
+        if (c.many) {
+            auto many = [&](auto parts) {
+                hipLaunchKernelGGL((kv4_attention_many_kernel<G, decltype(parts)::value, tiles_of(G), kWavesOf>), dim3(groups), dim3(64 * kWavesOf), 0,
+                                   (hipStream_t)stream, a);
+            };
+            if (q.type == GALA_F16)
+                many(std::integral_constant<int, 2>());
+            else
+                many(std::integral_constant<int, 1>());
+            return;
+        }
         auto waves = [&](auto w) {
             constexpr int W = decltype(w)::value;
             a.waves = W;

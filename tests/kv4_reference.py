@@ -87,12 +87,19 @@ def key_values(codes, exponents, head_dim):
     return x[..., :head_dim]
 
 
+def scales_of(page, head_dim):
+    """the values' scales of a head's part of a page"""
+    s = places(head_dim)[3]
+    bits = (page[s].astype(np.uint32) << 16) | (page[s + 1].astype(np.uint32) << 24)
+    return np.where((bits & 0x7f800000) == 0x7f800000, np.uint32(0x7fc00000), bits).astype(np.uint32).view(np.float32).astype(np.float64)
+
+
 def read(page, head_dim):
     """a head's part of a page (head_bytes,) uint8 -> keys and values (64, head_dim), in 64 bits"""
     k, v, e, s = places(head_dim)
     d, t = np.arange(k.shape[1])[None, :], np.arange(BLOCK)[:, None]
     kc, vc = page[k] >> 4 * (d % 2) & 15, page[v] >> 4 * (t % 2) & 15
-    scale = ((page[s].astype(np.uint32) << 16) | (page[s + 1].astype(np.uint32) << 24)).view(np.float32).astype(np.float64)
+    scale = scales_of(page, head_dim)
     keys = VALUES[kc] * np.repeat(np.ldexp(1.0, page[e].astype(int) - 127), 32, -1)
     return keys[:, :head_dim], (VALUES[vc] * scale[:, None])[:, :head_dim]
 
@@ -139,6 +146,24 @@ def attention(q, k, v, seen, scale, parts_q, parts_w):
     rel = np.expm1(2 * slack) + 2.0 ** -(8 * parts_w)
     spread = (w[:, None] * np.abs(v)).sum(0) / w.sum()
     return out, 2 * rel * spread + (len(w) * parts_w + 64) * u * spread
+
+
+def attention_in_halves(q, k, v, scales, seen, scale, parts_q):
+    """The same with weights times scales of values (`scales`, a token each) in half precision: rounded by at most 2^-11 of
+    themselves, or by half a step of 2^-31 of the largest of them; the scale's logarithm is one more term of a score's sum."""
+    dim = len(q)
+    if not seen.any():
+        return np.zeros(dim), np.zeros(dim)
+    k, v, scales = k[seen], v[seen], scales[seen]
+    s = scale * (k @ q)
+    w = np.exp(s - s.max())
+    out = (w[:, None] * v).sum(0) / w.sum()
+    u = 2.0 ** -24
+    size = abs(scale) * (np.abs(k) @ np.abs(q)).max() + np.abs(np.log(np.where(scales > 0, scales, 2.0 ** -64))).max()
+    slack = (dim * parts_q + 16) * u * size + 8 * u * (np.abs(s).max() + 1)
+    spread = (w[:, None] * np.abs(v)).sum(0) / w.sum()
+    bound = 2 * np.expm1(2 * slack) * spread + 2.0 ** -11 * spread + (len(w) + 64) * u * spread
+    return out, bound + len(w) * 6 * 2.0 ** -32 * (w * scales).max() / w.sum()
 
 
 def rms_norm(x, add, weight, epsilon):

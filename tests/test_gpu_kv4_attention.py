@@ -83,6 +83,7 @@ class Case:
             with np.errstate(invalid="ignore"):
                 held = [[ref.read(data[p if fine else 0, h], self.dim) for p, fine in zip(pages, ok)] for h in range(self.heads)]
             k, v = (np.stack([np.concatenate([x[i] for x in of]) for of in held]) for i in range(2))
+            scales = np.stack([np.concatenate([ref.scales_of(data[p if fine else 0, h], self.dim) for p, fine in zip(pages, ok)]) for h in range(self.heads)])
             there = np.repeat(ok, 64)[:end]
             for i in range(n):
                 row = self.starts[b] + i
@@ -97,8 +98,12 @@ class Case:
                     if not np.isfinite(q[row, h]).all():
                         assert np.isnan(got[row, h]).all()
                         continue
-                    want, bound = ref.attention(q[row, h], k[h // self.group, :tokens], v[h // self.group, :tokens], seen, self.scale,
-                                                PARTS_Q[self.kind] if parts_w == 2 else 3, parts_w)
+                    of = k[h // self.group, :tokens], v[h // self.group, :tokens]
+                    parts_q = PARTS_Q[self.kind] if parts_w == 2 else 3
+                    if parts_w == 2 and min(max(self.new), max_new) * self.group >= 64:
+                        want, bound = ref.attention_in_halves(q[row, h], *of, scales[h // self.group, :tokens], seen, self.scale, parts_q)
+                    else:
+                        want, bound = ref.attention(q[row, h], *of, seen, self.scale, parts_q, parts_w)
                     # one rounding to the output's type; half precision's smallest step
                     bound = bound + EPS.get(self.out_kind, 0) * (np.abs(want) + bound) + (UNIT / 2 if self.out_kind == "residue" else 0) + 2.0 ** -25
                     over = np.abs(got[row, h] - want) / bound
