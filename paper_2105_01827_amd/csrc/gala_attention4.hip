@@ -294,53 +294,108 @@ __global__ __launch_bounds__(64 * kWaves, G <= 4 ? 2 : 1) void kv4_attention_ker
 }
 
 // ---- many queries of a sequence ---------------------------------------------------------------------------------------
-// A wavefront has T tiles of 16 queries for all the keys that they see, so that codes are unpacked once for T x 16 queries.  A
+// A wavefront has 32 queries for all the keys that they see, in products of 32 x 32: those of 16 x 16 reach 0.7 of their rate, and
+// leave less room for the vector ALU between them (23 cycles for half the work, 31 with four multiply-adds; 33 and 35).  A
 // weight w = p * s, p = exp(score - ...) and s its token's scale of values, comes from one exponential: log2(s) is the score's initial
 // value in the accumulators.  It enters the second product in half precision, raised so that the largest is between 2^7 and 2^15: 11 bits down to
 // 2^-21 of the largest weight times scale, steps of 2^-31 of it below.  The divisor adds up w / s in 32 bits.
 constexpr float kRaised = 7, kHighest = 15;      // exponents
 constexpr float kNothing = 0x1p-64f;             // scale of values that are zeros: their weights count in the divisor
-template <int G, int NQ, int T, int kWaves>
+constexpr int kWide = 32;
+
+// Two lanes (halves) have a token's key: of two groups of 32 channels one each, of one left over half.  Product n takes their n-th words.
+template <int G>
+struct WideWords {
+    static constexpr int kTwos = G / 2;
+    static __device__ __forceinline__ int group(int n, int half) { return n < 4 * kTwos ? n / 4 * 2 + half : G - 1; }
+    static __device__ __forceinline__ int word(int n, int half) { return n < 4 * kTwos ? n & 3 : 2 * half + (n & 1); }
+};
+template <int G>
+struct WideKeys {
+    u32 code[2][2 * G];              // of two tiles of 32 tokens
+    u32 exponent[(G + 1) / 2];       // bytes of all tiles of 16
+};
+template <int G>
+__device__ __forceinline__ void load_keys(const char *data, int token, int half, WideKeys<G> &k) {
+    typedef WideWords<G> W;
+    const int low = token & 15, high = token >> 4;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        const char *tile = data + (2 * i + high) * G * 256 + low * 16;
+#pragma unroll
+        for (int n = 0; n < 4 * W::kTwos; n += 4) {
+            const int4 x = *(const int4 *)(tile + W::group(n, half) * 256);
+            k.code[i][n] = x.x, k.code[i][n + 1] = x.y, k.code[i][n + 2] = x.z, k.code[i][n + 3] = x.w;
+        }
+        if constexpr (G & 1) {
+            const int2 x = *(const int2 *)(tile + (G - 1) * 256 + half * 8);
+            k.code[i][2 * G - 2] = x.x, k.code[i][2 * G - 1] = x.y;
+        }
+    }
+#pragma unroll
+    for (int n = 0; n < (G + 1) / 2; ++n)         // the wanted bytes: the first, and the third for the second tile
+        k.exponent[n] = *(const u32 *)(data + kv4_exponents(G) + W::group(4 * n, half) * 64 + low * 4) >> 8 * high;
+}
+
+template <int G, int NQ, int kWaves>
 __global__ __launch_bounds__(64 * kWaves, G <= 4 ? 2 : 1) void kv4_attention_many_kernel(Attention a) {
-    constexpr int NV = 2 * G, kOf = T * kColumns;
+    typedef float v16f __attribute__((ext_vector_type(16)));
+    typedef WideWords<G> W;
     constexpr size_t kHead = 64 * (33 * G + 2);
     __shared__ __attribute__((aligned(16))) float of_scales[kWaves][2][kKvBlock];        // log2(s) / unit, 1 / s
     const KvArgs &kv = a.kv;
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 15, part = lane >> 4;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 31, half = lane >> 5;
     // the last queries see most keys: they go first, of all heads
     int unit = blockIdx.x;
     const int per_group = kv.count * kv.heads, group = a.tiles - 1 - unit / per_group;
     unit %= per_group;
     const int h = unit % kv.heads, b = unit / kv.heads;
-    const Seen s = seen_by(a, b, group * kWaves + wave, kOf);
+    const Seen s = seen_by(a, b, group * kWaves + wave, kWide);
     if (!s.cols) return;
-    int at[T];
-    v8b q[T][G][NQ];
-    bool bad[T];
+    const int mine = s.col0 + min(col, s.cols - 1), qi = mine / a.group, hq = h * a.group + mine % a.group;
+    const long row = s.start + qi;
+    const int at = s.at_lo - s.col0 / a.group + qi;
+    v8b q[2 * G][NQ];
+    bool bad;
+    {
+        int fine = 1;
+        auto load = [&](auto type) __attribute__((always_inline)) {
 #pragma unroll
-    for (int k = 0; k < T; ++k) {
-        const int c = s.col0 + min(k * kColumns + col, s.cols - 1), qi = c / a.group;
-        at[k] = s.at_lo - s.col0 / a.group + qi;
-        bad[k] = !load_query<G, NQ>(a, s.start + qi, h * a.group + c % a.group, part, q[k]);
+            for (int n = 0; n < 2 * G; ++n) {
+                float x[8];
+                load_channels<decltype(type)::value, 1>(a.q, a.pieces, row, hq * kv.dim + W::group(n, half) * 32 + W::word(n, half) * 8, hq * kv.dim + kv.dim, x);
+#pragma unroll
+                for (int k = 0; k < 8; ++k) {
+                    fine &= fabsf(x[k]) < INFINITY;
+                    x[k] = fabsf(x[k]) < INFINITY ? x[k] : 0.0f;
+                }
+                parts_of<NQ>(x, q[n]);
+            }
+        };
+        if (a.q.type == GALA_F16)
+            load(std::integral_constant<int, GALA_F16>());
+        else
+            load(std::integral_constant<int, GALA_BF16>());
+        fine &= __shfl_xor(fine, 32);
+        bad = !fine;
     }
     const float unit_q = a.scale * kLog2E, per_unit = 1.0f / unit_q;
-    v4f o[T][NV];
-    float base[T], limit[T], sum[T];                  // limit: what an exponent may be before the base is raised
+    v16f o[G];
+    float base = 0, limit = -INFINITY, sum = 0;       // limit: what an exponent may be before the base is raised
 #pragma unroll
-    for (int k = 0; k < T; ++k) {
-        base[k] = sum[k] = 0, limit[k] = -INFINITY;
+    for (int j = 0; j < G; ++j)
 #pragma unroll
-        for (int j = 0; j < NV; ++j) o[k][j] = v4f{0, 0, 0, 0};
-    }
-    Keys<G> keys;
+        for (int r = 0; r < 16; ++r) o[j][r] = 0;
+    WideKeys<G> keys;
     u32 scale;
     auto page_at = [&](int u) { return u < s.total ? page_of(kv, b, s.block(u)) : -1; };
+    // without a page the first one is read and not seen: no branch around what is under way
     auto data_of = [&](int page) { return (const char *)kv.codes + ((size_t)max(page, 0) * kv.heads + h) * kHead; };
     // tokens in the order of the scales' places, a lane each
     const int of_lane = (lane & 15) / 4 * 16 + (lane >> 4) * 4 + (lane & 3);
     auto load = [&](int page) __attribute__((always_inline)) {
         const char *data = data_of(page);
-        load_keys<G>(data, col, part, keys);
+        load_keys<G>(data, col, half, keys);
         scale = *(const unsigned short *)(data + kv4_scales(G) + of_lane * 2);
     };
     int page = page_at(0), page_next = page_at(1);
@@ -348,136 +403,138 @@ __global__ __launch_bounds__(64 * kWaves, G <= 4 ? 2 : 1) void kv4_attention_man
     for (int u = 0; u < s.total; ++u) {
         const int block = s.block(u), end = page < 0 ? 0 : kv.max_len, t0 = block * kKvBlock;
         const char *data = data_of(page);
-        u32 values[G][4];
+        // of 16 tokens that a lane's scores of a tile are: those of the first and third four, of the second and fourth
+        u32 values[G][2][2];
 #pragma unroll
-        for (int j = 0; j < G; ++j) {
-            const int4 x = *(const int4 *)(data + 1024 * G + j * 1024 + lane * 16);
-            values[j][0] = x.x, values[j][1] = x.y, values[j][2] = x.z, values[j][3] = x.w;
-        }
+        for (int j = 0; j < G; ++j)
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+                const int2 x = *(const int2 *)(data + 1024 * G + j * 1024 + ((half + 2 * k) * 16 + (col & 15)) * 16 + (col >> 4) * 8);
+                values[j][0][k] = x.x, values[j][1][k] = x.y;
+            }
         {
             // what is no scale of a number belongs to a token that is not seen, or to zeros
             const float given = __uint_as_float(scale << 16), held = given >= 0x1p-100f && given < INFINITY ? given : kNothing;
             of_scales[wave][0][lane] = __builtin_amdgcn_logf(held) * per_unit;
-            of_scales[wave][1][lane] = 1.0f / held;
+            of_scales[wave][1][lane] = __builtin_amdgcn_rcpf(held);
             __builtin_amdgcn_wave_barrier();                 // a wavefront's own: its instructions on LDS are done in order
         }
-        v4f acc[T][4];
+        v16f acc[2];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const v4f start = *(const v4f *)&of_scales[wave][0][i * 16 + part * 4];
-            v8b k[G];
+        for (int i = 0; i < 2; ++i) {
 #pragma unroll
-            for (int n = 0; n < G; ++n) k[n] = numbers_of(keys.code[i][n], power_of(keys.exponent[n], i));
+            for (int k = 0; k < 4; ++k) {
+                const v4f x = *(const v4f *)&of_scales[wave][0][i * 32 + k * 8 + half * 4];
 #pragma unroll
-            for (int t = 0; t < T; ++t) {
-                acc[t][i] = start;
-#pragma unroll
-                for (int p = NQ - 1; p >= 0; --p)
-#pragma unroll
-                    for (int n = 0; n < G; ++n) acc[t][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k[n], q[t][n][p], acc[t][i], 0, 0, 0);
+                for (int r = 0; r < 4; ++r) acc[i][4 * k + r] = x[r];
             }
         }
-        v4f inverse[4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) inverse[i] = *(const v4f *)&of_scales[wave][1][i * 16 + part * 4];
+        for (int n = 0; n < 2 * G; ++n)
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                const u32 e = keys.exponent[n < 4 * W::kTwos ? n / 4 : W::kTwos];
+                const v8b k = numbers_of(keys.code[i][n], __uint_as_float(i ? e << 7 & 0x7f800000u : e << 23));
+#pragma unroll
+                for (int p = NQ - 1; p >= 0; --p) acc[i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k, q[n][p], acc[i], 0, 0, 0);
+            }
         page = page_next;
         load(page);
         page_next = page_at(u + 2);
-        const bool edge = t0 + 63 > s.at_lo || t0 + 64 > end || (a.window && t0 <= s.at_hi - a.window);
-        v8h w[T][2];
 #pragma unroll
-        for (int t = 0; t < T; ++t) {
-            float most = -INFINITY;
+        for (int i = 0; i < 2; ++i)
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
+            for (int r = 0; r < 16; ++r) acc[i][r] = fmaf(acc[i][r], unit_q, -base);
+        if (t0 + 63 > s.at_lo || t0 + 64 > end || (a.window && t0 <= s.at_hi - a.window)) {
+            const int own = t0 + half * 4, hi = min(at, end - 1) - own;
+            const int lo = a.window ? at - a.window + 1 - own : -kKvBlock, sinks = a.window ? a.sinks - own : 0;
 #pragma unroll
-                for (int r = 0; r < 4; ++r) acc[t][i][r] = fmaf(acc[t][i][r], unit_q, -base[t]);
-            if (edge) {
-                const int own = t0 + part * 4, hi = min(at[t], end - 1) - own;
-                const int lo = a.window ? at[t] - a.window + 1 - own : -kKvBlock, sinks = a.window ? a.sinks - own : 0;
+            for (int i = 0; i < 2; ++i)
 #pragma unroll
-                for (int i = 0; i < 4; ++i)
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) {
-                        const int e = i * 16 + r;
-                        acc[t][i][r] = (e <= hi) & ((e >= lo) | (e < sinks)) ? acc[t][i][r] : -INFINITY;
-                    }
-            }
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-#pragma unroll
-                for (int r = 0; r < 4; ++r) most = fmaxf(most, acc[t][i][r]);
-            if (__any(most > limit[t])) {
-                most = fmaxf(most, __shfl_xor(most, 16));
-                most = fmaxf(most, __shfl_xor(most, 32));
-                if (most > limit[t] || most > kRaised) {
-                    most -= kRaised;
-                    const float was = limit[t] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(-most);          // nothing yet with the first base
-                    base[t] += most;
-                    limit[t] = kHighest;
-                    sum[t] *= was;
-#pragma unroll
-                    for (int j = 0; j < NV; ++j) o[t][j] *= was;
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) acc[t][i] -= most;
+                for (int r = 0; r < 16; ++r) {
+                    const int e = i * 32 + r / 4 * 8 + r % 4;
+                    acc[i][r] = (e <= hi) & ((e >= lo) | (e < sinks)) ? acc[i][r] : -INFINITY;
                 }
-            }
+        }
+        float most = -INFINITY;
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) most = fmaxf(most, acc[i][r]);
+        if (__any(most > limit)) {
+            most = fmaxf(most, __shfl_xor(most, 32));
+            if (most > limit || most > kRaised) {
+                most -= kRaised;
+                const float was = limit == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(-most);          // nothing yet with the first base
+                base += most;
+                limit = kHighest;
+                sum *= was;
+#pragma unroll
+                for (int j = 0; j < G; ++j) o[j] *= was;
+#pragma unroll
+                for (int i = 0; i < 2; ++i) acc[i] -= most;
+            }
+        }
+        v8h w[2][2];
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const v4f inverse = *(const v4f *)&of_scales[wave][1][i * 32 + k * 8 + half * 4];
 #pragma unroll
                 for (int r = 0; r < 4; ++r) {
-                    const float x = __builtin_amdgcn_exp2f(acc[t][i][r]);
-                    sum[t] = fmaf(x, inverse[i][r], sum[t]);
-                    w[t][i >> 1][(i & 1) * 4 + r] = (_Float16)x;
+                    const float x = __builtin_amdgcn_exp2f(acc[i][4 * k + r]);
+                    sum = fmaf(x, inverse[r], sum);
+                    w[i][k & 1][(k >> 1) * 4 + r] = (_Float16)x;
                 }
-        }
-#pragma unroll
-        for (int j = 0; j < NV; ++j)
-#pragma unroll
-            for (int half = 0; half < 2; ++half) {
-                const v8h v = halves_of(values[j >> 1][(j & 1) * 2 + half]);
-#pragma unroll
-                for (int t = 0; t < T; ++t) o[t][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, w[t][half], o[t][j], 0, 0, 0);
             }
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+            for (int k = 0; k < 2; ++k)
+#pragma unroll
+                for (int j = 0; j < G; ++j) o[j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(halves_of(values[j][i][k]), w[i][k], o[j], 0, 0, 0);
     }
+    sum += __shfl_xor(sum, 32);
+    const float f = bad ? __builtin_nanf("") : sum > 0 ? 1.0f / sum : 0.0f;
+    if (col >= s.cols) return;
+    auto store = [&](auto type) __attribute__((always_inline)) {
+        constexpr int T = decltype(type)::value;
+        typedef typename Element<T>::type E;
+        struct alignas(4 * sizeof(E)) Quad {
+            E e[4];
+        };
 #pragma unroll
-    for (int t = 0; t < T; ++t) {
-        float all = sum[t];
-        all += __shfl_xor(all, 16);
-        all += __shfl_xor(all, 32);
-        const float f = bad[t] ? __builtin_nanf("") : all > 0 ? 1.0f / all : 0.0f;
-        if (t * kColumns + col >= s.cols) continue;
-        const int c = s.col0 + t * kColumns + col, column = (h * a.group + c % a.group) * kv.dim + part * 4;
-        const long row = s.start + c / a.group;
+        for (int j = 0; j < G; ++j)
 #pragma unroll
-        for (int j = 0; j < NV; ++j) {
-            const int d = j * 16 + part * 4;
-            if (d + 4 <= kv.dim && a.out_quads) {
-                auto store = [&](auto type) __attribute__((always_inline)) {
-                    typedef typename Element<decltype(type)::value>::type E;
-                    struct alignas(4 * sizeof(E) < 16 ? 4 * sizeof(E) : 16) Quad {
-                        E e[4];
-                    } quad;
+            for (int k = 0; k < 4; ++k) {
+                const int d = j * 32 + k * 8 + half * 4;
+                float x[4];
 #pragma unroll
-                    for (int r = 0; r < 4; ++r) quad.e[r] = from_float<decltype(type)::value>(o[t][j][r] * f, a.out.unit, a.out.p);
-                    *(Quad *)((E *)a.out.data + row * a.out.stride + column + j * 16) = quad;
-                };
-                if (a.out.type == GALA_F16)
-                    store(std::integral_constant<int, GALA_F16>());
-                else
-                    store(std::integral_constant<int, GALA_BF16>());
-            } else {
+                for (int r = 0; r < 4; ++r) {
+                    x[r] = o[j][4 * k + r] * f;
+                    asm("" : "+v"(x[r]));            // rounded to 32 bits first, wherever the row lies
+                }
+                if (d + 4 <= kv.dim && a.out_quads) {
+                    Quad quad;
 #pragma unroll
-                for (int r = 0; r < 4; ++r)
-                    if (d + r < kv.dim) store_any(a.out, row, column + j * 16 + r, o[t][j][r] * f);
+                    for (int r = 0; r < 4; ++r) quad.e[r] = (E)x[r];
+                    *(Quad *)((E *)a.out.data + row * a.out.stride + hq * kv.dim + d) = quad;
+                } else {
+#pragma unroll
+                    for (int r = 0; r < 4; ++r)
+                        if (d + r < kv.dim) store_value<T>(a.out, row, hq * kv.dim + d + r, x[r]);
+                }
             }
-        }
-    }
+    };
+    if (a.out.type == GALA_F16)
+        store(std::integral_constant<int, GALA_F16>());
+    else
+        store(std::integral_constant<int, GALA_BF16>());
 }
 
 // How a call is cut up.
 constexpr int kWavesOf = 4;
-constexpr int tiles_of(int groups) { return groups <= 4 ? 2 : 1; }       // of a wavefront
 struct Cut {
     bool many;
     int tiles, splits, columns;
@@ -489,7 +546,7 @@ Cut cut_of(const KvArgs &kv, int heads_q, int window, int sinks, bool fine) {
     const long reach = std::min<long>(kv.max_len, (long)kv.table_stride * kKvBlock);
     const long keys = window ? std::min(reach, (long)window + kv.max_new + sinks + 2 * kKvBlock) : reach;
     const long blocks = std::max(1l, (keys + kKvBlock - 1) / kKvBlock);
-    const int of_group = tiles_of(kv4_groups(kv.dim)) * kWavesOf * kColumns;
+    const int of_group = kWide * kWavesOf;
     const long groups = (columns + of_group - 1) / of_group * kv.count * kv.heads;
     c.many = !fine && columns >= of_group && (groups >= 192 || blocks <= 16);
     if (c.many) {
@@ -534,7 +591,7 @@ int launch_kv4_attention(void *stream, const KvArgs &kv, int heads_q, float scal
         constexpr int G = decltype(n32)::value;
         if (c.many) {
             auto many = [&](auto parts) {
-                hipLaunchKernelGGL((kv4_attention_many_kernel<G, decltype(parts)::value, tiles_of(G), kWavesOf>), dim3(groups), dim3(64 * kWavesOf), 0,
+                hipLaunchKernelGGL((kv4_attention_many_kernel<G, decltype(parts)::value, kWavesOf>), dim3(groups), dim3(64 * kWavesOf), 0,
                                    (hipStream_t)stream, a);
             };
             if (q.type == GALA_F16)
