@@ -269,16 +269,31 @@ def _heads_values(t, heads, head_dim, unit, what):
     return values, shape[0], numbers // head_dim
 
 
-def _row_values(t, rows, width, unit, what, codes=False):
-    """gala_values of `rows` rows of `width` numbers on the GPU; int8 where a call writes codes"""
-    if t.shape[0] != rows or math.prod(t.shape[1:]) != width:
-        raise ValueError(f"{what} has to hold {rows} rows of {width} numbers, not {tuple(t.shape)}")
+def _row_values(t, shape, unit, what, codes=False):
+    """gala_values of rows of numbers on the GPU, of `shape` (rows, width); int8 where a call writes codes"""
+    kind = 4 if codes and t.dtype is _named.get("torch.int8") else _types.get(t.dtype)
+    if kind is not None and t.shape == shape:
+        strides = t.stride()
+        if strides[1] == 1 and t.is_cuda:                                     # as they mostly are
+            return _pack_values(t.data_ptr(), strides[0], kind, unit)
+    if t.shape[0] != shape[0] or math.prod(t.shape[1:]) != shape[1]:
+        raise ValueError(f"{what} has to hold {shape[0]} rows of {shape[1]} numbers, not {tuple(t.shape)}")
     _on_gpu(t, what)
     if codes and str(t.dtype) == "torch.int8":
+        _named["torch.int8"] = t.dtype
         if not t[:1].is_contiguous():
             raise ValueError("the values of a row have to be contiguous")
         return _pack_values(t.data_ptr(), t.stride(0), 4, unit)
     return _values(t, unit)
+
+
+def _one_row(t, width, what):
+    """gala_values of `width` numbers on the GPU"""
+    if len(t.shape) != 1 or t.shape[0] != width:
+        raise ValueError(f"{what} has to hold {width} numbers, not {tuple(t.shape)}")
+    _on_gpu(t, what)
+    kind = _types.get(t.dtype)
+    return _values(t[None], 1.0) if kind is None or t.stride(0) != 1 else _pack_values(t.data_ptr(), 0, kind, 1.0)
 
 
 def _scratch(t, size):
@@ -488,37 +503,43 @@ class Context:
     # ---- a language model's last step
     def rms_norm(self, x, out, add=None, sum_out=None, weight=None, epsilon=1e-6, limit=0, scales=None, group=0, unit=1.0,
                  x_unit=1.0, add_unit=1.0, stream=None):
-        """s = x + add into ``sum_out``, its root-mean-square norm times ``weight`` (one number a column) into ``out``: rows of numbers,
+        """s = x + add into ``sum_out``, its root-mean-square norm times ``weight`` (width numbers) into ``out``: rows of numbers,
         all of the same width.  ``out`` int8 or residues: whole numbers held to +-limit, of ``unit``, or with ``scales`` (rows, scales of
         a row) float32, one for every ``group`` columns (0: for the row)."""
-        rows = x.shape[0]
-        width = math.prod(x.shape[1:])
-        given = [None if t is None else _row_values(t, rows, width, u, what) for t, u, what in
-                 ((x, x_unit, "x"), (add, add_unit, "add"), (sum_out, 1.0, "sum_out"))]
-        given.append(None if weight is None else _row_values(weight.reshape(1, -1), 1, width, 1.0, "weight"))
-        given.append(_row_values(out, rows, width, unit, "out", codes=True))
+        shape = x.shape
+        if len(shape) != 2:
+            shape = (shape[0], math.prod(shape[1:]))
+        rows, width = shape
         at = 0
         if scales is not None:
             at = _words(scales, "torch.float32", "scales")
             _on_gpu(scales, "scales")
             if scales.numel() < rows * (-(-width // group) if group > 0 else 1):
                 raise ValueError("scales has to have a number for each row and group")
+        given = (_row_values(x, shape, x_unit, "x"), None if add is None else _row_values(add, shape, add_unit, "add"),
+                 None if sum_out is None else _row_values(sum_out, shape, 1.0, "sum_out"),
+                 None if weight is None else _one_row(weight, width, "weight"), _row_values(out, shape, unit, "out", True))
         _check(self.lib.gala_rms_norm(self.h, _stream(stream), _pack_norm(epsilon, limit, group, at), rows, width, *given), "gala_rms_norm")
 
     def rope_apply(self, rope, at, x, out, unit=1.0, stream=None):
         """x (rows, heads, head_dim) turned by an AxesRope into ``out`` of the same shape; at (rows, axes) int32 positions."""
-        if x.dim() != 3 or x.shape != out.shape:
+        shape, places = x.shape, at.shape
+        if len(shape) != 3 or shape != out.shape:
             raise ValueError("x and out are rows x heads x head_dim, both alike")
-        rows, heads, head_dim = x.shape
-        if at.dim() != 2 or at.shape[0] != rows or at.shape[1] < rope.axes or (at.shape[1] > 1 and at.stride(1) != 1):
+        rows, heads, head_dim = shape
+        if len(places) != 2 or places[0] != rows or places[1] < rope.axes:
             raise ValueError("at has a position on each axis for each row")
-        if str(at.dtype) != "torch.int32":
-            raise TypeError("at has to be an int32 tensor")
+        step, across = at.stride()
+        if across != 1 and places[1] > 1:
+            raise ValueError("a row's positions have to be contiguous")
+        if at.dtype is not _named.get("torch.int32"):
+            if str(at.dtype) != "torch.int32":
+                raise TypeError("at has to be an int32 tensor")
+            _named["torch.int32"] = at.dtype
+        _on_gpu(at, "at")
         x, _, _ = _heads_values(x, heads, head_dim, unit, "x")
         out, _, _ = _heads_values(out, heads, head_dim, unit, "out")
-        _on_gpu(at, "at")
-        _check(self.lib.gala_rope_apply(self.h, _stream(stream), rope.ref, at.data_ptr(), at.stride(0), rows, heads, head_dim, x, out),
-               "gala_rope_apply")
+        _check(self.lib.gala_rope_apply(self.h, _stream(stream), rope.ref, at.data_ptr(), step, rows, heads, head_dim, x, out), "gala_rope_apply")
 
     def sample_workspace_bytes(self, rows, vocab):
         return int(self.lib.gala_sample_workspace(rows, vocab))

@@ -574,7 +574,10 @@ int launch_kv4_attention(void *stream, const KvArgs &kv, int heads_q, float scal
     const bool fine = q.type == GALA_F32 || q.type == GALA_RESIDUE || out.type == GALA_F32 || out.type == GALA_RESIDUE;
     // a score times log2(e) and the logarithm of a scale share an accumulator: neither may drown the other
     const float unit = std::fabs(scale) * kLog2E;
-    const Cut c = cut_of(kv, heads_q, window, sinks, fine || !(unit >= 0x1p-20f && unit <= 0x1p20f));
+    const bool apart = unit >= 0x1p-20f && unit <= 0x1p20f;
+    // f16 queries of more than 192 channels, in two parts, do not fit the registers beside a wide tile's sums
+    const bool fits = q.type != GALA_F16 || kv.dim <= 192;
+    const Cut c = cut_of(kv, heads_q, window, sinks, fine || !apart || !fits);
     Attention a{};
     a.kv = kv, a.q = q, a.out = out;
     const size_t size = q.type == GALA_F32 ? 4 : q.type == GALA_RESIDUE ? 8 : 2;
@@ -594,10 +597,10 @@ int launch_kv4_attention(void *stream, const KvArgs &kv, int heads_q, float scal
                 hipLaunchKernelGGL((kv4_attention_many_kernel<G, decltype(parts)::value, kWavesOf>), dim3(groups), dim3(64 * kWavesOf), 0,
                                    (hipStream_t)stream, a);
             };
-            if (q.type == GALA_F16)
-                many(std::integral_constant<int, 2>());
-            else
+            if (q.type != GALA_F16)
                 many(std::integral_constant<int, 1>());
+            else if constexpr (G <= 6)
+                many(std::integral_constant<int, 2>());
             return;
         }
         auto waves = [&](auto w) {
