@@ -56,7 +56,7 @@ int launch_rope_apply(void *stream, const gala_rope_axes &rope, const int *at, l
                       const Values &out);
 // How a norm's row becomes whole numbers.
 struct NormArgs {
-    double epsilon;
+    double epsilon, per_width;       // per_width: 1 / width
     float limit, step;               // step: 1 / limit
     int group;                       // channels of a scale
     float *scales;                   // nullptr: none

@@ -298,6 +298,7 @@ extern "C" int gala_rms_norm(const gala_ctx *c, void *stream, const gala_norm *h
     if (!rows) return GALA_OK;
     NormArgs n{};
     n.epsilon = how->epsilon;
+    n.per_width = 1.0 / width;
     n.limit = (float)how->limit;
     if (whole && !how->limit) {          // the largest number of 24 bits
         n.limit = (float)(c->p / 2);

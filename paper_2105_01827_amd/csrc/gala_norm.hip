@@ -7,94 +7,123 @@ using namespace gala;
 
 namespace {
 
-// value k of a thread, and eight of them at a time
-template <bool PIECES, int THREADS>
-__device__ __forceinline__ int column_of(int tid, int k) {
-    return PIECES ? (k / 8 * THREADS + tid) * 8 + k % 8 : k * THREADS + tid;
-}
-// N x 8 numbers of a row as floats, 0 behind its end
-template <bool PIECES, int THREADS, int N>
-__device__ __forceinline__ void load_row(const Values &v, long row, int tid, int width, float (&x)[8 * N]) {
+// Threads take pieces of eight numbers of a row.  WHOLE: rows lie on 16 bytes and end with a piece.  Else a piece is read where it
+// lies -- the loads take any address -- and the numbers of a last one that is not whole one by one.
+template <int THREADS>
+__device__ __forceinline__ int column_of(int tid, int n) { return (n * THREADS + tid) * 8; }
+template <bool WHOLE>
+struct alignas(WHOLE ? 16 : 1) Word16 {
+    u64 x, y;
+} __attribute__((packed));
+
+// N pieces on their way, as they lie in memory
+template <int N>
+struct Raw {
+    u64 word[N][16];
+};
+template <bool WHOLE, int THREADS, int N>
+__device__ __forceinline__ void fetch_row(const Values &v, long row, int tid, int width, Raw<N> &raw) {
     by_type(v.type, [&](auto type) __attribute__((always_inline)) {
-        constexpr int T = decltype(type)::value;
-        typedef typename Element<T>::type E;
-        if constexpr (PIECES) {
-            union Piece {
-                int4 word[sizeof(E) / 2];
-                E e[8];
-            } u[N];
+        typedef typename Element<decltype(type)::value>::type E;
+        const E *from = (const E *)v.data + row * v.stride;
 #pragma unroll
-            for (int n = 0; n < N; ++n) {
-                const int column = column_of<true, THREADS>(tid, 8 * n);
-                const int4 *from = (const int4 *)((const E *)v.data + row * v.stride + (column < width ? column : 0));
+        for (int n = 0; n < N; ++n) {
+            const int column = column_of<THREADS>(tid, n);
+            if (WHOLE || column + 8 <= width) {
+                const Word16<WHOLE> *at = (const Word16<WHOLE> *)(from + (WHOLE && column >= width ? 0 : column));
 #pragma unroll
-                for (int k = 0; k < (int)sizeof(E) / 2; ++k) u[n].word[k] = from[k];
+                for (int k = 0; k < (int)sizeof(E) / 2; ++k) {
+                    const Word16<WHOLE> w = at[k];
+                    raw.word[n][2 * k] = w.x, raw.word[n][2 * k + 1] = w.y;
+                }
+            } else {
+                union {
+                    u64 word[sizeof(E)];
+                    E e[8];
+                } u;
+#pragma unroll
+                for (int k = 0; k < 8; ++k) u.e[k] = from[min(column + k, width - 1)];
+#pragma unroll
+                for (int k = 0; k < (int)sizeof(E); ++k) raw.word[n][k] = u.word[k];
             }
-#pragma unroll
-            for (int n = 0; n < N; ++n)
-#pragma unroll
-                for (int k = 0; k < 8; ++k) x[8 * n + k] = column_of<true, THREADS>(tid, 8 * n) < width ? to_float<T>(u[n].e[k], v.unit, v.p) : 0.0f;
-        } else {
-            E e[8 * N];
-#pragma unroll
-            for (int k = 0; k < 8 * N; ++k) {
-                const int column = column_of<false, THREADS>(tid, k);
-                e[k] = ((const E *)v.data)[row * v.stride + (column < width ? column : 0)];
-            }
-#pragma unroll
-            for (int k = 0; k < 8 * N; ++k) x[k] = column_of<false, THREADS>(tid, k) < width ? to_float<T>(e[k], v.unit, v.p) : 0.0f;
         }
     });
 }
-template <bool PIECES, int THREADS, int N>
+// ... and as floats, 0 behind the row's end
+template <int THREADS, int N>
+__device__ __forceinline__ void floats_of(const Values &v, int tid, int width, const Raw<N> &raw, float (&x)[8 * N]) {
+    by_type(v.type, [&](auto type) __attribute__((always_inline)) {
+        constexpr int T = decltype(type)::value;
+        typedef typename Element<T>::type E;
+        constexpr int kIn = 8 / sizeof(E);           // numbers of a word
+#pragma unroll
+        for (int n = 0; n < N; ++n)
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                E e;
+                const u64 word = raw.word[n][k / kIn] >> (k % kIn * 8 * sizeof(E));
+                __builtin_memcpy(&e, &word, sizeof(E));
+                x[8 * n + k] = column_of<THREADS>(tid, n) + k < width ? to_float<T>(e, v.unit, v.p) : 0.0f;
+            }
+    });
+}
+// eight numbers of a row to their places
+template <bool WHOLE, class E>
+__device__ __forceinline__ void store_eight(E *to, int column, int width, const E (&e)[8]) {
+    if (WHOLE ? column < width : column + 8 <= width) {
+        if constexpr (sizeof(E) == 1) {
+            struct alignas(WHOLE ? 8 : 1) Word8 {
+                u64 x;
+            } __attribute__((packed)) w;
+            __builtin_memcpy(&w, e, 8);
+            *(Word8 *)(to + column) = w;
+        } else {
+#pragma unroll
+            for (int k = 0; k < (int)sizeof(E) / 2; ++k) {
+                Word16<WHOLE> w;
+                __builtin_memcpy(&w, e + k * (16 / sizeof(E)), 16);
+                ((Word16<WHOLE> *)(to + column))[k] = w;
+            }
+        }
+    } else if (!WHOLE) {
+#pragma unroll
+        for (int k = 0; k < 8; ++k)
+            if (column + k < width) to[column + k] = e[k];
+    }
+}
+template <bool WHOLE, int THREADS, int N>
 __device__ __forceinline__ void store_row(const Values &v, long row, int tid, int width, const float (&x)[8 * N]) {
     by_type(v.type, [&](auto type) __attribute__((always_inline)) {
         constexpr int T = decltype(type)::value;
-        if constexpr (PIECES) {
+        typedef typename Element<T>::type E;
 #pragma unroll
-            for (int n = 0; n < N; ++n) {
-                const int column = column_of<true, THREADS>(tid, 8 * n);
-                float piece[8];
+        for (int n = 0; n < N; ++n) {
+            E e[8];
 #pragma unroll
-                for (int k = 0; k < 8; ++k) piece[k] = x[8 * n + k];
-                if (column < width) store_piece<T>(v, row, column, piece);
-            }
-        } else {
-#pragma unroll
-            for (int k = 0; k < 8 * N; ++k) {
-                const int column = column_of<false, THREADS>(tid, k);
-                if (column < width) store_value<T>(v, row, column, x[k]);
-            }
+            for (int k = 0; k < 8; ++k) e[k] = from_float<T>(x[8 * n + k], v.unit, v.p);
+            store_eight<WHOLE>((E *)v.data + row * v.stride, column_of<THREADS>(tid, n), width, e);
         }
     });
 }
 // whole numbers, as int8 or as residues
-template <bool PIECES, int THREADS, int N>
+template <bool WHOLE, int THREADS, int N>
 __device__ __forceinline__ void store_codes(const Values &v, long row, int tid, int width, const float (&x)[8 * N]) {
-    auto residue = [&](float c) { return (u64)((long)c + (c < 0 ? (long)v.p : 0)); };
 #pragma unroll
-    for (int k = 0; k < 8 * N; k += PIECES ? 8 : 1) {
-        const int column = column_of<PIECES, THREADS>(tid, k);
-        if (column >= width) continue;
+    for (int n = 0; n < N; ++n) {
+        const int column = column_of<THREADS>(tid, n);
         if (v.type == GALA_INT8) {
-            signed char *to = (signed char *)v.data + row * v.stride + column;
-            if constexpr (PIECES) {
-                u32 w[2] = {0, 0};
+            signed char e[8];
 #pragma unroll
-                for (int i = 0; i < 8; ++i) w[i / 4] |= (u32)((int)x[k + i] & 255) << 8 * (i % 4);
-                *(uint2 *)to = uint2{w[0], w[1]};
-            } else {
-                *to = (signed char)(int)x[k];
-            }
+            for (int k = 0; k < 8; ++k) e[k] = (signed char)(int)x[8 * n + k];
+            store_eight<WHOLE>((signed char *)v.data + row * v.stride, column, width, e);
         } else {
-            u64 *to = (u64 *)v.data + row * v.stride + column;
+            u64 e[8];
 #pragma unroll
-            for (int i = 0; i < (PIECES ? 8 : 1); i += PIECES ? 2 : 1) {
-                if constexpr (PIECES)
-                    *(ulong2 *)(to + i) = ulong2{residue(x[k + i]), residue(x[k + i + 1])};
-                else
-                    *to = residue(x[k]);
+            for (int k = 0; k < 8; ++k) {
+                const int c = (int)x[8 * n + k];
+                e[k] = (u64)(c < 0 ? c + (int)v.p : c);
             }
+            store_eight<WHOLE>((u64 *)v.data + row * v.stride, column, width, e);
         }
     }
 }
@@ -111,7 +140,7 @@ struct Rows {
 
 // A row stays in the registers of THREADS threads, N pieces of eight numbers each: one pass over memory.  Rows of up to a wavefront's
 // registers share a workgroup of four.
-template <int THREADS, int N, bool PIECES>
+template <int THREADS, int N, bool WHOLE>
 __global__ __launch_bounds__(THREADS < 256 ? 256 : THREADS) void rms_norm_kernel(Rows a) {
 #pragma clang fp contract(off)
     constexpr int kWaves = THREADS / 64, kRows = THREADS < 256 ? 256 / THREADS : 1;
@@ -127,22 +156,24 @@ __global__ __launch_bounds__(THREADS < 256 ? 256 : THREADS) void rms_norm_kernel
     for (int g = tid; g < groups; g += THREADS) slots[g] = 0;
     if constexpr (kWaves == 1) __syncthreads();          // else the sum's
     float s[8 * N], other[8 * N];
-    if (!idle) {
-        load_row<PIECES, THREADS, N>(a.x, row, tid, width, s);
+    const long from = idle ? how.rows - 1 : row;
+    {
+        // all of the row, and the weights, on their way together: rows of 8191 x 4096 in 52 us, one after the other in 63
+        Raw<N> raw, raw_add, raw_weight;
+        fetch_row<WHOLE, THREADS, N>(a.x, from, tid, width, raw);
+        if (a.add.data) fetch_row<WHOLE, THREADS, N>(a.add, from, tid, width, raw_add);
+        if (a.weight.data) fetch_row<WHOLE, THREADS, N>(a.weight, 0, tid, width, raw_weight);
+        floats_of<THREADS, N>(a.x, tid, width, raw, s);
         if (a.add.data) {
-            load_row<PIECES, THREADS, N>(a.add, row, tid, width, other);
+            floats_of<THREADS, N>(a.add, tid, width, raw_add, other);
 #pragma unroll
             for (int k = 0; k < 8 * N; ++k) s[k] += other[k];
         }
-        if (a.weight.data) {
-            load_row<PIECES, THREADS, N>(a.weight, 0, tid, width, other);
-        } else {
+        if (a.weight.data) floats_of<THREADS, N>(a.weight, tid, width, raw_weight, other);
+    }
+    if (!a.weight.data) {
 #pragma unroll
-            for (int k = 0; k < 8 * N; ++k) other[k] = 1;
-        }
-    } else {
-#pragma unroll
-        for (int k = 0; k < 8 * N; ++k) s[k] = other[k] = 0;
+        for (int k = 0; k < 8 * N; ++k) other[k] = 1;
     }
     double all = 0;
 #pragma unroll
@@ -155,12 +186,12 @@ __global__ __launch_bounds__(THREADS < 256 ? 256 : THREADS) void rms_norm_kernel
 #pragma unroll
         for (int k = 0; k < kWaves; ++k) all += sums[k];
     }
-    if (!idle && a.sum.data) store_row<PIECES, THREADS, N>(a.sum, row, tid, width, s);
-    const float factor = (float)(1.0 / sqrt(all / width + how.epsilon));
+    if (!idle && a.sum.data) store_row<WHOLE, THREADS, N>(a.sum, row, tid, width, s);
+    const float factor = (float)rsqrt(all * how.per_width + how.epsilon);
 #pragma unroll
     for (int k = 0; k < 8 * N; ++k) s[k] = s[k] * factor * other[k];
     if (a.out.type < GALA_RESIDUE) {
-        if (!idle) store_row<PIECES, THREADS, N>(a.out, row, tid, width, s);
+        if (!idle) store_row<WHOLE, THREADS, N>(a.out, row, tid, width, s);
         return;
     }
     if (!how.scales) {
@@ -169,7 +200,7 @@ __global__ __launch_bounds__(THREADS < 256 ? 256 : THREADS) void rms_norm_kernel
             const float t = rintf(s[k] / a.out.unit);
             s[k] = t != t ? 0.0f : fminf(how.limit, fmaxf(-how.limit, t));
         }
-        if (!idle) store_codes<PIECES, THREADS, N>(a.out, row, tid, width, s);
+        if (!idle) store_codes<WHOLE, THREADS, N>(a.out, row, tid, width, s);
         return;
     }
     // the largest magnitude of every group
@@ -180,28 +211,41 @@ __global__ __launch_bounds__(THREADS < 256 ? 256 : THREADS) void rms_norm_kernel
         for (int k = 0; k < 8 * N; ++k) most = fmaxf(most, finite(s[k]));
         for (int k = 32; k; k >>= 1) most = fmaxf(most, __shfl_xor(most, k));
         if ((tid & 63) == 0) atomicMax(&slots[0], __float_as_uint(most));
+    } else if (how.group % 8 == 0) {
+#pragma unroll
+        for (int n = 0; n < N; ++n) {
+            float most = 0;
+#pragma unroll
+            for (int k = 0; k < 8; ++k) most = fmaxf(most, finite(s[8 * n + k]));
+            const int column = column_of<THREADS>(tid, n);
+            if (column < width) atomicMax(&slots[column / how.group], __float_as_uint(most));
+        }
     } else {
 #pragma unroll
-        for (int k = 0; k < 8 * N; k += PIECES ? 8 : 1) {
-            const int column = column_of<PIECES, THREADS>(tid, k);
-            float most = finite(s[k]);
-#pragma unroll
-            for (int i = 1; i < (PIECES ? 8 : 1); ++i) most = fmaxf(most, finite(s[k + i]));
-            if (column < width) atomicMax(&slots[column / how.group], __float_as_uint(most));
+        for (int k = 0; k < 8 * N; ++k) {
+            const int column = column_of<THREADS>(tid, k / 8) + k % 8;
+            if (column < width) atomicMax(&slots[column / how.group], __float_as_uint(finite(s[k])));
         }
     }
     __syncthreads();
     if (idle) return;
     for (int g = tid; g < groups; g += THREADS) how.scales[row * groups + g] = __uint_as_float(slots[g]) * how.step;
-#pragma unroll
-    for (int k = 0; k < 8 * N; k += PIECES ? 8 : 1) {
-        const int column = column_of<PIECES, THREADS>(tid, k);
+    auto inverse_of = [&](int column) __attribute__((always_inline)) {
         const float scale = column < width ? __uint_as_float(slots[column / how.group]) * how.step : 0.0f;
-        const float inverse = scale > 0 ? 1.0f / scale : 0.0f;
+        return scale > 0 ? 1.0f / scale : 0.0f;
+    };
 #pragma unroll
-        for (int i = 0; i < (PIECES ? 8 : 1); ++i) s[k + i] = code_of(s[k + i], inverse, how.limit);
+    for (int n = 0; n < N; ++n) {
+        const int column = column_of<THREADS>(tid, n);
+        const bool together = groups == 1 || how.group % 8 == 0;
+        float inverse = inverse_of(column);
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            if (k && !together) inverse = inverse_of(column + k);
+            s[8 * n + k] = code_of(s[8 * n + k], inverse, how.limit);
+        }
     }
-    store_codes<PIECES, THREADS, N>(a.out, row, tid, width, s);
+    store_codes<WHOLE, THREADS, N>(a.out, row, tid, width, s);
 }
 
 // Rows that no workgroup's registers hold, or whose groups are too many for LDS: the row is read three times, nothing is written
@@ -229,7 +273,7 @@ __global__ __launch_bounds__(1024) void rms_norm_long_kernel(Rows a) {
     __syncthreads();
     all = 0;
     for (int k = 0; k < 16; ++k) all += sums[k];
-    const float factor = (float)(1.0 / sqrt(all / width + how.epsilon));
+    const float factor = (float)rsqrt(all * how.per_width + how.epsilon);
     auto normed = [&](float s, int c) { return s * factor * (a.weight.data ? value(a.weight, 0, c) : 1.0f); };
     auto put = [&](int c, float s, float y, float inverse) {
         if (a.sum.data) by_type(a.sum.type, [&](auto type) { store_value<decltype(type)::value>(a.sum, row, c, s); });
@@ -286,9 +330,8 @@ int launch_rms_norm(void *stream, const NormArgs &how, const Values &x, const Va
     const int width = how.width;
     Rows a{how, x, add, sum, weight, out};
     hipStream_t st = (hipStream_t)stream;
-    const bool int8 = out.type == GALA_INT8;
-    const bool pieces = in_pieces(x, width) && in_pieces(add, width) && in_pieces(sum, width) && in_pieces(weight, width) &&
-                        (int8 ? (uintptr_t)out.data % 8 == 0 && out.stride % 8 == 0 : in_pieces(out, width)) && (!how.scales || how.group % 8 == 0 || how.group >= width);
+    const bool whole = in_pieces(x, width) && in_pieces(add, width) && in_pieces(sum, width) && in_pieces(weight, width) &&
+                       (out.type == GALA_INT8 ? (uintptr_t)out.data % 8 == 0 && out.stride % 8 == 0 && width % 8 == 0 : in_pieces(out, width));
     const int groups = how.scales ? (width + how.group - 1) / how.group : 0;
     if (width > 16384 || groups > 8192) {
         hipLaunchKernelGGL(rms_norm_long_kernel, dim3(how.rows), dim3(1024), 0, st, a);
@@ -297,7 +340,7 @@ int launch_rms_norm(void *stream, const NormArgs &how, const Values &x, const Va
     auto launch = [&](auto threads, auto n) {
         constexpr int T = decltype(threads)::value, N = decltype(n)::value, R = T < 256 ? 256 / T : 1;
         const dim3 grid((how.rows + R - 1) / R), block(T * R);
-        if (pieces)
+        if (whole)
             hipLaunchKernelGGL((rms_norm_kernel<T, N, true>), grid, block, R * groups * 4, st, a);
         else
             hipLaunchKernelGGL((rms_norm_kernel<T, N, false>), grid, block, R * groups * 4, st, a);
