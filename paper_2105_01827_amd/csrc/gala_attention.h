@@ -24,6 +24,7 @@ struct Attention {
     float scale;
     int window, sinks;
     int waves;                       // wavefronts of a workgroup
+    bool ordered;                    // groups of queries of all sequences go by what they see
     int tiles, splits, columns;      // column tiles of a head, shares of its keys, columns of a tile that are kept
     float *sums, *stats;             // of every share: columns x dim, and columns x (largest, sum)
 };

@@ -143,7 +143,8 @@ __device__ __forceinline__ bool load_query(const Attention &a, long row, int hq,
 template <int G, int NQ, int NW, int kWaves>
 __global__ __launch_bounds__(64 * kWaves, G <= 4 ? 2 : 1) void kv4_attention_kernel(Attention a) {
     constexpr int NV = 2 * G;                                // tiles of 16 channels of values
-    __shared__ float sums[kWaves][kColumns][NV * 16 + 1];
+    constexpr int kRow = NV * 16 + 1;
+    extern __shared__ float sums[];                          // of each wavefront and column
     __shared__ float stats[kWaves][kColumns][2];
     const KvArgs &kv = a.kv;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 15, part = lane >> 4;
@@ -264,10 +265,13 @@ __global__ __launch_bounds__(64 * kWaves, G <= 4 ? 2 : 1) void kv4_attention_ker
     // the wavefronts' sums in one
     sum += __shfl_xor(sum, 16);
     sum += __shfl_xor(sum, 32);
+    if (col < a.columns) {
+        float *mine = sums + (wave * a.columns + col) * kRow + part * 4;
 #pragma unroll
-    for (int j = 0; j < NV; ++j)
+        for (int j = 0; j < NV; ++j)
 #pragma unroll
-        for (int r = 0; r < 4; ++r) sums[wave][col][j * 16 + part * 4 + r] = o[j][r];
+            for (int r = 0; r < 4; ++r) mine[j * 16 + r] = o[j][r];
+    }
     if (part == 0) stats[wave][col][0] = bad ? __builtin_nanf("") : top, stats[wave][col][1] = sum;
     __syncthreads();
     const long place = (((long)b * kv.heads + h) * a.tiles + tile) * a.splits + split;
@@ -281,7 +285,7 @@ __global__ __launch_bounds__(64 * kWaves, G <= 4 ? 2 : 1) void kv4_attention_ker
         for (int k = 0; k < kWaves; ++k) {
             const float f = __builtin_amdgcn_exp2f(stats[k][cc][0] - base);       // NaN where the query is
             all += f * stats[k][cc][1];
-            x += f * sums[k][cc][d];
+            x += f * sums[(k * a.columns + cc) * kRow + d];
         }
         if (a.splits == 1) {
             const int column = s.col0 + cc;
@@ -301,7 +305,7 @@ __global__ __launch_bounds__(64 * kWaves, G <= 4 ? 2 : 1) void kv4_attention_ker
 // 2^-21 of the largest weight times scale, steps of 2^-31 of it below.  The divisor adds up w / s in 32 bits.
 constexpr float kRaised = 7, kHighest = 15;      // exponents
 constexpr float kNothing = 0x1p-64f;             // scale of values that are zeros: their weights count in the divisor
-constexpr int kWide = 32;
+constexpr int kWide = 32, kWavesOf = 4, kColumnsOf = kWide * kWavesOf;
 
 // Two lanes (halves) have a token's key: of two groups of 32 channels one each, of one left over half.  Product n takes their n-th words.
 template <int G>
@@ -337,20 +341,53 @@ __device__ __forceinline__ void load_keys(const char *data, int token, int half,
         k.exponent[n] = *(const u32 *)(data + kv4_exponents(G) + W::group(4 * n, half) * 64 + low * 4) >> 8 * high;
 }
 
-template <int G, int NQ, int kWaves>
-__global__ __launch_bounds__(64 * kWaves, G <= 4 ? 2 : 1) void kv4_attention_many_kernel(Attention a) {
+// groups of kColumnsOf queries of a head of sequence b, and how many groups' positions it is shorter than max_len
+__device__ __forceinline__ int groups_of(const Attention &a, int b) {
+    const int n = min(a.kv.starts[b + 1] - a.kv.starts[b], a.kv.max_new);
+    return n > 0 ? (int)(((long)n * a.group + kColumnsOf - 1) / kColumnsOf) : 0;
+}
+__device__ __forceinline__ int later_of(const Attention &a, int b) {
+    return (int)min((long)max(a.kv.max_len - a.kv.lens[b], 0) * a.group / kColumnsOf, (long)a.tiles);
+}
+// The unit'th group of queries by level, of up to 64 sequences, one a lane: (sequence, group of it), group -1 for none.  Groups are
+// packed: workgroups with nothing to do between the others would leave their CUs with less than the rest.
+__device__ __forceinline__ int2 ordered(const Attention &a, int unit) {
+    const int lane = threadIdx.x & 63, mine = min(lane, a.kv.count - 1);
+    const int groups = lane < a.kv.count ? groups_of(a, mine) : 0, later = later_of(a, mine);
+    const int width = a.kv.count > 1 ? 64 >> __clz(a.kv.count - 1) - 26 : 1;             // lanes that have one
+    // groups before a level; the last level with at most `unit` of them
+    auto before = [&](int level) {
+        int n = min(max(level - later, 0), groups);
+        for (int k = width / 2; k; k >>= 1) n += __shfl_xor(n, k);
+        return __builtin_amdgcn_readfirstlane(n);
+    };
+    int lo = 0, hi = 2 * a.tiles;
+    if (before(hi) <= unit) return int2{0, -1};
+    while (lo + 1 < hi) {
+        const int mid = (lo + hi) >> 1;
+        (before(mid) <= unit ? lo : hi) = mid;
+    }
+    u64 there = __ballot(lo >= later && lo - later < groups);
+    for (int k = unit - before(lo); k > 0; --k) there &= there - 1;
+    const int b = __builtin_amdgcn_readfirstlane(__ffsll((unsigned long long)there) - 1);
+    return int2{b, __builtin_amdgcn_readlane(groups - 1 - (lo - later), b)};
+}
+
+template <int G, int NQ>
+__global__ __launch_bounds__(64 * kWavesOf, G <= 4 ? 2 : 1) void kv4_attention_many_kernel(Attention a) {
     typedef float v16f __attribute__((ext_vector_type(16)));
     typedef WideWords<G> W;
     constexpr size_t kHead = 64 * (33 * G + 2);
-    __shared__ __attribute__((aligned(16))) float of_scales[kWaves][2][kKvBlock];        // log2(s) / unit, 1 / s
+    __shared__ __attribute__((aligned(16))) float of_scales[kWavesOf][2][kKvBlock];        // log2(s) / unit, 1 / s
     const KvArgs &kv = a.kv;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 31, half = lane >> 5;
-    // the last queries see most keys: they go first, of all heads
-    int unit = blockIdx.x;
-    const int per_group = kv.count * kv.heads, group = a.tiles - 1 - unit / per_group;
-    unit %= per_group;
-    const int h = unit % kv.heads, b = unit / kv.heads;
-    const Seen s = seen_by(a, b, group * kWaves + wave, kWide);
+    // Groups of queries that see most keys go first, of all sequences and heads.  A level is that many positions as a group has; a
+    // sequence's last group is at the level of its distance from max_len.
+    const int h = blockIdx.x % kv.heads, b0 = blockIdx.x / kv.heads;
+    const int2 of = a.ordered ? ordered(a, b0) : int2{b0 % kv.count, groups_of(a, b0 % kv.count) - 1 - b0 / kv.count};
+    const int b = of.x, group = of.y;
+    if (group < 0) return;
+    const Seen s = seen_by(a, b, group * kWavesOf + wave, kWide);
     if (!s.cols) return;
     const int mine = s.col0 + min(col, s.cols - 1), qi = mine / a.group, hq = h * a.group + mine % a.group;
     const long row = s.start + qi;
@@ -534,10 +571,9 @@ __global__ __launch_bounds__(64 * kWaves, G <= 4 ? 2 : 1) void kv4_attention_man
 }
 
 // How a call is cut up.
-constexpr int kWavesOf = 4;
 struct Cut {
     bool many;
-    int tiles, splits, columns;
+    int tiles, splits, columns, waves;
     long places() const { return (long)tiles * splits * columns; }
 };
 Cut cut_of(const KvArgs &kv, int heads_q, int window, int sinks, bool fine) {
@@ -546,17 +582,24 @@ Cut cut_of(const KvArgs &kv, int heads_q, int window, int sinks, bool fine) {
     const long reach = std::min<long>(kv.max_len, (long)kv.table_stride * kKvBlock);
     const long keys = window ? std::min(reach, (long)window + kv.max_new + sinks + 2 * kKvBlock) : reach;
     const long blocks = std::max(1l, (keys + kKvBlock - 1) / kKvBlock);
-    const int of_group = kWide * kWavesOf;
-    const long groups = (columns + of_group - 1) / of_group * kv.count * kv.heads;
-    c.many = !fine && columns >= of_group && (groups >= 192 || blocks <= 16);
+    const long groups = (columns + kColumnsOf - 1) / kColumnsOf * kv.count * kv.heads;
+    c.many = !fine && columns >= kColumnsOf && (groups >= 192 || blocks <= 16);
     if (c.many) {
-        c.tiles = (int)((columns + of_group - 1) / of_group), c.splits = 1, c.columns = 0;
+        c.tiles = (int)((columns + kColumnsOf - 1) / kColumnsOf), c.splits = 1, c.columns = 0;
         return c;
     }
     c.tiles = (int)((columns + kColumns - 1) / kColumns);
     c.columns = (int)std::min<long>(columns, kColumns);
+    // A block takes a wavefront 1.2 us after the other, joining shares 5 us.  Eight wavefronts a workgroup where that leaves CUs with one:
+    // 32 windows of 1024 tokens take 12.3 us so and 14.5 with four, one sequence of 131072 25.0 and 26.4; 64 of 8192 in 512
+    // workgroups of 32 bits 121 and 114.  Shares for one round of the card, of 8 blocks at least, where there are 48: 4000 tokens take 18.5 us
+    // whole and 11.6 in shares.  Wide heads leave room for one wavefront a SIMD.
     const long units = std::max(1l, (long)kv.count * kv.heads * c.tiles);
-    c.splits = (int)std::max(1l, std::min((512 + units - 1) / units, (blocks + 31) / 32));
+    const bool wide = kv4_groups(kv.dim) > 4;
+    const bool few = !wide && (units <= 128 || (units <= 256 && blocks < 128));
+    const long room = few || wide ? 256 : 512;
+    c.waves = few ? 8 : 4;
+    c.splits = blocks < 48 ? 1 : (int)std::max(1l, std::min(room / units, blocks / 8));
     return c;
 }
 
@@ -593,9 +636,9 @@ int launch_kv4_attention(void *stream, const KvArgs &kv, int heads_q, float scal
     auto launch = [&](auto n32) {
         constexpr int G = decltype(n32)::value;
         if (c.many) {
+            a.ordered = kv.count > 1 && kv.count <= 64 && !window;
             auto many = [&](auto parts) {
-                hipLaunchKernelGGL((kv4_attention_many_kernel<G, decltype(parts)::value, kWavesOf>), dim3(groups), dim3(64 * kWavesOf), 0,
-                                   (hipStream_t)stream, a);
+                hipLaunchKernelGGL((kv4_attention_many_kernel<G, decltype(parts)::value>), dim3(groups), dim3(64 * kWavesOf), 0, (hipStream_t)stream, a);
             };
             if (q.type != GALA_F16)
                 many(std::integral_constant<int, 1>());
@@ -606,14 +649,22 @@ int launch_kv4_attention(void *stream, const KvArgs &kv, int heads_q, float scal
         auto waves = [&](auto w) {
             constexpr int W = decltype(w)::value;
             a.waves = W;
+            const unsigned lds = W * c.columns * (32 * G + 1) * sizeof(float);
             if (fine)
-                hipLaunchKernelGGL((kv4_attention_kernel<G, 3, 3, W>), dim3(groups), dim3(64 * W), 0, (hipStream_t)stream, a);
+                hipLaunchKernelGGL((kv4_attention_kernel<G, 3, 3, W>), dim3(groups), dim3(64 * W), lds, (hipStream_t)stream, a);
             else if (q.type == GALA_F16)
-                hipLaunchKernelGGL((kv4_attention_kernel<G, 2, 2, W>), dim3(groups), dim3(64 * W), 0, (hipStream_t)stream, a);
+                hipLaunchKernelGGL((kv4_attention_kernel<G, 2, 2, W>), dim3(groups), dim3(64 * W), lds, (hipStream_t)stream, a);
             else
-                hipLaunchKernelGGL((kv4_attention_kernel<G, 1, 2, W>), dim3(groups), dim3(64 * W), 0, (hipStream_t)stream, a);
+                hipLaunchKernelGGL((kv4_attention_kernel<G, 1, 2, W>), dim3(groups), dim3(64 * W), lds, (hipStream_t)stream, a);
         };
-        waves(std::integral_constant<int, 4>());
+        if constexpr (G <= 4) {
+            if (c.waves == 8)
+                waves(std::integral_constant<int, 8>());
+            else
+                waves(std::integral_constant<int, 4>());
+        } else {
+            waves(std::integral_constant<int, 4>());
+        }
         if (c.splits == 1) return;
         const unsigned rows = (unsigned)((long)kv.count * kv.heads * c.tiles * c.columns);
         hipLaunchKernelGGL((kv_attention_join_kernel<(G + 1) / 2>), dim3(rows), dim3(64 * kJoinWaves), 0, (hipStream_t)stream, a);
