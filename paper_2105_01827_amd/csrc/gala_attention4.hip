@@ -135,17 +135,57 @@ __device__ __forceinline__ bool load_query(const Attention &a, long row, int hq,
     return fine;
 }
 
+// ---- weights in half precision -------------------------------------------------------------------------------------------
+// Of 16-bit types a weight w = p * s, p = exp(score - ...) and s its token's scale of values, comes from one exponential: log2(s) is
+// the score's initial value in the accumulators.  It enters the second product in half precision, raised so that the largest is
+// between 2^7 and 2^15: 11 bits down to 2^-21 of the largest weight times scale, steps of 2^-31 of it below.  The divisor adds up w / s in
+// 32 bits.
+constexpr float kRaised = 7, kHighest = 15;      // exponents
+constexpr float kNothing = 0x1p-64f;             // scale of values that are zeros: their weights count in the divisor
+
+// A wavefront's scales of a block, a token a lane, in LDS: log2(s) / unit and 1 / s.  What is no scale of a number belongs to a token
+// that is not seen, or to zeros.
+typedef float Scales[2][kKvBlock];
+__device__ __forceinline__ void put_scales(Scales &to, int lane, u32 scale, float per_unit) {
+    const float given = __uint_as_float(scale << 16), held = given >= 0x1p-100f && given < INFINITY ? given : kNothing;
+    to[0][lane] = __builtin_amdgcn_logf(held) * per_unit;
+    to[1][lane] = __builtin_amdgcn_rcpf(held);
+    __builtin_amdgcn_wave_barrier();                 // a wavefront's own: its instructions on LDS are done in order
+}
+// where the scale of a lane's token lies
+template <int G>
+__device__ __forceinline__ int scale_place(int lane) { return kv4_scales(G) + (lane % 16 / 4 * 16 + lane / 16 * 4 + lane % 4) * 2; }
+// exponents of a column that the base is taken off already; other lanes with the same column are `apart`, 32 and more
+template <int N, int M, class V, class O>
+__device__ __forceinline__ void raise_base(V (&x)[N], float most, int apart, float &base, float &limit, float &sum, O (&o)[M]) {
+    if (!__any(most > limit)) return;
+    for (int k = apart; k < 64; k <<= 1) most = fmaxf(most, __shfl_xor(most, k));
+    if (most > limit || most > kRaised) {
+        most -= kRaised;
+        const float was = limit == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(-most);          // nothing yet with the first base
+        base += most;
+        limit = kHighest;
+        sum *= was;
+#pragma unroll
+        for (int j = 0; j < M; ++j) o[j] *= was;
+#pragma unroll
+        for (int i = 0; i < N; ++i) x[i] -= most;
+    }
+}
+
 // Scores are products of the codes with their powers of two, exact in bfloat16, and of the queries in NQ bfloat16 parts (8 bits
 // each; a query of 8, 11 or 24 bits is all of its parts).  Of a block's scores a lane has 16 of one column's, and they are
 // the very weights that it hands to the second product, because the values' codes lie in that order of tokens: a block goes from memory
-// to the sums without LDS or an exchange between lanes, but for the largest score.  A weight takes its token's scale of
-// values along and is cut into NW parts.  A wavefront has blocks of its own; a workgroup's wavefronts are joined at the end.
-template <int G, int NQ, int NW, int kWaves>
+// to the sums without LDS or an exchange between lanes, but for the largest score.  FINE: a weight takes its token's scale of
+// values along and is cut into three bfloat16 parts, 24 bits; else as above.  A wavefront has blocks of its own; a workgroup's wavefronts are joined at the end.
+template <int G, int NQ, bool FINE, int kWaves>
 __global__ __launch_bounds__(64 * kWaves, G <= 4 ? 2 : 1) void kv4_attention_kernel(Attention a) {
     constexpr int NV = 2 * G;                                // tiles of 16 channels of values
+    constexpr size_t kHead = 64 * (33 * G + 2);
     constexpr int kRow = NV * 16 + 1;
     extern __shared__ float sums[];                          // of each wavefront and column
     __shared__ float stats[kWaves][kColumns][2];
+    __shared__ __attribute__((aligned(16))) Scales of_scales[FINE ? 1 : kWaves];
     const KvArgs &kv = a.kv;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 15, part = lane >> 4;
     int unit = blockIdx.x;
@@ -159,25 +199,31 @@ __global__ __launch_bounds__(64 * kWaves, G <= 4 ? 2 : 1) void kv4_attention_ker
     const int share = share_of(a, s.total), from = split * share, to = min(s.total, from + share);
     if (split && from >= s.total) return;
     // The next block's keys are under way while this one's weights are made, the one after's page too.
-    constexpr size_t kHead = 64 * (33 * G + 2);
     Keys<G> keys;
+    u32 scale = 0;
     int u = from + wave, page, page_next;
     auto page_at = [&](int v) { return v < to ? page_of(kv, b, s.block(v)) : -1; };
     // without a page the first one is read and not seen: no branch around what is under way
     auto data_of = [&](int page) { return (const char *)kv.codes + ((size_t)max(page, 0) * kv.heads + h) * kHead; };
+    auto load = [&](int page) __attribute__((always_inline)) {
+        const char *data = data_of(page);
+        load_keys<G>(data, col, part, keys);
+        if constexpr (!FINE) scale = *(const unsigned short *)(data + scale_place<G>(lane));
+    };
     page = page_at(u), page_next = page_at(u + kWaves);
-    if (u < to) load_keys<G>(data_of(page), col, part, keys);
+    if (u < to) load(page);
     // the column's query
     const int c = s.col0 + min(col, s.cols - 1), qi = c / a.group, g = c % a.group;
     const long row = s.start + qi;
     const int at = s.at_lo - s.col0 / a.group + qi, hq = h * a.group + g;
     v8b q[G][NQ];
     const bool bad = !load_query<G, NQ>(a, row, hq, part, q);
-    const float unit_q = a.scale * kLog2E;
+    const float unit_q = a.scale * kLog2E, per_unit = FINE ? 0.0f : 1.0f / unit_q;
     v4f o[NV];
 #pragma unroll
     for (int j = 0; j < NV; ++j) o[j] = v4f{0, 0, 0, 0};
-    float top = -INFINITY, sum = 0;
+    // FINE: the base is the largest score; else limit is what an exponent may be before the base is raised
+    float base = FINE ? -INFINITY : 0, limit = -INFINITY, sum = 0;
     for (; u < to; u += kWaves) {
         const int block = s.block(u), end = page < 0 ? 0 : kv.max_len;
         const char *data = data_of(page);
@@ -187,30 +233,39 @@ __global__ __launch_bounds__(64 * kWaves, G <= 4 ? 2 : 1) void kv4_attention_ker
             const int4 x = *(const int4 *)(data + 1024 * G + j * 1024 + lane * 16);
             values[j][0] = x.x, values[j][1] = x.y, values[j][2] = x.z, values[j][3] = x.w;
         }
-        u32 scales[8];
-        {
+        v4f scale_v[4];          // FINE: the scales; else their reciprocals
+        if constexpr (FINE) {
             const int4 *from = (const int4 *)(data + kv4_scales(G) + part * 32);
             const int4 x = from[0], y = from[1];
-            scales[0] = x.x, scales[1] = x.y, scales[2] = x.z, scales[3] = x.w, scales[4] = y.x, scales[5] = y.y, scales[6] = y.z, scales[7] = y.w;
-        }
-        float t[16], scale_v[16];
+            const u32 w[8] = {(u32)x.x, (u32)x.y, (u32)x.z, (u32)x.w, (u32)y.x, (u32)y.y, (u32)y.z, (u32)y.w};
 #pragma unroll
-        for (int k = 0; k < 8; ++k) scale_v[2 * k] = __uint_as_float(scales[k] << 16), scale_v[2 * k + 1] = __uint_as_float(scales[k] & 0xffff0000u);
+            for (int k = 0; k < 16; ++k) scale_v[k / 4][k % 4] = __uint_as_float(k & 1 ? w[k / 2] & 0xffff0000u : w[k / 2] << 16);
+        } else {
+            put_scales(of_scales[wave], lane, scale, per_unit);
+        }
+        v4f t[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            v4f acc = v4f{0, 0, 0, 0};
+            if constexpr (FINE)
+                t[i] = v4f{0, 0, 0, 0};
+            else
+                t[i] = *(const v4f *)&of_scales[wave][0][i * 16 + part * 4];
             v8b k[G];
 #pragma unroll
             for (int n = 0; n < G; ++n) k[n] = numbers_of(keys.code[i][n], power_of(keys.exponent[n], i));
 #pragma unroll
             for (int p = NQ - 1; p >= 0; --p)        // the small parts first
 #pragma unroll
-                for (int n = 0; n < G; ++n) acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k[n], q[n][p], acc, 0, 0, 0);
+                for (int n = 0; n < G; ++n) t[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k[n], q[n][p], t[i], 0, 0, 0);
 #pragma unroll
-            for (int r = 0; r < 4; ++r) t[4 * i + r] = acc[r] * unit_q;
+            for (int r = 0; r < 4; ++r) t[i][r] = FINE ? t[i][r] * unit_q : fmaf(t[i][r], unit_q, -base);
+        }
+        if constexpr (!FINE) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) scale_v[i] = *(const v4f *)&of_scales[wave][1][i * 16 + part * 4];
         }
         page = page_next;
-        load_keys<G>(data_of(page), col, part, keys);
+        load(page);
         page_next = page_at(u + 2 * kWaves);
         const int t0 = block * kKvBlock;
         if (t0 + 63 > s.at_lo || t0 + 64 > end || (a.window && t0 <= s.at_hi - a.window)) {
@@ -223,48 +278,67 @@ __global__ __launch_bounds__(64 * kWaves, G <= 4 ? 2 : 1) void kv4_attention_ker
                 for (int r = 0; r < 4; ++r) {
                     const int e = i * 16 + r;
                     const bool seen = (e <= hi) & ((e >= lo) | (e < sinks));
-                    t[4 * i + r] = seen ? t[4 * i + r] : -INFINITY;
-                    scale_v[4 * i + r] = seen ? scale_v[4 * i + r] : 0.0f;           // what is not seen may be no number
+                    t[i][r] = seen ? t[i][r] : -INFINITY;
+                    if constexpr (FINE) scale_v[i][r] = seen ? scale_v[i][r] : 0.0f;           // what is not seen may be no number
                 }
         }
-        float most = t[0];
+        float most = t[0][0];
 #pragma unroll
-        for (int i = 1; i < 16; ++i) most = fmaxf(most, t[i]);
-        most = fmaxf(most, __shfl_xor(most, 16));
-        most = fmaxf(most, __shfl_xor(most, 32));
-        if (__any(most > top)) {
-            const float now = fmaxf(top, most), was = now > top ? __builtin_amdgcn_exp2f(top - now) : 1.0f;
-            top = now;
-            sum *= was;
+        for (int i = 1; i < 16; ++i) most = fmaxf(most, t[i / 4][i % 4]);
+        if constexpr (FINE) {
+            most = fmaxf(most, __shfl_xor(most, 16));
+            most = fmaxf(most, __shfl_xor(most, 32));
+            if (__any(most > base)) {
+                const float now = fmaxf(base, most), was = now > base ? __builtin_amdgcn_exp2f(base - now) : 1.0f;
+                base = now;
+                sum *= was;
 #pragma unroll
-            for (int j = 0; j < NV; ++j) o[j] *= was;
-        }
-        const float base = top == -INFINITY ? 0.0f : top;
-        v8b w[2][NW];
-#pragma unroll
-        for (int half = 0; half < 2; ++half) {
-            float x[8];
-#pragma unroll
-            for (int k = 0; k < 8; ++k) {
-                const float p = __builtin_amdgcn_exp2f(t[8 * half + k] - base);
-                sum += p;
-                x[k] = p * scale_v[8 * half + k];
+                for (int j = 0; j < NV; ++j) o[j] *= was;
             }
-            parts_of<NW>(x, w[half]);
-        }
-#pragma unroll
-        for (int j = 0; j < NV; ++j) {
+            const float off = base == -INFINITY ? 0.0f : base;
+            v8b w[2][3];
 #pragma unroll
             for (int half = 0; half < 2; ++half) {
-                const v8b v = numbers_of(values[j >> 1][(j & 1) * 2 + half], 1.0f);
+                float x[8];
 #pragma unroll
-                for (int p = NW - 1; p >= 0; --p) o[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, w[half][p], o[j], 0, 0, 0);
+                for (int k = 0; k < 8; ++k) {
+                    const float p = __builtin_amdgcn_exp2f(t[2 * half + k / 4][k % 4] - off);
+                    sum += p;
+                    x[k] = p * scale_v[2 * half + k / 4][k % 4];
+                }
+                parts_of<3>(x, w[half]);
             }
+#pragma unroll
+            for (int j = 0; j < NV; ++j) {
+#pragma unroll
+                for (int half = 0; half < 2; ++half) {
+                    const v8b v = numbers_of(values[j >> 1][(j & 1) * 2 + half], 1.0f);
+#pragma unroll
+                    for (int p = 2; p >= 0; --p) o[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, w[half][p], o[j], 0, 0, 0);
+                }
+            }
+        } else {
+            raise_base(t, most, 16, base, limit, sum, o);
+            v8h w[2];
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    const float x = __builtin_amdgcn_exp2f(t[i][r]);
+                    sum = fmaf(x, scale_v[i][r], sum);
+                    w[i >> 1][(i & 1) * 4 + r] = (_Float16)x;
+                }
+#pragma unroll
+            for (int half = 0; half < 2; ++half)
+#pragma unroll
+                for (int j = 0; j < NV; ++j)
+                    o[j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(halves_of(values[j >> 1][(j & 1) * 2 + half]), w[half], o[j], 0, 0, 0);
         }
     }
     // the wavefronts' sums in one
     sum += __shfl_xor(sum, 16);
     sum += __shfl_xor(sum, 32);
+    if (!FINE && limit == -INFINITY) base = -INFINITY;
     if (col < a.columns) {
         float *mine = sums + (wave * a.columns + col) * kRow + part * 4;
 #pragma unroll
@@ -272,7 +346,7 @@ __global__ __launch_bounds__(64 * kWaves, G <= 4 ? 2 : 1) void kv4_attention_ker
 #pragma unroll
             for (int r = 0; r < 4; ++r) mine[j * 16 + r] = o[j][r];
     }
-    if (part == 0) stats[wave][col][0] = bad ? __builtin_nanf("") : top, stats[wave][col][1] = sum;
+    if (part == 0) stats[wave][col][0] = bad ? __builtin_nanf("") : base, stats[wave][col][1] = sum;
     __syncthreads();
     const long place = (((long)b * kv.heads + h) * a.tiles + tile) * a.splits + split;
     for (int e = threadIdx.x; e < s.cols * kv.dim; e += 64 * kWaves) {
@@ -280,10 +354,10 @@ __global__ __launch_bounds__(64 * kWaves, G <= 4 ? 2 : 1) void kv4_attention_ker
         float most = -INFINITY, all = 0, x = 0;
 #pragma unroll
         for (int k = 0; k < kWaves; ++k) most = fmaxf(most, stats[k][cc][0]);
-        const float base = most == -INFINITY ? 0.0f : most;
+        const float off = most == -INFINITY ? 0.0f : most;
 #pragma unroll
         for (int k = 0; k < kWaves; ++k) {
-            const float f = __builtin_amdgcn_exp2f(stats[k][cc][0] - base);       // NaN where the query is
+            const float f = __builtin_amdgcn_exp2f(stats[k][cc][0] - off);       // NaN where the query is
             all += f * stats[k][cc][1];
             x += f * sums[(k * a.columns + cc) * kRow + d];
         }
@@ -299,12 +373,7 @@ __global__ __launch_bounds__(64 * kWaves, G <= 4 ? 2 : 1) void kv4_attention_ker
 
 // ---- many queries of a sequence ---------------------------------------------------------------------------------------
 // A wavefront has 32 queries for all the keys that they see, in products of 32 x 32: those of 16 x 16 reach 0.7 of their rate, and
-// leave less room for the vector ALU between them (23 cycles for half the work, 31 with four multiply-adds; 33 and 35).  A
-// weight w = p * s, p = exp(score - ...) and s its token's scale of values, comes from one exponential: log2(s) is the score's initial
-// value in the accumulators.  It enters the second product in half precision, raised so that the largest is between 2^7 and 2^15: 11 bits down to
-// 2^-21 of the largest weight times scale, steps of 2^-31 of it below.  The divisor adds up w / s in 32 bits.
-constexpr float kRaised = 7, kHighest = 15;      // exponents
-constexpr float kNothing = 0x1p-64f;             // scale of values that are zeros: their weights count in the divisor
+// leave less room for the vector ALU between them (23 cycles for half the work, 31 with four multiply-adds; 33 and 35).
 constexpr int kWide = 32, kWavesOf = 4, kColumnsOf = kWide * kWavesOf;
 
 // Two lanes (halves) have a token's key: of two groups of 32 channels one each, of one left over half.  Product n takes their n-th words.
@@ -378,7 +447,7 @@ __global__ __launch_bounds__(64 * kWavesOf, G <= 4 ? 2 : 1) void kv4_attention_m
     typedef float v16f __attribute__((ext_vector_type(16)));
     typedef WideWords<G> W;
     constexpr size_t kHead = 64 * (33 * G + 2);
-    __shared__ __attribute__((aligned(16))) float of_scales[kWavesOf][2][kKvBlock];        // log2(s) / unit, 1 / s
+    __shared__ __attribute__((aligned(16))) Scales of_scales[kWavesOf];
     const KvArgs &kv = a.kv;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 31, half = lane >> 5;
     // Groups of queries that see most keys go first, of all sequences and heads.  A level is that many positions as a group has; a
@@ -428,12 +497,10 @@ __global__ __launch_bounds__(64 * kWavesOf, G <= 4 ? 2 : 1) void kv4_attention_m
     auto page_at = [&](int u) { return u < s.total ? page_of(kv, b, s.block(u)) : -1; };
     // without a page the first one is read and not seen: no branch around what is under way
     auto data_of = [&](int page) { return (const char *)kv.codes + ((size_t)max(page, 0) * kv.heads + h) * kHead; };
-    // tokens in the order of the scales' places, a lane each
-    const int of_lane = (lane & 15) / 4 * 16 + (lane >> 4) * 4 + (lane & 3);
     auto load = [&](int page) __attribute__((always_inline)) {
         const char *data = data_of(page);
         load_keys<G>(data, col, half, keys);
-        scale = *(const unsigned short *)(data + kv4_scales(G) + of_lane * 2);
+        scale = *(const unsigned short *)(data + scale_place<G>(lane));
     };
     int page = page_at(0), page_next = page_at(1);
     if (s.total) load(page);
@@ -449,13 +516,7 @@ __global__ __launch_bounds__(64 * kWavesOf, G <= 4 ? 2 : 1) void kv4_attention_m
                 const int2 x = *(const int2 *)(data + 1024 * G + j * 1024 + ((half + 2 * k) * 16 + (col & 15)) * 16 + (col >> 4) * 8);
                 values[j][0][k] = x.x, values[j][1][k] = x.y;
             }
-        {
-            // what is no scale of a number belongs to a token that is not seen, or to zeros
-            const float given = __uint_as_float(scale << 16), held = given >= 0x1p-100f && given < INFINITY ? given : kNothing;
-            of_scales[wave][0][lane] = __builtin_amdgcn_logf(held) * per_unit;
-            of_scales[wave][1][lane] = __builtin_amdgcn_rcpf(held);
-            __builtin_amdgcn_wave_barrier();                 // a wavefront's own: its instructions on LDS are done in order
-        }
+        put_scales(of_scales[wave], lane, scale, per_unit);
         v16f acc[2];
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
@@ -498,20 +559,7 @@ __global__ __launch_bounds__(64 * kWavesOf, G <= 4 ? 2 : 1) void kv4_attention_m
         for (int i = 0; i < 2; ++i)
 #pragma unroll
             for (int r = 0; r < 16; ++r) most = fmaxf(most, acc[i][r]);
-        if (__any(most > limit)) {
-            most = fmaxf(most, __shfl_xor(most, 32));
-            if (most > limit || most > kRaised) {
-                most -= kRaised;
-                const float was = limit == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(-most);          // nothing yet with the first base
-                base += most;
-                limit = kHighest;
-                sum *= was;
-#pragma unroll
-                for (int j = 0; j < G; ++j) o[j] *= was;
-#pragma unroll
-                for (int i = 0; i < 2; ++i) acc[i] -= most;
-            }
-        }
+        raise_base(acc, most, 32, base, limit, sum, o);
         v8h w[2][2];
 #pragma unroll
         for (int i = 0; i < 2; ++i)
@@ -614,13 +662,12 @@ size_t kv4_attention_workspace(const KvArgs &kv, int heads_q, int window, int si
 
 int launch_kv4_attention(void *stream, const KvArgs &kv, int heads_q, float scale, int window, int sinks, const Values &q,
                          const Values &out, void *workspace) {
-    const bool fine = q.type == GALA_F32 || q.type == GALA_RESIDUE || out.type == GALA_F32 || out.type == GALA_RESIDUE;
     // a score times log2(e) and the logarithm of a scale share an accumulator: neither may drown the other
     const float unit = std::fabs(scale) * kLog2E;
-    const bool apart = unit >= 0x1p-20f && unit <= 0x1p20f;
+    const bool fine = q.type == GALA_F32 || q.type == GALA_RESIDUE || out.type == GALA_F32 || out.type == GALA_RESIDUE ||
+                      !(unit >= 0x1p-20f && unit <= 0x1p20f);
     // f16 queries of more than 192 channels, in two parts, do not fit the registers beside a wide tile's sums
-    const bool fits = q.type != GALA_F16 || kv.dim <= 192;
-    const Cut c = cut_of(kv, heads_q, window, sinks, fine || !apart || !fits);
+    const Cut c = cut_of(kv, heads_q, window, sinks, fine || (q.type == GALA_F16 && kv.dim > 192));
     Attention a{};
     a.kv = kv, a.q = q, a.out = out;
     const size_t size = q.type == GALA_F32 ? 4 : q.type == GALA_RESIDUE ? 8 : 2;
@@ -651,11 +698,11 @@ int launch_kv4_attention(void *stream, const KvArgs &kv, int heads_q, float scal
             a.waves = W;
             const unsigned lds = W * c.columns * (32 * G + 1) * sizeof(float);
             if (fine)
-                hipLaunchKernelGGL((kv4_attention_kernel<G, 3, 3, W>), dim3(groups), dim3(64 * W), lds, (hipStream_t)stream, a);
+                hipLaunchKernelGGL((kv4_attention_kernel<G, 3, true, W>), dim3(groups), dim3(64 * W), lds, (hipStream_t)stream, a);
             else if (q.type == GALA_F16)
-                hipLaunchKernelGGL((kv4_attention_kernel<G, 2, 2, W>), dim3(groups), dim3(64 * W), lds, (hipStream_t)stream, a);
+                hipLaunchKernelGGL((kv4_attention_kernel<G, 2, false, W>), dim3(groups), dim3(64 * W), lds, (hipStream_t)stream, a);
             else
-                hipLaunchKernelGGL((kv4_attention_kernel<G, 1, 2, W>), dim3(groups), dim3(64 * W), lds, (hipStream_t)stream, a);
+                hipLaunchKernelGGL((kv4_attention_kernel<G, 1, false, W>), dim3(groups), dim3(64 * W), lds, (hipStream_t)stream, a);
         };
         if constexpr (G <= 4) {
             if (c.waves == 8)

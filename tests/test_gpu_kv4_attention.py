@@ -74,7 +74,7 @@ class Case:
     def check(self, out, rows=None):
         got, q = _plain(out), _plain(self.q)
         data = self.cache.data.cpu().numpy().reshape(-1, self.heads, ref.head_bytes(self.dim))
-        parts_w = 3 if {self.kind, self.out_kind} & {"f32", "residue"} else 2
+        fine = bool({self.kind, self.out_kind} & {"f32", "residue"})
         max_new, max_len = self.most or (max(self.new), max(self.lens))
         for b, (n, length) in enumerate(zip(self.new, self.lens)):
             end = min(length, max_len)
@@ -99,11 +99,11 @@ class Case:
                         assert np.isnan(got[row, h]).all()
                         continue
                     of = k[h // self.group, :tokens], v[h // self.group, :tokens]
-                    parts_q = PARTS_Q[self.kind] if parts_w == 2 else 3
-                    if parts_w == 2 and min(max(self.new), max_new) * self.group >= 64:
+                    parts_q = 3 if fine else PARTS_Q[self.kind]
+                    if not fine:
                         want, bound = ref.attention_in_halves(q[row, h], *of, scales[h // self.group, :tokens], seen, self.scale, parts_q)
                     else:
-                        want, bound = ref.attention(q[row, h], *of, seen, self.scale, parts_q, parts_w)
+                        want, bound = ref.attention(q[row, h], *of, seen, self.scale, parts_q, 3)
                     # one rounding to the output's type; half precision's smallest step
                     bound = bound + EPS.get(self.out_kind, 0) * (np.abs(want) + bound) + (UNIT / 2 if self.out_kind == "residue" else 0) + 2.0 ** -25
                     over = np.abs(got[row, h] - want) / bound
