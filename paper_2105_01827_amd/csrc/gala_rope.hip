@@ -124,7 +124,7 @@ int launch_rope_apply(void *stream, const gala_rope_axes &rope, const int *at, l
     const bool whole = in_pieces(x, dim) && in_pieces(out, dim) && rope.rot_dim / 2 % (rope.interleaved ? 4 : 8) == 0;
     Axes a{rope, at, at_stride, rows, heads, dim, 0, 0};
     if (whole) {
-        const long turns = std::min(8l, std::max(1l, (long)rows * each * heads / (256 * 512)));        // heads of a thread
+        const long turns = std::min(2l, std::max(1l, (long)rows * each * heads / (256 * 512)));        // heads of a thread
         a.slots = (int)((heads + turns - 1) / turns);
         a.slots = std::min(a.slots, std::max(1, 32768 / each));
         a.rows_of = std::max(1, kThreads / (each * a.slots));
