@@ -62,25 +62,40 @@ __device__ __forceinline__ void load_rotated(const Values &x, bool pieces, const
     const bool has = !rope.table || (t >= 0 && t < rope.positions);
     const float *table = rope.table && has ? rope.table + (long)t * rope.half * 2 : nullptr;
     if (pieces) {
+        // loads without branches between them, so that those of several pieces are under way together
+        const bool turned = rope.table && d < 2 * rope.half, second = !rope.interleaved && d >= rope.half;
+        const int own = d < dim ? d : 0, partner = !turned || rope.interleaved ? own : second ? d - rope.half : d + rope.half;
+        load_piece<TYPE>(x, row, h * dim + own, v);
+        if (rope.table) {
+            const long at = has ? t : 0;
+            const int pair = !turned ? 0 : rope.interleaved ? d / 2 : second ? d - rope.half : d;
+            float angles[16], other[8];
+            const float4 *from = (const float4 *)(rope.table + (at * rope.half + pair) * 2);
+#pragma unroll
+            for (int k = 0; k < 2; ++k) *(float4 *)(angles + 4 * k) = from[k];
+            if (!rope.interleaved) {
+#pragma unroll
+                for (int k = 2; k < 4; ++k) *(float4 *)(angles + 4 * k) = from[k];
+                load_piece<TYPE>(x, row, h * dim + partner, other);
+            }
+            if (turned) {
+                if (rope.interleaved) {
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) turn_pair(angles[2 * k], angles[2 * k + 1], v[2 * k], v[2 * k + 1]);
+                } else {
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) {
+                        float low = second ? other[k] : v[k], high = second ? v[k] : other[k];
+                        turn_pair(angles[2 * k], angles[2 * k + 1], low, high);
+                        v[k] = second ? high : low;
+                    }
+                }
+            }
+        }
         if (d >= dim) {
 #pragma unroll
             for (int k = 0; k < 8; ++k) v[k] = 0;
             return;
-        }
-        load_piece<TYPE>(x, row, h * dim + d, v);
-        if (table && d < 2 * rope.half) {
-            if (rope.interleaved) {
-                turn(table + d, v);
-            } else {
-                float other[8];
-                const bool second = d >= rope.half;
-                load_piece<TYPE>(x, row, h * dim + (second ? d - rope.half : d + rope.half), other);
-                if (second) {
-                    turn(table + 2 * (d - rope.half), other, v);
-                } else {
-                    turn(table + 2 * d, v, other);
-                }
-            }
         }
     } else {
         auto row_at = [&](int c) { return load_value<TYPE>(x, row, h * dim + c); };
@@ -127,19 +142,34 @@ __device__ void append_keys(const KvArgs &kv, const RopeArgs &rope, const Values
     const int groups = kv4_groups(kv.dim), count = o.hi - o.lo;
     char *data = (char *)kv.codes + ((size_t)o.page * kv.heads + h) * kv4_head_bytes(groups);
     const Divisor of(4 * groups);
-    for (int e = threadIdx.x; e < count * 4 * groups; e += THREADS) {
-        const int i = of(e), d = (e - i * 4 * groups) * 8, t = o.lo + i - o.at;
-        float v[8];
-        load_rotated<TYPE>(x, pieces, rope, o.start + (o.lo + i - o.first), o.lo + i, h, d, kv.dim, v);
-        float most = clean(v);
-        most = fmaxf(most, __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(most), 0xb1, 0xf, 0xf, true)));        // of the four lanes
-        most = fmaxf(most, __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(most), 0x4e, 0xf, 0xf, true)));
-        // most = f * 2^e with 1 <= f < 2: at most 7 * 2^(e-2) if f <= 7/4
-        const u32 bits = __float_as_uint(most);
-        const int exponent = min(max((int)(bits >> 23) - 127 - 2 + ((bits & 0x7fffffu) > 0x600000u), kLeastExponent), kMostExponent);
-        *(u32 *)(data + key_word(t, d, groups)) = codes_of(v, __uint_as_float((u32)(exponent + 127) << 23));
-        if ((e & 3) == 0) data[kv4_exponents(groups) + (d >> 5) * 64 + (t & 15) * 4 + (t >> 4)] = (char)(exponent + 127);
-    }
+    const int items = count * 4 * groups;
+    auto work = [&](auto n, int e0) __attribute__((always_inline)) {
+        constexpr int N = decltype(n)::value;
+        float v[N][8];
+#pragma unroll
+        for (int k = 0; k < N; ++k) {
+            const int e = k ? min(e0 + k * THREADS, items - 4 + (e0 & 3)) : e0, i = of(e), d = (e - i * 4 * groups) * 8;
+            load_rotated<TYPE>(x, pieces, rope, o.start + (o.lo + i - o.first), o.lo + i, h, d, kv.dim, v[k]);
+        }
+#pragma unroll
+        for (int k = 0; k < N; ++k) {
+            const int e = e0 + k * THREADS, i = of(e), d = (e - i * 4 * groups) * 8, t = o.lo + i - o.at;
+            if (e >= items) break;
+            float most = clean(v[k]);
+            most = fmaxf(most, __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(most), 0xb1, 0xf, 0xf, true)));        // of the four lanes
+            most = fmaxf(most, __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(most), 0x4e, 0xf, 0xf, true)));
+            // most = f * 2^e with 1 <= f < 2: at most 7 * 2^(e-2) if f <= 7/4
+            const u32 bits = __float_as_uint(most);
+            const int exponent = min(max((int)(bits >> 23) - 127 - 2 + ((bits & 0x7fffffu) > 0x600000u), kLeastExponent), kMostExponent);
+            *(u32 *)(data + key_word(t, d, groups)) = codes_of(v[k], __uint_as_float((u32)(exponent + 127) << 23));
+            if ((e & 3) == 0) data[kv4_exponents(groups) + (d >> 5) * 64 + (t & 15) * 4 + (t >> 4)] = (char)(exponent + 127);
+        }
+    };
+    // two pieces under way at a time, where there are as many
+    if (items > THREADS)
+        for (int e = threadIdx.x; e < items; e += 2 * THREADS) work(std::integral_constant<int, 2>(), e);
+    else if ((int)threadIdx.x < items)
+        work(std::integral_constant<int, 1>(), threadIdx.x);
 }
 
 // One workgroup: the values of one head in one touched block.  A token's scale needs its whole row, a word of codes eight tokens of
@@ -203,11 +233,12 @@ __device__ void append_values(const KvArgs &kv, const Values &x, bool pieces, in
     }
 }
 
-// Workgroups of a launch: one for the keys and one for the values of each head in each touched block, then those with `tokens` tokens'
-// queries each, `rows` of a sequence.
+// Workgroups of a launch: one for the keys and one for the values of each head in each touched block, then those with some
+// tokens' queries each, `rows` of a sequence.
 struct Shares {
     Order order;
-    int blocks, groups, tokens, rows;
+    int blocks, groups, rows;
+    Turns turns;
 };
 
 template <int TYPE, int OUT, int THREADS, int MOST>
@@ -225,11 +256,28 @@ __global__ __launch_bounds__(THREADS) void kv4_append_kernel(KvArgs kv, RopeArgs
         else
             append_keys<TYPE, THREADS>(kv, rope, k, pieces, h, o);
     } else {
-        const int u = blockIdx.x - shares.groups, b = u / shares.rows, i0 = (u - b * shares.rows) * shares.tokens;
-        if (pieces)
-            rotate_pieces<TYPE, OUT, THREADS>(kv, rope, q, q_out, Pieces(kv.dim, rope.half, rope.interleaved), heads_q, b, i0, shares.tokens);
-        else
-            for (int i = i0; i < min(i0 + shares.tokens, kv.max_new); ++i) rotate_row<TYPE, OUT, THREADS>(kv, rope, q, q_out, heads_q, b * kv.max_new + i);
+        const int all = blockIdx.x - shares.groups, u = all / shares.turns.parts, part = all - u * shares.turns.parts;
+        const int b = u / shares.rows, i0 = (u - b * shares.rows) * shares.turns.rows;
+        if (pieces) {
+            const int start = kv.starts[b], n = kv.starts[b + 1] - start, first = kv.lens[b] - n, most = min(n, kv.max_new);
+            turn_heads<TYPE, OUT, THREADS>(shares.turns, part, q, q_out, [&](int r) { return i0 + r < most ? (long)start + i0 + r : -1; },
+                                           [&](int r, bool two, bool turned, int d, float(&angle)[16]) __attribute__((always_inline)) {
+                const int t = first + i0 + r;
+                const bool has = !rope.table || (t >= 0 && t < rope.positions);
+                if (rope.table && has && turned) {
+                    const float4 *from = (const float4 *)(rope.table + ((long)t * rope.half + (two ? d : d / 2)) * 2);
+#pragma unroll
+                    for (int k = 0; k < 4; ++k)
+                        if (k < 2 || two) {
+                            const float4 x = from[k];
+                            angle[4 * k] = x.x, angle[4 * k + 1] = x.y, angle[4 * k + 2] = x.z, angle[4 * k + 3] = x.w;
+                        }
+                }
+                return has;
+            });
+        } else {
+            for (int i = i0; i < min(i0 + shares.turns.rows, kv.max_new); ++i) rotate_row<TYPE, OUT, THREADS>(kv, rope, q, q_out, heads_q, b * kv.max_new + i);
+        }
     }
 }
 
@@ -309,13 +357,13 @@ int launch_kv4_append(void *stream, const KvArgs &kv, const RopeArgs &rope, int 
             if constexpr (O != GALA_RESIDUE) {
                 auto launch = [&](auto threads, auto most) {
                     constexpr int N = decltype(threads)::value, M = decltype(most)::value;
-                    // two items a thread, where a sequence has as many
-                    const int items = std::max(1, heads_q * kv.dim / 16);
-                    Shares s{order_of(k.data ? kv.count * blocks : 0, kv.heads, kv.dim, k), blocks, 0,
-                             pieces ? std::max(1, std::min(2 * N / items, kv.max_new)) : 1, 0};
+                    Shares s{order_of(k.data ? kv.count * blocks : 0, kv.heads, kv.dim, k), blocks, 0, 0,
+                             turns_of((long)kv.count * kv.max_new, std::max(1, heads_q), kv.dim, rope.half, rope.interleaved, N)};
+                    s.turns.rows = pieces ? std::min(s.turns.rows, kv.max_new) : 1;
+                    if (!pieces) s.turns.parts = 1;
                     s.groups = s.order.groups();
-                    s.rows = (kv.max_new + s.tokens - 1) / s.tokens;
-                    hipLaunchKernelGGL((kv4_append_kernel<T, O, N, M>), dim3(s.groups + (heads_q ? kv.count * s.rows : 0)), dim3(N), 0,
+                    s.rows = (kv.max_new + s.turns.rows - 1) / s.turns.rows;
+                    hipLaunchKernelGGL((kv4_append_kernel<T, O, N, M>), dim3(s.groups + (heads_q ? kv.count * s.rows * s.turns.parts : 0)), dim3(N), 0,
                                        (hipStream_t)stream, kv, rope, heads_q, q, q_out, k, v, s, pieces);
                 };
                 const bool few = kv.max_new <= 16, narrow = kv.dim <= 128;

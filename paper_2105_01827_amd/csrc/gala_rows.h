@@ -159,6 +159,66 @@ __device__ void rotate_pieces(const KvArgs &kv, const RopeArgs &rope, const Valu
     }
 }
 
+// products and sums rounded one by one
+__device__ __forceinline__ void turn_pair(float cos, float sin, float &x, float &y) {
+#pragma clang fp contract(off)
+    const float a = cos * x - sin * y, b = cos * y + sin * x;
+    x = a, y = b;
+}
+// How a workgroup turns rows of heads: threads take a piece of a row, in the half layout both members of eight pairs, find its angles
+// once and turn it in every `slots`-th head.
+struct Turns {
+    Pieces pieces;
+    int half, heads, dim, slots;
+    int rows, parts;                         // rows of a workgroup, or workgroups of a row
+};
+inline Turns turns_of(long rows, int heads, int dim, int half, bool interleaved, int threads) {
+    const Pieces pieces(dim, half, interleaved);
+    const int each = std::max(1, pieces.pairs + pieces.singles);         // none in rows of less than a piece
+    // One head a thread where that does not fill the card twice: 6000 rows of 32 heads of 128 bf16 channels take 25.1 us with one, 22.7 with
+    // two, 23.5 with four.
+    const long turns = std::min(2l, std::max(1l, rows * each * heads / (256 * 512)));
+    int slots = (int)((heads + turns - 1) / turns);
+    slots = std::min(slots, std::max(1, 32768 / each));
+    return Turns{pieces, half, heads, dim, slots, std::max(1, threads / (each * slots)), (each * slots + threads - 1) / threads};
+}
+// part: of the row, where it has several workgroups; row_of(r): row r of the workgroup's, -1 for none; angles(row, two, d, angle): the angles of the piece at channel d, whether there are any
+template <int TYPE, int OUT, int THREADS, class R, class A>
+__device__ __forceinline__ void turn_heads(const Turns &t, int part, const Values &x, const Values &out, R row_of, A angles) {
+    const int pairs = t.pieces.pairs, each = pairs + t.pieces.singles, slots = t.slots, heads = t.heads, dim = t.dim, half = t.half;
+    const int e = part * THREADS + threadIdx.x;
+    const Divisor of_row(each * slots), of_each(each);
+    if (e < t.rows * each * slots) {
+        const int r = of_row(e), rest = e - r * each * slots, slot = of_each(rest), piece = rest - slot * each;
+        const long row = row_of(r);
+        if (row < 0) return;
+        const bool two = piece < pairs;
+        const int d = two ? piece * 8 : (pairs + piece) * 8;          // singles lie behind both members of the pairs
+        const bool turned = d < 2 * half;
+        float angle[16] = {};                    // cosine and sine of each pair
+        const bool has = angles(r, two, turned, d, angle);
+        // one head at a time: two under way take registers from other wavefronts (25.4 us against 22.7 for the rows above)
+        for (int h = slot; h < heads; h += slots) {
+            float u[8], v[8] = {};
+            load_piece<TYPE>(x, row, h * dim + d, u);
+            if (two) load_piece<TYPE>(x, row, h * dim + half + d, v);
+            if (turned && two) {
+#pragma unroll
+                for (int k = 0; k < 8; ++k) turn_pair(angle[2 * k], angle[2 * k + 1], u[k], v[k]);
+            } else if (turned) {
+#pragma unroll
+                for (int k = 0; k < 4; ++k) turn_pair(angle[2 * k], angle[2 * k + 1], u[2 * k], u[2 * k + 1]);
+            }
+            if (!has) {
+#pragma unroll
+                for (int k = 0; k < 8; ++k) u[k] = v[k] = __builtin_nanf("");
+            }
+            store_piece<OUT>(out, row, h * dim + d, u);
+            if (two) store_piece<OUT>(out, row, h * dim + half + d, v);
+        }
+    }
+}
+
 // The order of a launch's workgroups with a block of a head each.  Workgroups go to the eight XCDs in turn; where a head's
 // part of a row does not end on a cache line, neighbouring heads share lines, and all heads of a block go to one XCD.  8191
 // tokens of 72 heads of 80 f16 channels take 84 us so, with the export that follows them, and 90 us in turn; whole lines gain nothing
