@@ -440,7 +440,7 @@ int gala_kv_attention(const gala_ctx *ctx, void *stream, const gala_kv_cache *ca
                       int heads_q, float scale, int window, int sinks, const gala_values *q, const gala_values *out,
                       void *workspace, size_t workspace_bytes);
 
-/* The same cache in 4 bits, at 1 / 1.8 of the bytes.  A code is a sign (its bit 3) and one of the magnitudes 0, 1/2, 1, 3/2, 2, 3,
+/* The same cache in 4 bits, a little over half of the bytes.  A code is a sign (its bit 3) and one of the magnitudes 0, 1/2, 1, 3/2, 2, 3,
  * 4, 6 (its bits 0 to 2).  Every 32 channels of a token's key share a power of two: the smallest 2^e, -120 <= e <= 125, of which
  * the largest magnitude among them is at most 7 times.  A token's value in a head has one bfloat16 scale: max|x| * (1/6)
  * rounded to it, 0 where that is below 2^-100 (and the value is stored as zeros then).  x is stored as the code nearest
@@ -467,7 +467,8 @@ size_t gala_kv4_cache_bytes(int pages, int heads, int head_dim);
  * exact in bfloat16, with queries as they are (in up to three bfloat16 parts, 24 bits), sums in 32 bits; a weight times its
  * token's scale enters the second product in three bfloat16 parts, 24 bits, where q or out is GALA_F32 or GALA_RESIDUE.  Where
  * neither is (and |scale| is between 2^-20 and 2^19) it enters in half precision: 11 bits, in steps of 2^-31 of the largest so far at the
- * most where it is small; weights times scales of less than 2^-100 of the largest count for nothing, also in the divisor. */
+ * most where it is small; weights times scales of less than 2^-100 of the largest count for nothing, also in the divisor.  Scores have
+ * to stay within 32 bits: a query that meets one that does not gives NaN. */
 int gala_kv4_append(const gala_ctx *ctx, void *stream, const gala_kv4_cache *cache, const gala_kv_batch *batch,
                     const gala_rope *rope, int heads_q, const gala_values *q, const gala_values *q_out,
                     const gala_values *k, const gala_values *v);

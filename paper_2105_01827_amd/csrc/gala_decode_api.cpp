@@ -73,6 +73,8 @@ bool attention4_ok(const gala_kv4_cache *cache, const gala_kv_batch *batch, int 
 bool apart_or_same(const gala_values *a, const gala_values *b) {
     return !a || !b || a->data != b->data || (a->type == b->type && a->stride == b->stride);
 }
+// workgroups that turn a row's heads, at most: pieces of eight channels, a wavefront's worth each
+int64_t turning(int heads, int dim) { return ((int64_t)heads * ((dim + 7) / 8) + 63) / 64; }
 bool rope_ok(const gala_rope *rope, int dim) {
     return !rope || (rope->table && rope->positions >= 1 && rope->rot_dim >= 2 && rope->rot_dim % 2 == 0 && rope->rot_dim <= dim &&
                      (uintptr_t)rope->table % 8 == 0);
@@ -191,7 +193,9 @@ extern "C" int gala_kv4_append(const gala_ctx *c, void *stream, const gala_kv4_c
         return GALA_EARG;
     if ((q && k && q->type != k->type) || !rope_ok(rope, dim)) return GALA_EARG;
     const int64_t blocks = (batch->max_new + 62) / 64 + 1, of_blocks = batch->count * blocks + 7, rows = (int64_t)batch->count * batch->max_new;
-    if (!fits_launch(of_blocks, 256) || !fits_launch(rows, 256) || !fits_launch(of_blocks * cache->heads * 2 + rows, 256)) return GALA_EARG;
+    if (!fits_launch(of_blocks, 256) || !fits_launch(rows, 256) ||
+        !fits_launch(of_blocks * cache->heads * 2 + rows * std::max<int64_t>(1, turning(heads_q, dim)), 256))
+        return GALA_EARG;
     if (!c->has_device) return GALA_EHIP;
     if (!batch->count || !batch->max_new || (!q && !k)) return GALA_OK;
     const RopeArgs r{rope ? rope->table : nullptr, rope ? rope->positions : 0, rope ? rope->rot_dim / 2 : 0,
@@ -269,7 +273,7 @@ extern "C" int gala_rope_apply(const gala_ctx *c, void *stream, const gala_rope_
         if (rope->axis[i] >= rope->axes || rope->column[i] >= rope->columns) return GALA_EARG;
     const int64_t row = (int64_t)heads * head_dim;
     if (!values_ok(x, row, false) || !values_ok(out, row, true) || out->type == GALA_RESIDUE || !apart_or_same(x, out)) return GALA_EARG;
-    if (!fits_launch(rows, 256)) return GALA_EARG;
+    if (!fits_launch(rows, 256) || !fits_launch(rows * turning(heads, head_dim), 256)) return GALA_EARG;
     if (!c->has_device) return GALA_EHIP;
     if (!rows) return GALA_OK;
     return launch_rope_apply(stream, *rope, at, (long)at_stride, rows, heads, head_dim, values(c, x), values(c, out)) ? GALA_EHIP : GALA_OK;
