@@ -177,10 +177,13 @@ __device__ __forceinline__ void raise_base(V (&x)[N], float most, int apart, flo
 // each; a query of 8, 11 or 24 bits is all of its parts).  Of a block's scores a lane has 16 of one column's, and they are
 // the very weights that it hands to the second product, because the values' codes lie in that order of tokens: a block goes from memory
 // to the sums without LDS or an exchange between lanes, but for the largest score.  FINE: a weight takes its token's scale of
-// values along and is cut into three bfloat16 parts, 24 bits; else as above.  A wavefront has blocks of its own; a workgroup's wavefronts are joined at the end.
+// values along and is cut into three bfloat16 parts, 24 bits; else as above, where f16 comes in or out in two parts, 22 bits: one
+// rounding of a weight is as large as that of an f16 result, and few keys do not average it out.  A wavefront has blocks of its
+// own; a workgroup's wavefronts are joined at the end.
 template <int G, int NQ, bool FINE, int kWaves>
 __global__ __launch_bounds__(64 * kWaves, G <= 4 ? 2 : 1) void kv4_attention_kernel(Attention a) {
     constexpr int NV = 2 * G;                                // tiles of 16 channels of values
+    constexpr int kParts = NQ == 2 ? 2 : 1;                  // of a weight in half precision
     constexpr size_t kHead = 64 * (33 * G + 2);
     constexpr int kRow = NV * 16 + 1;
     extern __shared__ float sums[];                          // of each wavefront and column
@@ -319,20 +322,25 @@ __global__ __launch_bounds__(64 * kWaves, G <= 4 ? 2 : 1) void kv4_attention_ker
             }
         } else {
             raise_base(t, most, 16, base, limit, sum, o);
-            v8h w[2];
+            v8h w[2][kParts];
 #pragma unroll
             for (int i = 0; i < 4; ++i)
 #pragma unroll
                 for (int r = 0; r < 4; ++r) {
                     const float x = __builtin_amdgcn_exp2f(t[i][r]);
                     sum = fmaf(x, scale_v[i][r], sum);
-                    w[i >> 1][(i & 1) * 4 + r] = (_Float16)x;
+                    const _Float16 first = (_Float16)x;
+                    w[i >> 1][0][(i & 1) * 4 + r] = first;
+                    if constexpr (kParts == 2) w[i >> 1][1][(i & 1) * 4 + r] = (_Float16)(x - (float)first);
                 }
 #pragma unroll
             for (int half = 0; half < 2; ++half)
 #pragma unroll
-                for (int j = 0; j < NV; ++j)
-                    o[j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(halves_of(values[j >> 1][(j & 1) * 2 + half]), w[half], o[j], 0, 0, 0);
+                for (int j = 0; j < NV; ++j) {
+                    const v8h v = halves_of(values[j >> 1][(j & 1) * 2 + half]);
+#pragma unroll
+                    for (int p = kParts - 1; p >= 0; --p) o[j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, w[half][p], o[j], 0, 0, 0);
+                }
         }
     }
     // the wavefronts' sums in one
@@ -699,7 +707,7 @@ int launch_kv4_attention(void *stream, const KvArgs &kv, int heads_q, float scal
             const unsigned lds = W * c.columns * (32 * G + 1) * sizeof(float);
             if (fine)
                 hipLaunchKernelGGL((kv4_attention_kernel<G, 3, true, W>), dim3(groups), dim3(64 * W), lds, (hipStream_t)stream, a);
-            else if (q.type == GALA_F16)
+            else if (q.type == GALA_F16 || out.type == GALA_F16)
                 hipLaunchKernelGGL((kv4_attention_kernel<G, 2, false, W>), dim3(groups), dim3(64 * W), lds, (hipStream_t)stream, a);
             else
                 hipLaunchKernelGGL((kv4_attention_kernel<G, 1, false, W>), dim3(groups), dim3(64 * W), lds, (hipStream_t)stream, a);
