@@ -55,6 +55,11 @@ __device__ __forceinline__ void floats_of(u32 w, float (&x)[8]) {
     x[0] = a[0], x[1] = a[1], x[2] = b[0], x[3] = b[1], x[4] = c[0], x[5] = c[1], x[6] = d[0], x[7] = d[1];
 }
 
+// one member of a pair; products and the sum rounded one by one
+__device__ __forceinline__ float turned_by(float cos, float sin, float own, float other) {
+#pragma clang fp contract(off)
+    return cos * own + sin * other;
+}
 // A piece of eight channels of a row's head, as floats, 0 behind the head's end; of keys with the position rotated in (NaN where the
 // table does not have it).  `pieces`: rows are read in pieces, and pairs lie in them.
 template <int TYPE>
@@ -84,11 +89,7 @@ __device__ __forceinline__ void load_rotated(const Values &x, bool pieces, const
                     for (int k = 0; k < 4; ++k) turn_pair(angles[2 * k], angles[2 * k + 1], v[2 * k], v[2 * k + 1]);
                 } else {
 #pragma unroll
-                    for (int k = 0; k < 8; ++k) {
-                        float low = second ? other[k] : v[k], high = second ? v[k] : other[k];
-                        turn_pair(angles[2 * k], angles[2 * k + 1], low, high);
-                        v[k] = second ? high : low;
-                    }
+                    for (int k = 0; k < 8; ++k) v[k] = turned_by(angles[2 * k], second ? angles[2 * k + 1] : -angles[2 * k + 1], v[k], other[k]);
                 }
             }
         }
@@ -109,15 +110,22 @@ __device__ __forceinline__ void load_rotated(const Values &x, bool pieces, const
         for (int k = 0; k < 8; ++k) v[k] = __builtin_nanf("");
     }
 }
-// the largest finite magnitude of eight numbers; NaN among them becomes 0
-__device__ __forceinline__ float clean(float (&v)[8]) {
-    float most = 0;
+// the largest finite magnitude of eight numbers; NaN among them becomes 0.  `infinite`: infinities may be among them.
+__device__ __forceinline__ float clean(float (&v)[8], bool &infinite) {
+    u32 bits[8];
 #pragma unroll
-    for (int k = 0; k < 8; ++k) {
-        if (v[k] != v[k]) v[k] = 0;
-        if (fabsf(v[k]) < INFINITY) most = fmaxf(most, fabsf(v[k]));
+    for (int k = 0; k < 8; ++k) bits[k] = __float_as_uint(v[k]) & 0x7fffffffu;
+    u32 most = max(max(max(bits[0], bits[1]), max(bits[2], bits[3])), max(max(bits[4], bits[5]), max(bits[6], bits[7])));
+    infinite = __any(most >= 0x7f800000u);
+    if (infinite) {
+        most = 0;
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            if (bits[k] > 0x7f800000u) v[k] = 0;
+            if (bits[k] < 0x7f800000u) most = max(most, bits[k]);
+        }
     }
-    return most;
+    return __uint_as_float(most);
 }
 
 // The new tokens of one touched block of one sequence: [lo, hi) of the sequence, which lie in `page`.
@@ -155,7 +163,8 @@ __device__ void append_keys(const KvArgs &kv, const RopeArgs &rope, const Values
         for (int k = 0; k < N; ++k) {
             const int e = e0 + k * THREADS, i = of(e), d = (e - i * 4 * groups) * 8, t = o.lo + i - o.at;
             if (e >= items) break;
-            float most = clean(v[k]);
+            bool infinite;
+            float most = clean(v[k], infinite);
             most = fmaxf(most, __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(most), 0xb1, 0xf, 0xf, true)));        // of the four lanes
             most = fmaxf(most, __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(most), 0x4e, 0xf, 0xf, true)));
             // most = f * 2^e with 1 <= f < 2: at most 7 * 2^(e-2) if f <= 7/4
@@ -185,12 +194,14 @@ __device__ void append_values(const KvArgs &kv, const Values &x, bool pieces, in
     if (tid < kKvBlock) largest[tid] = 0;
     __syncthreads();
     float v[kItems][8];
+    bool infinite[kItems];
 #pragma unroll
     for (int k = 0; k < kItems; ++k) {
         const int e = tid + k * THREADS, i = of(e), d = (e - i * 4 * groups) * 8;
+        infinite[k] = false;
         if (i < count) {
             load_rotated<TYPE>(x, pieces, none, o.start + (o.lo + i - o.first), o.lo + i, h, d, kv.dim, v[k]);
-            atomicMax(&largest[t_lo + i], __float_as_uint(clean(v[k])));
+            atomicMax(&largest[t_lo + i], __float_as_uint(clean(v[k], infinite[k])));
         }
     }
     __syncthreads();
@@ -206,10 +217,14 @@ __device__ void append_values(const KvArgs &kv, const Values &x, bool pieces, in
 #pragma unroll
             for (int c = 0; c < 8; ++c) {
                 // the quotient rounded once: the remainder of a first one is exact
-                const float first = v[k][c] * inverse, rest = fmaf(-first, scale, v[k][c]), next = fmaf(rest, inverse, first);
-                q[c] = scale == 0 ? 0.0f : fabsf(v[k][c]) < INFINITY ? copysignf(next, v[k][c]) : v[k][c];
+                const float first = v[k][c] * inverse, rest = fmaf(-first, scale, v[k][c]);
+                q[c] = copysignf(fmaf(rest, inverse, first), v[k][c]);
             }
-            tile[t][d >> 3] = codes_of(q, 1.0f);
+            if (infinite[k]) {
+#pragma unroll
+                for (int c = 0; c < 8; ++c) q[c] = fabsf(v[k][c]) < INFINITY ? q[c] : v[k][c];
+            }
+            tile[t][d >> 3] = scale > 0 ? codes_of(q, 1.0f) : 0;
             if (d == 0) *(__bf16 *)(data + kv4_scales(groups) + ((t & 15) >> 2) * 32 + (t >> 4) * 8 + (t & 3) * 2) = (__bf16)scale;
         }
     }
