@@ -141,7 +141,8 @@ __device__ __forceinline__ bool load_query(const Attention &a, long row, int hq,
 // between 2^7 and 2^15: 11 bits down to 2^-21 of the largest weight times scale, steps of 2^-31 of it below.  The divisor adds up w / s in
 // 32 bits.
 constexpr float kRaised = 7, kHighest = 15;      // exponents
-constexpr float kNothing = 0x1p-64f;             // scale of values that are zeros: their weights count in the divisor
+constexpr float kNothing = 0x1p-88f;             // scale of values that are zeros: their weights count in the divisor
+constexpr float kOrdinary = 0x1p14f;             // up to here and down to kNothing w / s stays within 32 bits where its weight matters
 
 // A wavefront's scales of a block, a token a lane, in LDS: log2(s) / unit and 1 / s.  What is no scale of a number belongs to a token
 // that is not seen, or to zeros.
@@ -152,20 +153,50 @@ __device__ __forceinline__ void put_scales(Scales &to, int lane, u32 scale, floa
     to[1][lane] = __builtin_amdgcn_rcpf(held);
     __builtin_amdgcn_wave_barrier();                 // a wavefront's own: its instructions on LDS are done in order
 }
+// of a block's scales, all
+__device__ __forceinline__ bool ordinary_scale(u32 scale) {
+    const float s = __uint_as_float(scale << 16);
+    return !__any((s >= 0x1p-100f && s < kNothing) || (s > kOrdinary && s < INFINITY));
+}
+// From a wavefront's first scale on that is not ordinary (bfloat16 alone has such), a lane's divisor is sum * 2^apart with
+// the largest weight's exponent for `apart`: weights' own exponents are those of w less log2(s).
+template <int N>
+__device__ __forceinline__ void add_apart(const float (&x)[N], float &sum, float &apart) {
+    float most = sum > 0 ? apart : -INFINITY;
+#pragma unroll
+    for (int k = 0; k < N; ++k) most = fmaxf(most, x[k]);
+    if (most == -INFINITY) return;
+    sum = sum > 0 ? sum * __builtin_amdgcn_exp2f(apart - most) : 0.0f;
+#pragma unroll
+    for (int k = 0; k < N; ++k) sum += __builtin_amdgcn_exp2f(x[k] - most);
+    apart = most;
+}
+// ... and in the end, of lanes with the same column: what the column's sums are multiplied by
+__device__ __forceinline__ float joined_apart(int lanes, float &sum, float &apart) {
+    float most = sum > 0 ? apart : -INFINITY;
+    for (int k = lanes; k < 64; k <<= 1) most = fmaxf(most, __shfl_xor(most, k));
+    if (most == -INFINITY) most = 0;
+    sum = sum > 0 ? sum * __builtin_amdgcn_exp2f(apart - most) : 0.0f;
+    apart = most;
+    return __builtin_amdgcn_exp2f(-most);
+}
 // where the scale of a lane's token lies
 template <int G>
 __device__ __forceinline__ int scale_place(int lane) { return kv4_scales(G) + (lane % 16 / 4 * 16 + lane / 16 * 4 + lane % 4) * 2; }
-// exponents of a column that the base is taken off already; other lanes with the same column are `apart`, 32 and more
+// exponents of a column that the base is taken off already; other lanes with the same column are `lanes` and more apart
 template <int N, int M, class V, class O>
-__device__ __forceinline__ void raise_base(V (&x)[N], float most, int apart, float &base, float &limit, float &sum, O (&o)[M]) {
+__device__ __forceinline__ void raise_base(V (&x)[N], float most, int lanes, const bool ordinary, float &base, float &limit, float &sum, float &apart, O (&o)[M]) {
     if (!__any(most > limit)) return;
-    for (int k = apart; k < 64; k <<= 1) most = fmaxf(most, __shfl_xor(most, k));
+    for (int k = lanes; k < 64; k <<= 1) most = fmaxf(most, __shfl_xor(most, k));
     if (most > limit || most > kRaised) {
         most -= kRaised;
         const float was = limit == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(-most);          // nothing yet with the first base
         base += most;
         limit = kHighest;
-        sum *= was;
+        if (ordinary)
+            sum *= was;
+        else
+            apart -= most;
 #pragma unroll
         for (int j = 0; j < M; ++j) o[j] *= was;
 #pragma unroll
@@ -226,8 +257,9 @@ __global__ __launch_bounds__(64 * kWaves, G <= 4 ? 2 : 1) void kv4_attention_ker
 #pragma unroll
     for (int j = 0; j < NV; ++j) o[j] = v4f{0, 0, 0, 0};
     // FINE: the base is the largest score; else limit is what an exponent may be before the base is raised
-    float base = FINE ? -INFINITY : 0, limit = -INFINITY, sum = 0;
-    for (; u < to; u += kWaves) {
+    float base = FINE ? -INFINITY : 0, limit = -INFINITY, sum = 0, apart = 0;
+    auto step = [&](auto all_ordinary) __attribute__((always_inline)) {
+        constexpr bool ordinary = decltype(all_ordinary)::value;
         const int block = s.block(u), end = page < 0 ? 0 : kv.max_len;
         const char *data = data_of(page);
         u32 values[G][4];
@@ -244,6 +276,7 @@ __global__ __launch_bounds__(64 * kWaves, G <= 4 ? 2 : 1) void kv4_attention_ker
 #pragma unroll
             for (int k = 0; k < 16; ++k) scale_v[k / 4][k % 4] = __uint_as_float(k & 1 ? w[k / 2] & 0xffff0000u : w[k / 2] << 16);
         } else {
+            if (ordinary && !ordinary_scale(scale)) return false;
             put_scales(of_scales[wave], lane, scale, per_unit);
         }
         v4f t[4];
@@ -321,18 +354,26 @@ __global__ __launch_bounds__(64 * kWaves, G <= 4 ? 2 : 1) void kv4_attention_ker
                 }
             }
         } else {
-            raise_base(t, most, 16, base, limit, sum, o);
+            raise_base(t, most, 16, ordinary, base, limit, sum, apart, o);
+            if (!ordinary) {
+                float x[16];
+#pragma unroll
+                for (int k = 0; k < 16; ++k) x[k] = fmaf(-of_scales[wave][0][k / 4 * 16 + part * 4 + k % 4], unit_q, t[k / 4][k % 4]);
+                add_apart(x, sum, apart);
+            }
+            float added = 0;
             v8h w[2][kParts];
 #pragma unroll
             for (int i = 0; i < 4; ++i)
 #pragma unroll
                 for (int r = 0; r < 4; ++r) {
                     const float x = __builtin_amdgcn_exp2f(t[i][r]);
-                    sum = fmaf(x, scale_v[i][r], sum);
+                    added = fmaf(x, scale_v[i][r], added);
                     const _Float16 first = (_Float16)x;
                     w[i >> 1][0][(i & 1) * 4 + r] = first;
                     if constexpr (kParts == 2) w[i >> 1][1][(i & 1) * 4 + r] = (_Float16)(x - (float)first);
                 }
+            if (ordinary) sum += added;
 #pragma unroll
             for (int half = 0; half < 2; ++half)
 #pragma unroll
@@ -342,8 +383,19 @@ __global__ __launch_bounds__(64 * kWaves, G <= 4 ? 2 : 1) void kv4_attention_ker
                     for (int p = kParts - 1; p >= 0; --p) o[j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, w[half][p], o[j], 0, 0, 0);
                 }
         }
-    }
+        return true;
+    };
+    for (; u < to && step(std::true_type()); u += kWaves) {}
+    const bool ordinary = FINE || u >= to;
+    if constexpr (!FINE)
+        for (; u < to; u += kWaves) step(std::false_type());
     // the wavefronts' sums in one
+    if (!ordinary) {
+        const float f = joined_apart(16, sum, apart);
+        base += apart;
+#pragma unroll
+        for (int j = 0; j < NV; ++j) o[j] *= f;
+    }
     sum += __shfl_xor(sum, 16);
     sum += __shfl_xor(sum, 32);
     if (!FINE && limit == -INFINITY) base = -INFINITY;
@@ -466,12 +518,13 @@ __global__ __launch_bounds__(64 * kWavesOf, G <= 4 ? 2 : 1) void kv4_attention_m
     if (group < 0) return;
     const Seen s = seen_by(a, b, group * kWavesOf + wave, kWide);
     if (!s.cols) return;
-    const int mine = s.col0 + min(col, s.cols - 1), qi = mine / a.group, hq = h * a.group + mine % a.group;
-    const long row = s.start + qi;
+    const int mine = s.col0 + min(col, s.cols - 1), qi = mine / a.group;
     const int at = s.at_lo - s.col0 / a.group + qi;
     v8b q[2 * G][NQ];
-    bool bad;
+    u64 bad;                                 // a bit a lane
     {
+        const int hq = h * a.group + mine % a.group;
+        const long row = s.start + qi;
         int fine = 1;
         auto load = [&](auto type) __attribute__((always_inline)) {
 #pragma unroll
@@ -491,11 +544,11 @@ __global__ __launch_bounds__(64 * kWavesOf, G <= 4 ? 2 : 1) void kv4_attention_m
         else
             load(std::integral_constant<int, GALA_BF16>());
         fine &= __shfl_xor(fine, 32);
-        bad = !fine;
+        bad = __ballot(!fine);
     }
     const float unit_q = a.scale * kLog2E, per_unit = 1.0f / unit_q;
     v16f o[G];
-    float base = 0, limit = -INFINITY, sum = 0;       // limit: what an exponent may be before the base is raised
+    float base = 0, limit = -INFINITY, sum = 0, apart = 0;       // limit: what an exponent may be before the base is raised
 #pragma unroll
     for (int j = 0; j < G; ++j)
 #pragma unroll
@@ -512,9 +565,12 @@ __global__ __launch_bounds__(64 * kWavesOf, G <= 4 ? 2 : 1) void kv4_attention_m
     };
     int page = page_at(0), page_next = page_at(1);
     if (s.total) load(page);
-    for (int u = 0; u < s.total; ++u) {
+    // Two loops: a branch among the weights costs heads of 128 channels 1 %, of 64 and 256 5 %
+    int u = 0;
+    auto step = [&](auto ordinary) __attribute__((always_inline)) {
         const int block = s.block(u), end = page < 0 ? 0 : kv.max_len, t0 = block * kKvBlock;
         const char *data = data_of(page);
+        if (!ordinary) load(page);               // no registers for the next one's
         // of 16 tokens that a lane's scores of a tile are: those of the first and third four, of the second and fourth
         u32 values[G][2][2];
 #pragma unroll
@@ -545,7 +601,7 @@ __global__ __launch_bounds__(64 * kWavesOf, G <= 4 ? 2 : 1) void kv4_attention_m
                 for (int p = NQ - 1; p >= 0; --p) acc[i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k, q[n][p], acc[i], 0, 0, 0);
             }
         page = page_next;
-        load(page);
+        if (ordinary) load(page);
         page_next = page_at(u + 2);
 #pragma unroll
         for (int i = 0; i < 2; ++i)
@@ -567,7 +623,17 @@ __global__ __launch_bounds__(64 * kWavesOf, G <= 4 ? 2 : 1) void kv4_attention_m
         for (int i = 0; i < 2; ++i)
 #pragma unroll
             for (int r = 0; r < 16; ++r) most = fmaxf(most, acc[i][r]);
-        raise_base(acc, most, 32, base, limit, sum, o);
+        raise_base(acc, most, 32, ordinary, base, limit, sum, apart, o);
+        if (!ordinary) {
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) {             // one at a time: registers
+                    const float x[1] = {fmaf(-of_scales[wave][0][i * 32 + r / 4 * 8 + half * 4 + r % 4], unit_q, acc[i][r])};
+                    add_apart(x, sum, apart);
+                }
+        }
+        float added = 0;
         v8h w[2][2];
 #pragma unroll
         for (int i = 0; i < 2; ++i)
@@ -577,20 +643,29 @@ __global__ __launch_bounds__(64 * kWavesOf, G <= 4 ? 2 : 1) void kv4_attention_m
 #pragma unroll
                 for (int r = 0; r < 4; ++r) {
                     const float x = __builtin_amdgcn_exp2f(acc[i][4 * k + r]);
-                    sum = fmaf(x, inverse[r], sum);
+                    added = fmaf(x, inverse[r], added);
                     w[i][k & 1][(k >> 1) * 4 + r] = (_Float16)x;
                 }
             }
+        if (ordinary) sum += added;
 #pragma unroll
         for (int i = 0; i < 2; ++i)
 #pragma unroll
             for (int k = 0; k < 2; ++k)
 #pragma unroll
                 for (int j = 0; j < G; ++j) o[j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(halves_of(values[j][i][k]), w[i][k], o[j], 0, 0, 0);
-    }
+    };
+    for (; u < s.total && ordinary_scale(scale); ++u) step(std::true_type());
+    const bool ordinary = u >= s.total;
+    for (; u < s.total; ++u) step(std::false_type());
+    const float by = ordinary ? 1.0f : joined_apart(32, sum, apart);
     sum += __shfl_xor(sum, 32);
-    const float f = bad ? __builtin_nanf("") : sum > 0 ? 1.0f / sum : 0.0f;
+    const float f = bad >> lane & 1 ? __builtin_nanf("") : sum > 0 ? by / sum : 0.0f;
     if (col >= s.cols) return;
+    int column = s.col0 + col;
+    asm("" : "+v"(column));                  // found anew: no registers for its row and head in the loop
+    const int hq = h * a.group + column % a.group;
+    const long row = s.start + column / a.group;
     auto store = [&](auto type) __attribute__((always_inline)) {
         constexpr int T = decltype(type)::value;
         typedef typename Element<T>::type E;

@@ -150,7 +150,8 @@ def attention(q, k, v, seen, scale, parts_q, parts_w):
 
 def attention_in_halves(q, k, v, scales, seen, scale, parts_q):
     """The same with weights times scales of values (`scales`, a token each) in half precision: rounded by at most 2^-11 of
-    themselves, or by half a step of 2^-31 of the largest of them; the scale's logarithm is one more term of a score's sum."""
+    themselves, or by half a step of 2^-31 of the largest of them; the scale's logarithm is one more term of a score's sum,
+    88 in binary where the scale is 0."""
     dim = len(q)
     if not seen.any():
         return np.zeros(dim), np.zeros(dim)
@@ -159,7 +160,7 @@ def attention_in_halves(q, k, v, scales, seen, scale, parts_q):
     w = np.exp(s - s.max())
     out = (w[:, None] * v).sum(0) / w.sum()
     u = 2.0 ** -24
-    size = abs(scale) * (np.abs(k) @ np.abs(q)).max() + np.abs(np.log(np.where(scales > 0, scales, 2.0 ** -64))).max()
+    size = abs(scale) * (np.abs(k) @ np.abs(q)).max() + np.abs(np.log(np.where(scales > 0, scales, 2.0 ** -88))).max()
     slack = (dim * parts_q + 16) * u * size + 8 * u * (np.abs(s).max() + 1)
     spread = (w[:, None] * np.abs(v)).sum(0) / w.sum()
     bound = 2 * np.expm1(2 * slack) * spread + 2.0 ** -11 * spread + (len(w) + 64) * u * spread

@@ -200,6 +200,27 @@ def test_exponents_and_scales_far_apart(ctx, kind, new):
         c.check(c.run(scale=scale), rows)
 
 
+@pytest.mark.parametrize("kind,new,length", [("bf16", 1, 500), ("bf16", 140, 500), ("f16", 1, 7000), ("f32", 2, 500)])
+@pytest.mark.parametrize("some", [(-99,), (110,), (110, -60), (100, 60, -30, -99)])
+def test_scales_further_apart_than_32_bits(ctx, kind, new, length, some):
+    """Scales of 2^some, none and ordinary ones, in any order: a token's weight counts in the divisor whatever its value's scale is."""
+    c = Case(ctx, [new, 4], [length, 300], 2, 2, 64, kind, "f32" if kind == "f32" else "bf16", seed=71, spread=0.5)
+    k, v, e, s = ref.places(64)
+    data = c.cache.data.view(-1, 2, ref.head_bytes(64)).cpu().numpy()
+    rng = np.random.default_rng(len(some) + new)
+    choice = np.array([0] + [x + 127 << 7 for x in (0, -3) + some])
+    for p in range(data.shape[0]):
+        for h in range(2):
+            live = (data[p, h, s + 1] < 255).copy()
+            bits = choice[rng.integers(0, len(choice), 64)]
+            if p % 3 == 0:
+                bits = choice[rng.integers(0, 3, 64)]           # blocks with ordinary scales alone, before and behind the others
+            data[p, h, s] = np.where(live, bits & 255, data[p, h, s])
+            data[p, h, s + 1] = np.where(live, bits >> 8, data[p, h, s + 1])
+    c.cache.data.copy_(torch.from_numpy(data).view(c.cache.data.shape))
+    c.check(c.run(), None if new < 3 else {(0, 0), (0, 77), (0, 139), (1, 3)})
+
+
 def test_many_small_weights_beside_a_large_one(ctx):
     """The first key has nearly all weight and a value of nothing; thousands of others share the rest."""
     for kind in ("bf16", "f16", "f32"):
