@@ -508,6 +508,8 @@ class Context:
         a row) float32, one for every ``group`` columns (0: for the row)."""
         shape = x.shape
         if len(shape) != 2:
+            if len(shape) < 2:
+                raise ValueError("x has to hold rows of numbers")
             shape = (shape[0], math.prod(shape[1:]))
         rows, width = shape
         at = 0

@@ -200,6 +200,12 @@ def test_norm_refuses_other_shapes(change):
         Context().rms_norm(**(dict(x=_on_gpu(5, 8), out=_on_gpu(5, 8)) | change))
 
 
+def test_norm_refuses_a_row_that_is_no_row():
+    for shape in ((8,), ()):
+        with pytest.raises(ValueError):
+            Context().rms_norm(_on_gpu(*shape), _on_gpu(*shape))
+
+
 @pytest.mark.parametrize("change", [dict(x=torch.zeros(5, 8)), dict(add=torch.zeros(5, 8)), dict(add=_on_gpu(5, 8, dtype=torch.int8)), dict(x=_on_gpu(5, 8, dtype=torch.float64)),
                                     dict(scales=torch.zeros(5), out=_on_gpu(5, 8, dtype=torch.int8)), dict(scales=_on_gpu(5, dtype=torch.float64), out=_on_gpu(5, 8, dtype=torch.int8))])
 def test_norm_refuses_other_tensors(change):
