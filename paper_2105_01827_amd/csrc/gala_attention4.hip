@@ -211,6 +211,9 @@ __device__ __forceinline__ void raise_base(V (&x)[N], float most, int lanes, con
 // values along and is cut into three bfloat16 parts, 24 bits; else as above, where f16 comes in or out in two parts, 22 bits: one
 // rounding of a weight is as large as that of an f16 result, and few keys do not average it out.  A wavefront has blocks of its
 // own; a workgroup's wavefronts are joined at the end.
+// Bound by HBM where the cache is large (64 queries of up to 8192 tokens, 424 MB: 86 us, 4.9 TB/s; 131072 tokens, 70 MB: 18 us and 5
+// for the join), by a chain of starts, table, codes where it is not (1000 tokens 8.8 us).  Products of 16 x 16: of few queries most
+// columns are empty, and a tile of 32 would have twice as many.
 template <int G, int NQ, bool FINE, int kWaves>
 __global__ __launch_bounds__(64 * kWaves, G <= 4 ? 2 : 1) void kv4_attention_kernel(Attention a) {
     constexpr int NV = 2 * G;                                // tiles of 16 channels of values
@@ -434,6 +437,10 @@ __global__ __launch_bounds__(64 * kWaves, G <= 4 ? 2 : 1) void kv4_attention_ker
 // ---- many queries of a sequence ---------------------------------------------------------------------------------------
 // A wavefront has 32 queries for all the keys that they see, in products of 32 x 32: those of 16 x 16 reach 0.7 of their rate, and
 // leave less room for the vector ALU between them (23 cycles for half the work, 31 with four multiply-adds; 33 and 35).
+// Keys and values come to the registers straight from memory: through LDS they are loaded once a workgroup, but its wavefronts wait for
+// each other (4 x 4096 queries over 8192 tokens 1671 us against 1600).  Bound by the vector ALU (0.57 of the SIMDs' cycles) and the products
+// (0.38), which the two wavefronts of a SIMD overlap little: 2000 and 1258 queries over 5207 and 3276 tokens, 192 G of operations, 0.8 to 0.9 P
+// a second, 4 x 4096 over 8192 1.03.
 constexpr int kWide = 32, kWavesOf = 4, kColumnsOf = kWide * kWavesOf;
 
 // Two lanes (halves) have a token's key: of two groups of 32 channels one each, of one left over half.  Product n takes their n-th words.

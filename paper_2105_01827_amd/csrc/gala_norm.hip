@@ -138,8 +138,11 @@ struct Rows {
     Values x, add, sum, weight, out;
 };
 
-// A row stays in the registers of THREADS threads, N pieces of eight numbers each: one pass over memory.  Rows of up to a wavefront's
-// registers share a workgroup of four.
+// A row stays in the registers of THREADS threads, N pieces of eight numbers each: one pass over memory, which bounds long calls (8191 rows
+// of 4096 bf16 numbers, 235 MB, 53 us: 4.4 TB/s; rows off 16 bytes 78 us, their stores split lines).  Few rows are a launch and one chain
+// of loads, a sum over the workgroup and stores (1 x 2048 4.4 us, 64 x 5120 6.1 us).  Rows of up to a wavefront's registers share
+// a workgroup of four.  The sum of squares is kept in 64 bits: its rounding to the 32-bit factor then is the same in any order of
+// addition but for one case in 2^28 or so, and codes with it.
 template <int THREADS, int N, bool WHOLE>
 __global__ __launch_bounds__(THREADS < 256 ? 256 : THREADS) void rms_norm_kernel(Rows a) {
 #pragma clang fp contract(off)
