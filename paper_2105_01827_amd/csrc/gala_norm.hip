@@ -350,6 +350,9 @@ int launch_rms_norm(void *stream, const NormArgs &how, const Values &x, const Va
     };
     const std::integral_constant<int, 1> one;
     const std::integral_constant<int, 2> two;
+    // One or two pieces a thread, a wavefront a row where one holds it: with four pieces 1000 x 8192 take 20.1 us instead of 17.8, 1000 x 16384 37.8
+    // instead of 34.4, 4000 x 2048 20.3 (a wavefront a row) instead of 15.8; with one instead of two 1000 x 8192 22.5, 8191 x 4095
+    // 81 instead of 78.5 (64 x 4096 4.6 instead of 5.1).
     if (width <= 512)
         launch(std::integral_constant<int, 64>(), one);
     else if (width <= 2048)
