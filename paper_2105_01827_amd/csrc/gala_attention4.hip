@@ -721,7 +721,11 @@ Cut cut_of(const KvArgs &kv, int heads_q, int window, int sinks, bool fine) {
     const long keys = window ? std::min(reach, (long)window + kv.max_new + sinks + 2 * kKvBlock) : reach;
     const long blocks = std::max(1l, (keys + kKvBlock - 1) / kKvBlock);
     const long groups = (columns + kColumnsOf - 1) / kColumnsOf * kv.count * kv.heads;
-    c.many = !fine && columns >= kColumnsOf && (groups >= 192 || blocks <= 16);
+    // Wide tiles take their time whatever the groups are until those fill the card, narrow ones with shares of the keys grow with them.  128
+    // channels of bf16, 1000 tokens: 64 groups 27 us and 17, 128 27 and 27, 160 27 and 31; 6000 tokens: 160 groups 114 and 95, 256 120 and
+    // 149.  64 channels, 1000 tokens: 160 groups 21 and 21; 256 channels: 64 groups 47 and 39, 96 47 and 57.
+    const int g32 = kv4_groups(kv.dim), fives = g32 <= 2 ? 6 : g32 <= 4 ? 5 : 3;
+    c.many = !fine && columns >= kColumnsOf && groups >= std::min(192l, 96 + 2 * blocks) * fives / 5;
     if (c.many) {
         c.tiles = (int)((columns + kColumnsOf - 1) / kColumnsOf), c.splits = 1, c.columns = 0;
         return c;
@@ -733,7 +737,7 @@ Cut cut_of(const KvArgs &kv, int heads_q, int window, int sinks, bool fine) {
     // workgroups of 32 bits 121 and 114.  Shares for one round of the card, of 8 blocks at least, where there are 48: 4000 tokens take 18.5 us
     // whole and 11.6 in shares.  Wide heads leave room for one wavefront a SIMD.
     const long units = std::max(1l, (long)kv.count * kv.heads * c.tiles);
-    const bool wide = kv4_groups(kv.dim) > 4;
+    const bool wide = g32 > 4;
     const bool few = !wide && (units <= 128 || (units <= 256 && blocks < 128));
     const long room = few || wide ? 256 : 512;
     c.waves = few ? 8 : 4;
