@@ -325,6 +325,15 @@ def test_a_long_sequence(ctx):
         assert torch.equal(c.run(), out)
 
 
+@pytest.mark.parametrize("count", [33, 64, 65, 100])
+def test_prompts_of_many_sequences(ctx, count):
+    """As many as a wavefront has lanes, more, and a number that is no power of two; lengths of all kinds, some without new tokens."""
+    new = [(b * 53) % 140 if b % 7 else 0 for b in range(count)]
+    new[5] = 140
+    c = Case(ctx, new, [n + (b * 29) % 200 for b, n in enumerate(new)], 4, 2, 32, "bf16", seed=count)
+    c.check(c.run(), {(b, i) for b in range(count) for i in (0, new[b] - 1) if new[b]})
+
+
 def test_prompts_are_the_same_bits_again(ctx):
     c = Case(ctx, [300, 200], [400, 200], 8, 4, 96, "f16", seed=53)
     want = c.run()
