@@ -12,7 +12,7 @@ SOURCES = ["gala_host.cpp", "gala_api.cpp", "gala_kernels.hip", "gala_conv_mfma.
            "gala_decode_api.cpp", "gala_kv.hip", "gala_attention.hip", "gala_sample.hip",
            "gala_kv4.hip", "gala_attention4.hip", "gala_rope.hip", "gala_norm.hip",
            "gala_ring1024.hip", "gala_ring2048.hip", "gala_ring4096.hip", "gala_ring8192.hip"]
-HEADERS = ["gala_internal.h", "gala_ring_impl.h", "gala_decode.h", "gala_rows.h", "gala_attention.h", "modarith.h", os.path.join("..", "..", "include", "gala.h")]
+HEADERS = ["gala_internal.h", "gala_ring_impl.h", "gala_decode.h", "gala_rows.h", "gala_attention.h", "gala_attention4_cut.h", "modarith.h", os.path.join("..", "..", "include", "gala.h")]
 # packed-FP32 instructions are switched off for every device compile on the test machines
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-pthread", "-Wno-unused-value", "-Wno-unused-command-line-argument",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops"]

@@ -13,9 +13,6 @@ namespace {
 typedef int v4i __attribute__((ext_vector_type(4)));
 typedef float v4f __attribute__((ext_vector_type(4)));
 
-constexpr int kColumns = 16;         // queries that a wavefront's products take at once
-constexpr float kLog2E = 1.4426950408889634f;
-
 struct Attention {
     KvArgs kv;
     Values q, out;

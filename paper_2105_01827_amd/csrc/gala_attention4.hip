@@ -1,7 +1,6 @@
 // Attention of a batch's queries over the paged 4-bit cache.
-#include <cmath>
-
 #include "gala_attention.h"
+#include "gala_attention4_cut.h"
 
 using namespace gala;
 
@@ -448,8 +447,6 @@ __global__ __launch_bounds__(64 * kWaves, G <= 4 ? 2 : 1) void kv4_attention_ker
 // each other (4 x 4096 queries over 8192 tokens 1671 us against 1600).  Bound by the vector ALU (0.57 of the SIMDs' cycles) and the products
 // (0.38), which the two wavefronts of a SIMD overlap little: 2000 and 1258 queries over 5207 and 3276 tokens, 192 G of operations, 0.8 to 0.9 P
 // a second, 4 x 4096 over 8192 1.03.
-constexpr int kWide = 32, kWavesOf = 4, kColumnsOf = kWide * kWavesOf;
-
 // Two lanes (halves) have a token's key: of two groups of 32 channels one each, of one left over half.  Product n takes their n-th words.
 template <int G>
 struct WideWords {
@@ -718,43 +715,6 @@ __global__ __launch_bounds__(64 * kWavesOf, G <= 4 ? 2 : 1) void kv4_attention_m
         store(std::integral_constant<int, GALA_BF16>());
 }
 
-// How a call is cut up.
-struct Cut {
-    bool many;
-    int tiles, splits, columns, waves;
-    long places() const { return (long)tiles * splits * columns; }
-};
-Cut cut_of(const KvArgs &kv, int heads_q, int window, int sinks, bool fine) {
-    Cut c;
-    const long columns = (long)kv.max_new * (heads_q / kv.heads);
-    const long reach = std::min<long>(kv.max_len, (long)kv.table_stride * kKvBlock);
-    const long keys = window ? std::min(reach, (long)window + kv.max_new + sinks + 2 * kKvBlock) : reach;
-    const long blocks = std::max(1l, (keys + kKvBlock - 1) / kKvBlock);
-    const long groups = (columns + kColumnsOf - 1) / kColumnsOf * kv.count * kv.heads;
-    // Wide tiles take their time whatever the groups are until those fill the card, narrow ones with shares of the keys grow with them.  128
-    // channels of bf16, 1000 tokens: 64 groups 27 us and 17, 128 27 and 27, 160 27 and 31; 6000 tokens: 160 groups 114 and 95, 256 120 and
-    // 149.  64 channels, 1000 tokens: 160 groups 21 and 21; 256 channels: 64 groups 47 and 39, 96 47 and 57.
-    const int g32 = kv4_groups(kv.dim), fives = g32 <= 2 ? 6 : g32 <= 4 ? 5 : 3;
-    c.many = !fine && columns >= kColumnsOf && groups >= std::min(192l, 96 + 2 * blocks) * fives / 5;
-    if (c.many) {
-        c.tiles = (int)((columns + kColumnsOf - 1) / kColumnsOf), c.splits = 1, c.columns = 0;
-        return c;
-    }
-    c.tiles = (int)((columns + kColumns - 1) / kColumns);
-    c.columns = (int)std::min<long>(columns, kColumns);
-    // A block takes a wavefront 1.2 us after the other, joining shares 5 us.  Eight wavefronts a workgroup where that leaves CUs with one:
-    // 32 windows of 1024 tokens take 12.3 us so and 14.5 with four, one sequence of 131072 25.0 and 26.4; 64 of 8192 in 512
-    // workgroups of 32 bits 121 and 114.  Shares for one round of the card, of 8 blocks at least, where there are 48: 4000 tokens take 18.5 us
-    // whole and 11.6 in shares.  Wide heads leave room for one wavefront a SIMD.
-    const long units = std::max(1l, (long)kv.count * kv.heads * c.tiles);
-    const bool wide = g32 > 4;
-    const bool few = !wide && (units <= 128 || (units <= 256 && blocks < 128));
-    const long room = few || wide ? 256 : 512;
-    c.waves = few ? 8 : 4;
-    c.splits = blocks < 48 ? 1 : (int)std::max(1l, std::min(room / units, blocks / 8));
-    return c;
-}
-
 }  // namespace
 
 namespace gala {
@@ -766,12 +726,8 @@ size_t kv4_attention_workspace(const KvArgs &kv, int heads_q, int window, int si
 
 int launch_kv4_attention(void *stream, const KvArgs &kv, int heads_q, float scale, int window, int sinks, const Values &q,
                          const Values &out, void *workspace) {
-    // a score times log2(e) and the logarithm of a scale share an accumulator: neither may drown the other
-    const float unit = std::fabs(scale) * kLog2E;
-    const bool fine = q.type == GALA_F32 || q.type == GALA_RESIDUE || out.type == GALA_F32 || out.type == GALA_RESIDUE ||
-                      !(unit >= 0x1p-20f && unit <= 0x1p20f);
-    // f16 queries of more than 192 channels, in two parts, do not fit the registers beside a wide tile's sums
-    const Cut c = cut_of(kv, heads_q, window, sinks, fine || (q.type == GALA_F16 && kv.dim > 192));
+    const bool fine = !in_halves(scale, q.type, out.type);
+    const Cut c = cut_of(kv, heads_q, window, sinks, fine || !fits_wide(q.type, kv.dim));
     Attention a{};
     a.kv = kv, a.q = q, a.out = out;
     const size_t size = q.type == GALA_F32 ? 4 : q.type == GALA_RESIDUE ? 8 : 2;

@@ -8,6 +8,8 @@ namespace gala {
 
 constexpr int kKvBlock = GALA_KV_BLOCK;
 constexpr int kMaxHeadDim = 256;
+constexpr int kColumns = 16;         // queries that a wavefront's products of attention take at once
+constexpr float kLog2E = 1.4426950408889634f;
 
 // Values of a call, as kernels take them.
 struct Values {
