@@ -463,9 +463,10 @@ typedef struct {
 } gala_kv4_cache;
 size_t gala_kv4_cache_bytes(int pages, int heads, int head_dim);
 /* As gala_kv_append, gala_kv_export, gala_kv_attention_workspace and gala_kv_attention on such a cache, but that a key whose position
- * the rope table does not have is stored as 0.  Attention: the products are those of the codes with their powers of two,
- * exact in bfloat16, with queries as they are (in up to three bfloat16 parts, 24 bits), sums in 32 bits; a weight times its
- * token's scale enters the second product in three bfloat16 parts, 24 bits, where q or out is GALA_F32 or GALA_RESIDUE.  Where
+ * the rope table does not have is stored as 0, and that the rows of a call with count or max_new 0 need no address.
+ * Attention: the products are those of the codes with their powers of two, exact in bfloat16, with queries as they are (in up to three
+ * bfloat16 parts, 24 bits), sums in 32 bits; a weight times its token's scale enters the second product in three bfloat16 parts,
+ * 24 bits, where q or out is GALA_F32 or GALA_RESIDUE.  Where
  * neither is (and |scale| is between 2^-20 and 2^19) it enters in half precision: 11 bits, 22 bits where q or out is GALA_F16 and
  * max_new * heads_q / heads less than 128, in steps of 2^-31 of the largest so far at the most where it is small (a
  * value of zeros counts there as one with a scale of 2^-88); the divisor adds up weights in 32 bits.  Scores have to stay within 32
@@ -499,7 +500,8 @@ typedef enum { GALA_AXES_BLOCKS = 0, GALA_AXES_TURNS = 1, GALA_AXES_OWN = 2 } ga
 int gala_rope_axes_layout(int axes, const int32_t *sections, int order, gala_rope_axes *out);
 /* x, out: rows of heads x head_dim (queries and keys that lie together in a row are heads of one call); out is not GALA_RESIDUE
  * and may be x where the types agree.  at (device memory): row i stands at at[i * at_stride + a] on axis a.  A row that has a
- * position that the table does not have comes out as NaN.  Asynchronous, allocates nothing. */
+ * position that the table does not have comes out as NaN.  Without rows, at, x and out need no address.  Asynchronous,
+ * allocates nothing. */
 int gala_rope_apply(const gala_ctx *ctx, void *stream, const gala_rope_axes *rope, const int32_t *at, int64_t at_stride,
                     int rows, int heads, int head_dim, const gala_values *x, const gala_values *out);
 
@@ -515,7 +517,8 @@ int gala_rope_apply(const gala_ctx *ctx, void *stream, const gala_rope_axes *rop
  * nearest to y / unit, ties to even; with scales (rows x ceil(width / group) floats; group 0: the row) the nearest to y * (1 / scale),
  * scale = max|y| * (1 / limit) over `group` numbers at a time, infinities and NaN aside.  NaN becomes 0, infinities +-limit (0
  * where the scale is 0).  What the next layer returns is then worth scale times the unit of its weights: a scale a row stands
- * outside of the products, one for each group does not.  Asynchronous, allocates nothing. */
+ * outside of the products, one for each group does not.  Without rows, x, add, sum_out, out and scales need no address.  Asynchronous,
+ * allocates nothing. */
 #define GALA_INT8 4
 typedef struct {
     double epsilon;              /* >= 0 */

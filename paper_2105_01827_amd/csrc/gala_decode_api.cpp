@@ -17,9 +17,9 @@ constexpr double kTwoPi = 6.283185307179586476925286766559;
 
 size_t type_size(int type) { return type == GALA_F32 ? 4 : type == GALA_RESIDUE ? 8 : type == GALA_INT8 ? 1 : 2; }
 
-// `row`: numbers of a row; an output's rows must not overlap
-bool values_ok(const gala_values *v, int64_t row, bool output) {
-    if (!v || !v->data || v->type < GALA_F32 || v->type > GALA_RESIDUE || v->stride < (output ? row : 0)) return false;
+// `row`: numbers of a row; an output's rows must not overlap; `any`: whether there are rows; none need no address
+bool values_ok(const gala_values *v, int64_t row, bool output, bool any = true) {
+    if (!v || (any && !v->data) || v->type < GALA_F32 || v->type > GALA_RESIDUE || v->stride < (output ? row : 0)) return false;
     if ((uintptr_t)v->data % type_size(v->type)) return false;
     return v->type != GALA_RESIDUE || (v->unit > 0 && std::isfinite(v->unit));
 }
@@ -71,7 +71,7 @@ bool attention4_ok(const gala_kv4_cache *cache, const gala_kv_batch *batch, int 
 }
 // what a call writes may be what it reads where every number lies at the same place
 bool apart_or_same(const gala_values *a, const gala_values *b) {
-    return !a || !b || a->data != b->data || (a->type == b->type && a->stride == b->stride);
+    return !a || !b || !a->data || a->data != b->data || (a->type == b->type && a->stride == b->stride);
 }
 // workgroups that turn a row's heads, at most: pieces of eight channels, a wavefront's worth each
 int64_t turning(int heads, int dim) { return ((int64_t)heads * ((dim + 7) / 8) + 63) / 64; }
@@ -185,10 +185,11 @@ extern "C" int gala_kv4_append(const gala_ctx *c, void *stream, const gala_kv4_c
     if (!c || !cache4_ok(cache) || !batch_ok(batch) || heads_q < 0 || heads_q > (1 << 20)) return GALA_EARG;
     if (!q != !q_out || !q != !heads_q || !k != !v) return GALA_EARG;
     const int dim = cache->head_dim;
-    if (q && (!values_ok(q, (int64_t)heads_q * dim, false) || !values_ok(q_out, (int64_t)heads_q * dim, true) ||
+    const bool any = batch->count && batch->max_new;
+    if (q && (!values_ok(q, (int64_t)heads_q * dim, false, any) || !values_ok(q_out, (int64_t)heads_q * dim, true, any) ||
               q_out->type == GALA_RESIDUE || !apart_or_same(q, q_out)))
         return GALA_EARG;
-    if (k && (!values_ok(k, (int64_t)cache->heads * dim, false) || !values_ok(v, (int64_t)cache->heads * dim, false) ||
+    if (k && (!values_ok(k, (int64_t)cache->heads * dim, false, any) || !values_ok(v, (int64_t)cache->heads * dim, false, any) ||
               k->type != v->type))
         return GALA_EARG;
     if ((q && k && q->type != k->type) || !rope_ok(rope, dim)) return GALA_EARG;
@@ -197,7 +198,7 @@ extern "C" int gala_kv4_append(const gala_ctx *c, void *stream, const gala_kv4_c
         !fits_launch(of_blocks * cache->heads * 2 + rows * std::max<int64_t>(1, turning(heads_q, dim)), 256))
         return GALA_EARG;
     if (!c->has_device) return GALA_EHIP;
-    if (!batch->count || !batch->max_new || (!q && !k)) return GALA_OK;
+    if (!any || (!q && !k)) return GALA_OK;
     const RopeArgs r{rope ? rope->table : nullptr, rope ? rope->positions : 0, rope ? rope->rot_dim / 2 : 0,
                      rope ? rope->interleaved != 0 : 0};
     return launch_kv4_append(stream, kv4_args(cache, batch), r, heads_q, values(c, q), values(c, q_out), values(c, k),
@@ -208,11 +209,12 @@ extern "C" int gala_kv4_export(const gala_ctx *c, void *stream, const gala_kv4_c
                                const gala_values *k_out, const gala_values *v_out) {
     if (!c || !cache4_ok(cache) || !batch_ok(batch)) return GALA_EARG;
     const int64_t row = (int64_t)cache->heads * cache->head_dim;
-    if (!values_ok(k_out, row, true) || !values_ok(v_out, row, true) || k_out->type != v_out->type) return GALA_EARG;
+    const bool any = batch->count && batch->max_new;
+    if (!values_ok(k_out, row, true, any) || !values_ok(v_out, row, true, any) || k_out->type != v_out->type) return GALA_EARG;
     const int64_t of_blocks = (int64_t)batch->count * ((batch->max_new + 62) / 64 + 1) + 7;
     if (!fits_launch(of_blocks, 256) || !fits_launch(of_blocks * cache->heads * 2, 256)) return GALA_EARG;
     if (!c->has_device) return GALA_EHIP;
-    if (!batch->count || !batch->max_new) return GALA_OK;
+    if (!any) return GALA_OK;
     return launch_kv4_export(stream, kv4_args(cache, batch), values(c, k_out), values(c, v_out)) ? GALA_EHIP : GALA_OK;
 }
 
@@ -227,14 +229,15 @@ extern "C" int gala_kv4_attention(const gala_ctx *c, void *stream, const gala_kv
                                   void *workspace, size_t workspace_bytes) {
     if (!c || !attention4_ok(cache, batch, heads_q, window, sinks) || !std::isfinite(scale)) return GALA_EARG;
     const int64_t row = (int64_t)heads_q * cache->head_dim;
-    if (!values_ok(q, row, false) || !values_ok(out, row, true) || !apart_or_same(q, out)) return GALA_EARG;
+    const bool any = batch->count && batch->max_new;
+    if (!values_ok(q, row, false, any) || !values_ok(out, row, true, any) || !apart_or_same(q, out)) return GALA_EARG;
     const KvArgs kv = kv4_args(cache, batch);
     window = std::min(window, kFarthest), sinks = std::min(sinks, kFarthest);
     const size_t need = kv4_attention_workspace(kv, heads_q, window, sinks);
     if (need && (!workspace || (uintptr_t)workspace % 16)) return GALA_EARG;
     if (workspace_bytes < need) return GALA_ENOMEM;
     if (!c->has_device) return GALA_EHIP;
-    if (!batch->count || !batch->max_new) return GALA_OK;
+    if (!any) return GALA_OK;
     return launch_kv4_attention(stream, kv, heads_q, scale, window, sinks, values(c, q), values(c, out), workspace) ? GALA_EHIP
                                                                                                                     : GALA_OK;
 }
@@ -264,7 +267,7 @@ extern "C" int gala_rope_axes_layout(int axes, const int32_t *sections, int orde
 
 extern "C" int gala_rope_apply(const gala_ctx *c, void *stream, const gala_rope_axes *rope, const int32_t *at, int64_t at_stride,
                                int rows, int heads, int head_dim, const gala_values *x, const gala_values *out) {
-    if (!c || !rope || !at || (uintptr_t)at % 4 || at_stride < 0 || rows < 0 || heads < 1 || heads > (1 << 20) || head_dim < 1 || head_dim > kMaxHeadDim)
+    if (!c || !rope || (rows && !at) || (uintptr_t)at % 4 || at_stride < 0 || rows < 0 || heads < 1 || heads > (1 << 20) || head_dim < 1 || head_dim > kMaxHeadDim)
         return GALA_EARG;
     if (!rope->table || (uintptr_t)rope->table % 8 || rope->positions < 1 || rope->columns < 1 || rope->columns > 256 || rope->rot_dim < 2 ||
         rope->rot_dim % 2 || rope->rot_dim > head_dim || rope->axes < 1 || rope->axes > 4 || rope->reserved)
@@ -272,7 +275,7 @@ extern "C" int gala_rope_apply(const gala_ctx *c, void *stream, const gala_rope_
     for (int i = 0; i < rope->rot_dim / 2; ++i)
         if (rope->axis[i] >= rope->axes || rope->column[i] >= rope->columns) return GALA_EARG;
     const int64_t row = (int64_t)heads * head_dim;
-    if (!values_ok(x, row, false) || !values_ok(out, row, true) || out->type == GALA_RESIDUE || !apart_or_same(x, out)) return GALA_EARG;
+    if (!values_ok(x, row, false, rows) || !values_ok(out, row, true, rows) || out->type == GALA_RESIDUE || !apart_or_same(x, out)) return GALA_EARG;
     if (!fits_launch(rows, 256) || !fits_launch(rows * turning(heads, head_dim), 256)) return GALA_EARG;
     if (!c->has_device) return GALA_EHIP;
     if (!rows) return GALA_OK;
@@ -283,20 +286,20 @@ extern "C" int gala_rms_norm(const gala_ctx *c, void *stream, const gala_norm *h
                              const gala_values *add, const gala_values *sum_out, const gala_values *weight, const gala_values *out) {
     if (!c || !how || rows < 0 || width < 1 || !(how->epsilon >= 0) || !std::isfinite(how->epsilon)) return GALA_EARG;
     if (how->limit < 0 || how->limit >= 1 << 24 || how->group < 0 || (uintptr_t)how->scales % 4) return GALA_EARG;
-    if (!values_ok(x, width, false) || (add && !values_ok(add, width, false)) || (weight && !values_ok(weight, width, false)) ||
-        (weight && weight->type == GALA_RESIDUE) || (sum_out && (!values_ok(sum_out, width, true) || sum_out->type == GALA_RESIDUE)))
+    if (!values_ok(x, width, false, rows) || (add && !values_ok(add, width, false, rows)) || (weight && !values_ok(weight, width, false)) ||
+        (weight && weight->type == GALA_RESIDUE) || (sum_out && (!values_ok(sum_out, width, true, rows) || sum_out->type == GALA_RESIDUE)))
         return GALA_EARG;
     const bool codes = out && out->type == GALA_INT8;
-    if (codes ? (!out->data || out->stride < width || !how->limit || how->limit > 127) : !values_ok(out, width, true)) return GALA_EARG;
+    if (codes ? ((rows && !out->data) || out->stride < width || !how->limit || how->limit > 127) : !values_ok(out, width, true, rows)) return GALA_EARG;
     const bool whole = codes || out->type == GALA_RESIDUE;
     if (!whole && (how->scales || how->limit || how->group)) return GALA_EARG;
-    if (how->group && !how->scales) return GALA_EARG;
+    if (rows && how->group && !how->scales) return GALA_EARG;
     if (codes && !how->scales && !(out->unit > 0 && std::isfinite(out->unit))) return GALA_EARG;
     if (out->type == GALA_RESIDUE && (uint64_t)how->limit > c->p / 2) return GALA_EARG;
     for (const gala_values *written : {out, sum_out})
         for (const gala_values *read : {x, add, weight})
             if (!apart_or_same(written, read)) return GALA_EARG;
-    if ((sum_out && sum_out->data == out->data) || (weight && (weight->data == out->data || (sum_out && sum_out->data == weight->data)))) return GALA_EARG;
+    if ((sum_out && sum_out->data && sum_out->data == out->data) || (weight && (weight->data == out->data || (sum_out && sum_out->data == weight->data)))) return GALA_EARG;
     if (!fits_launch(rows, 1024)) return GALA_EARG;
     if (!c->has_device) return GALA_EHIP;
     if (!rows) return GALA_OK;
