@@ -504,13 +504,11 @@ class Context:
     def rms_norm(self, x, out, add=None, sum_out=None, weight=None, epsilon=1e-6, limit=0, scales=None, group=0, unit=1.0,
                  x_unit=1.0, add_unit=1.0, stream=None):
         """s = x + add into ``sum_out``, its root-mean-square norm times ``weight`` (width numbers) into ``out``: rows of numbers,
-        all of the same width.  ``out`` int8 or residues: whole numbers held to +-limit, of ``unit``, or with ``scales`` (rows, scales of
+        x (rows, width), the others of as many numbers a row.  ``out`` int8 or residues: whole numbers held to +-limit, of ``unit``, or with ``scales`` (rows, scales of
         a row) float32, one for every ``group`` columns (0: for the row)."""
         shape = x.shape
-        if len(shape) != 2:
-            if len(shape) < 2:
-                raise ValueError("x has to hold rows of numbers")
-            shape = (shape[0], math.prod(shape[1:]))
+        if len(shape) != 2:                        # of (batch, tokens, width), say: which of them are a row's is the caller's to say
+            raise ValueError(f"x has to hold rows of numbers, rows x width, not {tuple(shape)}")
         rows, width = shape
         at = 0
         if scales is not None:
