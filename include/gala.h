@@ -509,7 +509,7 @@ int gala_rope_apply(const gala_ctx *ctx, void *stream, const gala_rope_axes *rop
  * each row, and y in whole numbers of few bits, as a layer on ciphertexts takes its inputs.  Sums of a row are
  * carried in 64 bits and the factor rounded to 32; x + add, both products and all that follows are 32-bit operations
  * rounded one by one, so that codes do not depend on the order of a sum.
- * x, add, out: rows of `width` numbers; add NULL for none.  sum_out: s, rounded to its type (not GALA_RESIDUE), NULL where
+ * x, add, out: rows of `width` numbers, 2^30 at most; add NULL for none.  sum_out: s, rounded to its type (not GALA_RESIDUE), NULL where
  * it is not wanted; weight: one row (not GALA_RESIDUE), NULL for 1.  sum_out may be x or add, and out may be any of them, where type and stride
  * agree; out and sum_out may not be the same.
  * out GALA_F32, GALA_F16, GALA_BF16: y; `scales` is NULL then.  Else whole numbers held to +-limit, as int8_t (GALA_INT8, a type

@@ -12,6 +12,7 @@ using namespace gala;
 namespace {
 
 constexpr int kFarthest = 1 << 30;      // no sequence is longer: distances beyond it are cut to it
+constexpr int kWidest = 1 << 30;        // row of a norm: columns and a group beyond them fit 32 bits
 constexpr int kMostTokens = (1 << 24) - 1;      // of a vocabulary: that many weights of 2^40 add up in 64 bits
 constexpr double kTwoPi = 6.283185307179586476925286766559;
 
@@ -284,7 +285,7 @@ extern "C" int gala_rope_apply(const gala_ctx *c, void *stream, const gala_rope_
 
 extern "C" int gala_rms_norm(const gala_ctx *c, void *stream, const gala_norm *how, int rows, int width, const gala_values *x,
                              const gala_values *add, const gala_values *sum_out, const gala_values *weight, const gala_values *out) {
-    if (!c || !how || rows < 0 || width < 1 || !(how->epsilon >= 0) || !std::isfinite(how->epsilon)) return GALA_EARG;
+    if (!c || !how || rows < 0 || width < 1 || width > kWidest || !(how->epsilon >= 0) || !std::isfinite(how->epsilon)) return GALA_EARG;
     if (how->limit < 0 || how->limit >= 1 << 24 || how->group < 0 || (uintptr_t)how->scales % 4) return GALA_EARG;
     if (!values_ok(x, width, false, rows) || (add && !values_ok(add, width, false, rows)) || (weight && !values_ok(weight, width, false)) ||
         (weight && weight->type == GALA_RESIDUE) || (sum_out && (!values_ok(sum_out, width, true, rows) || sum_out->type == GALA_RESIDUE)))
