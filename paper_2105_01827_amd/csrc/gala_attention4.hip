@@ -478,7 +478,7 @@ __device__ __forceinline__ void load_keys(const char *data, int token, int half,
     }
 #pragma unroll
     for (int n = 0; n < (G + 1) / 2; ++n)         // the wanted bytes: the first, and the third for the second tile
-        k.exponent[n] = *(const u32 *)(data + kv4_exponents(G) + W::group(4 * n, half) * 64 + low * 4) >> 8 * high;
+        k.exponent[n] = *(const u32 *)(data + kv4_exponents(G) + W::group(4 * n, half) * 64 + low * 4) >> 8 * high & 0xff00ffu;
 }
 
 // groups of kColumnsOf queries of a head of sequence b, and how many groups' positions it is shorter than max_len
