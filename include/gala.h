@@ -469,8 +469,8 @@ size_t gala_kv4_cache_bytes(int pages, int heads, int head_dim);
  * 24 bits, where q or out is GALA_F32 or GALA_RESIDUE.  Where
  * neither is (and |scale| is between 2^-20 and 2^19) it enters in half precision: 11 bits, 22 bits where q or out is GALA_F16 and
  * max_new * heads_q / heads less than 128, in steps of 2^-31 of the largest so far at the most where it is small (a
- * value of zeros counts there as one with a scale of 2^-88); the divisor adds up weights in 32 bits.  Scores have to stay within 32
- * bits: a query that meets one that does not gives NaN. */
+ * value of zeros counts there as one with a scale of 2^-88); the divisor adds up weights in 32 bits.  Scores are
+ * numbers of 32 bits: a query that meets one above them gives NaN, a key whose score lies below them has no weight. */
 int gala_kv4_append(const gala_ctx *ctx, void *stream, const gala_kv4_cache *cache, const gala_kv_batch *batch,
                     const gala_rope *rope, int heads_q, const gala_values *q, const gala_values *q_out,
                     const gala_values *k, const gala_values *v);
