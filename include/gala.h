@@ -466,11 +466,11 @@ size_t gala_kv4_cache_bytes(int pages, int heads, int head_dim);
  * the rope table does not have is stored as 0, and that the rows of a call with count or max_new 0 need no address.
  * Attention: the products are those of the codes with their powers of two, exact in bfloat16, with queries as they are (in up to three
  * bfloat16 parts, 24 bits), sums in 32 bits; a weight times its token's scale enters the second product in three bfloat16 parts,
- * 24 bits, where q or out is GALA_F32 or GALA_RESIDUE.  Where
- * neither is (and |scale| is between 2^-20 and 2^19) it enters in half precision: 11 bits, 22 bits where q or out is GALA_F16 and
- * max_new * heads_q / heads less than 128, in steps of 2^-31 of the largest so far at the most where it is small (a
- * value of zeros counts there as one with a scale of 2^-88); the divisor adds up weights in 32 bits.  Scores are
- * numbers of 32 bits: a query that meets one above them gives NaN, a key whose score lies below them has no weight. */
+ * 24 bits, where q or out is GALA_F32 or GALA_RESIDUE.  Where neither is (and |scale| is between 2^-20 and 2^19) it enters in half
+ * precision: with 11 bits at least, with 22 where q or out is GALA_F16 and max_new * heads_q / heads less than 128, in steps of 2^-31 of
+ * the largest so far at the most where it is small (a value of zeros counts there as one with a scale of 2^-88); the divisor adds up
+ * weights in 32 bits.  Scores are numbers of 32 bits: a query that meets one above them gives NaN, a key whose score lies below
+ * them has no weight. */
 int gala_kv4_append(const gala_ctx *ctx, void *stream, const gala_kv4_cache *cache, const gala_kv_batch *batch,
                     const gala_rope *rope, int heads_q, const gala_values *q, const gala_values *q_out,
                     const gala_values *k, const gala_values *v);

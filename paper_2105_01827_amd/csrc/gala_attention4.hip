@@ -139,6 +139,10 @@ __device__ __forceinline__ bool load_query(const Attention &a, long row, int hq,
 // the score's initial value in the accumulators.  It enters the second product in half precision, raised so that the largest is
 // between 2^7 and 2^15: 11 bits down to 2^-21 of the largest weight times scale, steps of 2^-31 of it below.  The divisor adds up w / s in
 // 32 bits.
+// A choice: a weight is off by at most 2^-12 of itself, an eighth of the rounding of a bf16 result, whose distance from the exact one grows
+// by less than 1 % (2 x 1000 queries over 2000 tokens: 1.669e-3 root-mean-square, 1.658e-3 rounded from exact ones).  For f16 it is as large
+// as the result's rounding: single tokens have a second part (2.09e-4, the rounding alone), prompts, whose registers do not hold one
+// beside two parts of the queries (253 of 256 at 128 channels), do not (2.84e-4 instead of 2.08e-4).
 constexpr float kRaised = 7, kHighest = 15;      // exponents
 constexpr float kNothing = 0x1p-88f;             // scale of values that are zeros: their weights count in the divisor
 constexpr float kOrdinary = 0x1p14f;             // up to here and down to kNothing w / s stays within 32 bits where its weight matters
@@ -217,8 +221,8 @@ __device__ __forceinline__ void raise_base(V (&x)[N], float most, int lanes, con
 // values along and is cut into three bfloat16 parts, 24 bits; else as above, where f16 comes in or out in two parts, 22 bits: one
 // rounding of a weight is as large as that of an f16 result, and few keys do not average it out.  A wavefront has blocks of its
 // own; a workgroup's wavefronts are joined at the end.
-// Bound by HBM where the cache is large (64 queries of up to 8192 tokens, 424 MB: 86 us, 4.9 TB/s; 131072 tokens, 70 MB: 18 us and 5
-// for the join), by a chain of starts, table, codes where it is not (1000 tokens 8.8 us).  Products of 16 x 16: of few queries most
+// Bound by HBM where the cache is large (64 queries of up to 8192 tokens, 424 MB: 86 us, 4.9 TB/s; 131072 tokens, 70 MB: 22 us
+// with 5 for the join, 24 where none of it is in the last-level cache), by a chain of starts, table, codes where it is not (1000 tokens 8 us).  Products of 16 x 16: of few queries most
 // columns are empty, and a tile of 32 would have twice as many.
 template <int G, int NQ, bool FINE, int kWaves>
 __global__ __launch_bounds__(64 * kWaves, G <= 4 ? 2 : 1) void kv4_attention_kernel(Attention a) {
@@ -445,8 +449,8 @@ __global__ __launch_bounds__(64 * kWaves, G <= 4 ? 2 : 1) void kv4_attention_ker
 // leave less room for the vector ALU between them (23 cycles for half the work, 31 with four multiply-adds; 33 and 35).
 // Keys and values come to the registers straight from memory: through LDS they are loaded once a workgroup, but its wavefronts wait for
 // each other (4 x 4096 queries over 8192 tokens 1671 us against 1600).  Bound by the vector ALU (0.57 of the SIMDs' cycles) and the products
-// (0.38), which the two wavefronts of a SIMD overlap little: 2000 and 1258 queries over 5207 and 3276 tokens, 192 G of operations, 0.8 to 0.9 P
-// a second, 4 x 4096 over 8192 1.03.
+// (0.38), which the two wavefronts of a SIMD overlap little: 2000 and 1258 queries over 5207 and 3276 tokens, 192 G of operations, 216 us
+// (241 from idle clocks), 0.89 P a second, 4 x 4096 over 8192 1.01.
 // Two lanes (halves) have a token's key: of two groups of 32 channels one each, of one left over half.  Product n takes their n-th words.
 template <int G>
 struct WideWords {

@@ -149,7 +149,7 @@ __device__ __forceinline__ Block block_of(const KvArgs &kv, int b, int j) {
 
 // One workgroup: the keys of one head in one touched block.  Four lanes have a token's 32 channels: its largest comes from two
 // exchanges within four lanes, its codes are a word a lane, 16 consecutive bytes a group.  Bound by the wait for rows (half of a wavefront's
-// time); 4 x 2000 tokens of 4 heads of 128 with 16 heads of queries, 74 MB with the export, take 15 us.
+// time); 5609 tokens of four sequences, 4 heads of 128 f16 channels with 16 heads of queries, 61 MB, take 13.0 us where the last-level cache has them, 16.7 from HBM.
 template <int TYPE, int THREADS>
 __device__ void append_keys(const KvArgs &kv, const RopeArgs &rope, const Values &x, bool pieces, int h, const Block &o) {
     const int groups = kv4_groups(kv.dim), count = o.hi - o.lo;
@@ -249,8 +249,8 @@ struct Shares {
     Turns turns;
 };
 
-// Six wavefronts a SIMD where heads are narrow: registers that the compiler takes beyond that cost more than they save (prompts of 4 x 2000
-// 17.1 us against 18.0; eight 17.7).
+// Six wavefronts a SIMD where heads are narrow: registers that the compiler takes beyond that cost more than they save (the
+// prompts above from HBM 16.7 us against 17.7, eight 17.1; from the cache 13.0, 13.0 and 12.6).
 template <int TYPE, int OUT, int THREADS, int MOST>
 __global__ __launch_bounds__(THREADS, MOST == 4 ? 6 : 1) void kv4_append_kernel(KvArgs kv, RopeArgs rope, int heads_q, Values q, Values q_out, Values k, Values v,
                                                              Shares shares, bool pieces) {
@@ -292,8 +292,8 @@ __global__ __launch_bounds__(THREADS, MOST == 4 ? 6 : 1) void kv4_append_kernel(
 }
 
 // One workgroup: the keys or the values of one head in one block of one sequence.  A code times its scale is rounded once, to the output's
-// type.  Values: eight words, turned as they were on their way in, are eight channels of eight tokens.  8000 tokens of 4 heads of
-// 128 f16 channels take 7.4 us (21 MB); blocks of 64 sequences 7.8 us; four pieces under way gain nothing.
+// type.  Values: eight words, turned as they were on their way in, are eight channels of eight tokens.  5810 tokens of 4 heads of
+// 128 f16 channels, 15 MB, take 6.2 us, 7.2 from HBM; blocks of 64 sequences 7.9 us; four pieces under way gain nothing.
 template <int OUT>
 __global__ __launch_bounds__(kThreads) void kv4_export_kernel(KvArgs kv, Values k_out, Values v_out, int blocks, Order order, bool pieces) {
     const int2 unit = order.unit_of(blockIdx.x);

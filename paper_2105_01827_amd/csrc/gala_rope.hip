@@ -1,6 +1,6 @@
 // Rotary positions with several axes into rows of heads: the pair (u, v) of channels becomes (c u - s v, c v + s u) with the cosine and
 // sine of its axis' position.  A read and a write of the rows: bound by HBM (9801 rows of 32 heads of 80 f16 channels, 100 MB, 26 us: 3.8 TB/s; 6000
-// of 32 of 128 in bfloat16, 98 MB, 22.6 us: 4.4), by the launch where rows are few (8 rows 4.4 us).
+// of 32 of 128 in bfloat16, 98 MB, 22.2 us: 4.4), by the launch where rows are few (8 rows 4.2 us).
 #include "gala_rows.h"
 
 using namespace gala;
